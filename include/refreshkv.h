@@ -562,6 +562,102 @@ int rk_decode_step_batched(const rk_geom* geom, const rk_schedule* sched, int32_
                            const int32_t* seq_lens, int32_t max_len, int32_t max_recent,
                            void* const* workspaces, size_t workspace_bytes, void* stream);
 
+/* ---- new tokens on their way into the caches ---------------------------------------------- */
+
+/* Rotary positions.  A head's first rot_dim dims are r / 2 pairs (r = rot_dim), pair i being dims (i, i + r / 2), or
+ * (2i, 2i + 1) where `interleaved` is not 0; at position p they are turned by the angle p * f_i:
+ *     a' = a cos - b sin,   b' = b cos + a sin          (fp32, each product and sum rounded, the result rounded to bf16)
+ * and the dims from r on are copied.  table: fp32 [max_pos, rot_dim], 16-byte aligned: row p holds the r / 2 cosines, then the r / 2
+ * sines (rk_rope_table, or a caller's own).  A position outside [0, max_pos) turns the pairs into NaN.
+ * rot_dim: a multiple of 16, at most 128 (RK_ERR_UNSUPPORTED otherwise). */
+typedef struct rk_rope {
+    const float* table;
+    int32_t max_pos;
+    int32_t rot_dim;
+    int32_t interleaved;
+} rk_rope;
+
+/* Frequencies of the table: f_i = base^(-2i / rot_dim), scaled for contexts longer than those of the training:
+ *   original_len <= 0: every f_i is divided by `factor`;
+ *   original_len > 0:  by the turns t = original_len * f_i / (2 pi) that a pair makes within it: divided by `factor` where
+ *                      t <= low_turns, kept where t >= high_turns, and the two mixed linearly in t between
+ *                      (low_turns < high_turns).
+ * amplitude multiplies cosines and sines (1: none). */
+typedef struct rk_rope_scaling {
+    double base;
+    double factor;
+    double low_turns, high_turns;
+    double original_len;
+    double amplitude;
+} rk_rope_scaling;
+
+/* Fills the table of an rk_rope; angles, cosines and sines in fp64, rounded once. */
+int rk_rope_table(float* table, int32_t max_pos, int32_t rot_dim, const rk_rope_scaling* scaling, void* stream);
+
+/* Query, key and value rows of n_new new tokens per sequence, bf16: row (b, t, head) of q is at q + b * q_stride_b + t * q_stride_t +
+ * head * 128 (k, v likewise), so that they may be parts of one projection's output.  16-byte aligned, strides in elements,
+ * non-negative multiples of 8. */
+typedef struct rk_new_rows {
+    const void* q;         /* [batch, n_new, n_q_heads, 128], or NULL: none                        */
+    const void* k;         /* [batch, n_new, n_kv_heads, 128]                                      */
+    const void* v;
+    int64_t q_stride_b, q_stride_t;
+    int64_t k_stride_b, k_stride_t;
+    int64_t v_stride_b, v_stride_t;
+    int32_t n_new;
+} rk_new_rows;
+
+/* Rotary positions of new tokens and their way into the full cache (what the caller of a decode step has to do before it).
+ * Sequence b has n = new_lens[b] new tokens (new_lens: device int32[batch], clamped to [0, n_new]; NULL: n_new of each), entries 0 .. n-1
+ * of its rows; entry i is row r = seq_lens[b] - n + i of the cache (seq_lens counts the new tokens), and its position is r, or
+ * positions[b * n_new + i] where positions (device int32 [batch, n_new]) is given.
+ *   q_out[b, i, h, :] = q turned           bf16 [batch, n_new, n_q_heads, 128] contiguous, 16-byte aligned; may be q itself
+ *   cache.k[b, g, r, :] = k turned,  cache.v[b, g, r, :] = v
+ * rope NULL: nothing is turned (q must be NULL then: it would be a copy).  Entries beyond n, and all other rows of the cache, are
+ * left as they were; rows outside [0, cache.capacity) are not written (their q is). */
+int rk_rope_append(const rk_geom* geom, const rk_new_rows* rows, const rk_rope* rope, const int32_t* positions,
+                   rk_kv cache, const int32_t* seq_lens, const int32_t* new_lens, void* q_out,
+                   const int32_t* pred, int32_t pred_val, void* stream);
+
+/* ---- a cache of 8 bits ---------------------------------------------------------------------- */
+
+#define RK_Q8_E4M3 0           /* 8-bit floating point: 4 bits of exponent, 3 of mantissa, largest 448, no infinities */
+#define RK_Q8_INT8 1           /* whole numbers -127 .. 127                                       */
+
+/* A KV cache at half the bytes of rk_kv.  Rows are kept in blocks of `block` tokens.  A row of a block that is full stands for
+ * scale * k8[row, :], with one fp32 scale per (sequence, KV head, block); the rows of the block that is not full yet (row >=
+ * len / block * block in a sequence of len rows) are in `k_tail` as bf16, at slot row % block.  (So the cache depends on
+ * the rows that it was given and not on how many came at a time, and every row is rounded to 8 bits once.)
+ *   k, v       8-bit [batch, n_kv_heads, capacity, 128], strides in elements (non-negative multiples of 16, stride_h below 2^31),
+ *              16-byte aligned; capacity a multiple of block
+ *   k_scale..  fp32 [batch, n_kv_heads, capacity / block] contiguous
+ *   k_tail ..  bf16 [batch, n_kv_heads, block, 128] contiguous, 16-byte aligned
+ *   block      16, 32, 64 or 128;  format RK_Q8_* (RK_ERR_UNSUPPORTED otherwise) */
+typedef struct rk_kv8 {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    void* k_tail;
+    void* v_tail;
+    int64_t stride_b;
+    int64_t stride_h;
+    int64_t capacity;
+    int32_t block;
+    int32_t format;
+} rk_kv8;
+
+/* rk_rope_append into a cache of 8 bits.  New rows of a block that is not full go to the tail; a block that fills is quantised, the
+ * rows that were there already being taken from the tail: with a its largest magnitude (of the bf16 rows, keys turned),
+ *   scale = the smallest power of two, at least 2^-126, with a <= M * scale (M = 448 or 127);  1 for a block of zeros,
+ *   k8 = k / scale (exact), rounded to the nearest value of the format, ties to even.
+ * A block with an infinity or a NaN gets a NaN as its scale (and zeros), so that whatever is computed from it is NaN.
+ * The rows before the new ones must have been put there the same way: a sequence can be shortened and continued only within the
+ * rows of the block that is not full. */
+int rk_rope_append_q8(const rk_geom* geom, const rk_new_rows* rows, const rk_rope* rope, const int32_t* positions,
+                      const rk_kv8* cache, const int32_t* seq_lens, const int32_t* new_lens, void* q_out,
+                      const int32_t* pred, int32_t pred_val, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

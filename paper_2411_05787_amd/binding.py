@@ -18,7 +18,8 @@ LIB_PATH = os.path.join(HERE, "librefreshkv.so")
 
 EXPORTS = ["rk_version", "rk_status_string", "rk_workspace_bytes", "rk_workspace_init",
            "rk_full_attn", "rk_full_attn_scores", "rk_topk_select", "rk_full_attn_select", "rk_full_attn_pool", "rk_full_attn_deferred", "rk_select_pooled", "rk_score_select", "rk_window_select", "rk_gather_small_kv", "rk_partial_attn", "rk_partial_attn_static", "rk_partial_attn_static_bytes", "rk_partial_attn_fixed", "rk_partial_attn_lazy", "rk_gather_attn", "rk_partial_attn_triggered", "rk_decode_step", "rk_decode_step_overlapped", "rk_refresh_batched", "rk_decode_step_batched",
-           "rk_query_sim", "rk_mark_refresh", "rk_calibration_copy", "rk_calibration_read", "rk_debug_set_slice_spin", "rk_h2o_append", "rk_h2o_update", "rk_h2o_step"]
+           "rk_query_sim", "rk_mark_refresh", "rk_calibration_copy", "rk_calibration_read", "rk_debug_set_slice_spin", "rk_h2o_append", "rk_h2o_update", "rk_h2o_step",
+           "rk_rope_table", "rk_rope_append", "rk_rope_append_q8"]
 
 RK_AGG_MAX, RK_AGG_MEAN, RK_AGG_FIRST = 0, 1, 2
 
@@ -58,6 +59,27 @@ class _Overlap(C.Structure):
     _fields_ = [("side_stream", C.c_void_p), ("ready", C.POINTER(C.c_void_p)), ("done", C.POINTER(C.c_void_p)),
                 ("join", C.c_void_p), ("workspaces", C.POINTER(C.c_void_p)), ("n_workspaces", C.c_int32),
                 ("workspace_bytes", C.c_size_t)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("max_pos", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class _RopeScaling(C.Structure):
+    _fields_ = [("base", C.c_double), ("factor", C.c_double), ("low_turns", C.c_double), ("high_turns", C.c_double),
+                ("original_len", C.c_double), ("amplitude", C.c_double)]
+
+
+class _NewRows(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_t", C.c_int64),
+                ("k_stride_b", C.c_int64), ("k_stride_t", C.c_int64), ("v_stride_b", C.c_int64), ("v_stride_t", C.c_int64),
+                ("n_new", C.c_int32)]
+
+
+class _Kv8(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_tail", C.c_void_p),
+                ("v_tail", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("capacity", C.c_int64),
+                ("block", C.c_int32), ("format", C.c_int32)]
 
 
 STEP_KINDS = {1: "full", 2: "partial", 3: "both"}
@@ -139,6 +161,12 @@ def _load(path: str = LIB_PATH) -> C.CDLL:
     l.rk_h2o_update.restype = C.c_int
     l.rk_h2o_step.argtypes = [G, _H2oState, P, P, P, P, I32, I32, I32, P, P, P, SZ, P]
     l.rk_h2o_step.restype = C.c_int
+    l.rk_rope_table.argtypes = [P, I32, I32, C.POINTER(_RopeScaling), P]
+    l.rk_rope_table.restype = C.c_int
+    l.rk_rope_append.argtypes = [G, C.POINTER(_NewRows), C.POINTER(_Rope), P, _Kv, P, P, P, P, I32, P]
+    l.rk_rope_append.restype = C.c_int
+    l.rk_rope_append_q8.argtypes = [G, C.POINTER(_NewRows), C.POINTER(_Rope), P, C.POINTER(_Kv8), P, P, P, P, I32, P]
+    l.rk_rope_append_q8.restype = C.c_int
     return l
 
 
@@ -707,3 +735,155 @@ def rk_decode_step_batched(geom: Geom, sched: _Schedule, t: int, layers, q_ptrs,
     if rc <= 0:
         _check("rk_decode_step_batched", rc if rc < 0 else -1)
     return STEP_KINDS[rc]
+
+
+# ---- new tokens on their way into the caches ----
+
+class Rope:
+    """A table of rotary positions (fp32 [max_pos, rot_dim]: cosines, then sines; see rope_table) and the layout of the pairs."""
+
+    def __init__(self, table: torch.Tensor, interleaved: bool = False):
+        if table.dim() != 2:
+            raise ValueError("table must be [max_pos, rot_dim]")
+        self.table, self.interleaved = table, bool(interleaved)
+        self.rot_dim = table.shape[1]
+        self._c = _Rope(_dev(table, torch.float32, "table"), table.shape[0], table.shape[1], int(self.interleaved))
+
+
+def rope_table(max_pos: int, rot_dim: int, base: float = 10000.0, factor: float = 1.0, low_turns: float = 0.0, high_turns: float = 0.0,
+               original_len: float = 0, amplitude: float = 1.0, device="cuda", stream=None) -> torch.Tensor:
+    """The table of a Rope, made on the GPU (rk_rope_table says what the numbers mean)."""
+    if max_pos < 1 or rot_dim < 1:
+        raise ValueError("max_pos and rot_dim must be positive")
+    table = torch.empty(int(max_pos), int(rot_dim), dtype=torch.float32, device=device)
+    with torch.cuda.device(table.device):
+        rk_rope_table(table, base, factor, low_turns, high_turns, original_len, amplitude, stream=stream)
+    return table
+
+
+def rk_rope_table(table: torch.Tensor, base: float = 10000.0, factor: float = 1.0, low_turns: float = 0.0, high_turns: float = 0.0,
+                  original_len: float = 0, amplitude: float = 1.0, stream=None) -> None:
+    if table.dim() != 2:
+        raise ValueError("table must be [max_pos, rot_dim]")
+    s = _RopeScaling(float(base), float(factor), float(low_turns), float(high_turns), float(original_len), float(amplitude))
+    _check("rk_rope_table", lib.rk_rope_table(_dev(table, torch.float32, "table"), table.shape[0], table.shape[1], C.byref(s), _stream(stream)))
+
+
+Q8_FORMATS = {torch.float8_e4m3fn: 0, torch.int8: 1}
+
+
+class Kv8:
+    """A cache of 8 bits (rk_kv8): k, v float8_e4m3fn or int8 [B, Hkv, capacity, 128]; k_scale, v_scale fp32 [B, Hkv, capacity / block];
+    k_tail, v_tail bf16 [B, Hkv, block, 128], which give the block."""
+
+    def __init__(self, geom: Geom, k, v, k_scale, v_scale, k_tail, v_tail):
+        B, H, D = geom.batch, geom.n_kv_heads, geom.head_dim
+        for t, n in ((k, "k"), (v, "v")):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in Q8_FORMATS:
+                raise ValueError("%s must be a float8_e4m3fn or int8 tensor in GPU memory" % n)
+            if t.dim() != 4 or t.shape[0] != B or t.shape[1] != H or t.shape[3] != D:
+                raise ValueError("%s must be [batch, n_kv_heads, capacity, head_dim], got %s" % (n, tuple(t.shape)))
+            if t.stride(3) != 1 or t.stride(2) != D:
+                raise ValueError("%s rows must be contiguous" % n)
+        if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("k and v must share type, shape and strides")
+        if k_tail.dim() != 4:
+            raise ValueError("k_tail must be [batch, n_kv_heads, block, head_dim]")
+        cap, block = k.shape[2], k_tail.shape[2]
+        if block < 1 or cap % block:
+            raise ValueError("the capacity %d must be whole blocks of %d" % (cap, block))
+        self.geom, self.capacity, self.block = geom, cap, block
+        self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail = k, v, k_scale, v_scale, k_tail, v_tail
+        self._c = _Kv8(k.data_ptr(), v.data_ptr(), _dev(k_scale, torch.float32, "k_scale", (B, H, cap // block)),
+                       _dev(v_scale, torch.float32, "v_scale", (B, H, cap // block)),
+                       _dev(k_tail, torch.bfloat16, "k_tail", (B, H, block, D)), _dev(v_tail, torch.bfloat16, "v_tail", (B, H, block, D)),
+                       k.stride(0), k.stride(1), cap, block, Q8_FORMATS[k.dtype])
+        _same_device(k, v, k_scale, v_scale, k_tail, v_tail)
+
+    @classmethod
+    def empty(cls, geom: Geom, capacity: int, block: int = 32, dtype=torch.float8_e4m3fn, device="cuda") -> "Kv8":
+        """A cache with room for `capacity` rows (rounded up to whole blocks) and nothing in it."""
+        B, H, D = geom.batch, geom.n_kv_heads, geom.head_dim
+        cap = (int(capacity) + block - 1) // block * block
+        new = lambda shape, t: torch.zeros(shape, dtype=t, device=device)  # noqa: E731
+        return cls(geom, *(torch.zeros(B, H, cap, D, dtype=torch.uint8, device=device).view(dtype) for _ in range(2)),
+                   *(new((B, H, cap // block), torch.float32) for _ in range(2)), *(new((B, H, block, D), torch.bfloat16) for _ in range(2)))
+
+
+def _same_device(*tensors) -> torch.device:
+    """The device of all of them (None: absent)."""
+    d = None
+    for t in tensors:
+        if t is not None:
+            if d is None:
+                d = t.device
+            elif t.device != d:
+                raise ValueError("tensors on %s and %s: one call takes one device" % (d, t.device))
+    return d
+
+
+def _launch(name: str, device: torch.device, stream, *args) -> None:
+    """Calls the library with `device` the current one, on its current stream unless another is given."""
+    fn = getattr(lib, name)
+    if _device is not None and _device() == device.index:
+        return _check(name, fn(*args, _stream(stream)))
+    with torch.cuda.device(device):
+        _check(name, fn(*args, _stream(stream)))
+
+
+def _rows(t: torch.Tensor, B: int, T: int, H: int, D: int, name: str) -> tuple:
+    """Pointer and strides of [B, T, H, D] whose heads lie side by side."""
+    if t.__class__ is not _Tensor and not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError("%s must be a bf16 tensor in GPU memory" % name)
+    if tuple(t.shape) != (B, T, H, D):
+        raise ValueError("%s must have shape %s, got %s" % (name, (B, T, H, D), tuple(t.shape)))
+    sb, st, sh, sd = t.stride()
+    if (sd != 1 and D > 1) or (sh != D and H > 1):
+        raise ValueError("%s: the heads of a token must lie side by side" % name)
+    return t.data_ptr(), sb if B > 1 else 0, st if T > 1 else 0
+
+
+def _new_rows(geom: Geom, q, k, v, rope, positions, seq_lens, new_lens, q_out):
+    B, Hq, H, D = geom.batch, geom.n_q_heads, geom.n_kv_heads, geom.head_dim
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("k must be [batch, n_new, n_kv_heads, head_dim]")
+    T = k.shape[1]
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None and rope is None:
+        raise ValueError("q without a rope would be a copy")
+    qp = (None, 0, 0) if q is None else _rows(q, B, T, Hq, D, "q")
+    kp, vp = _rows(k, B, T, H, D, "k"), _rows(v, B, T, H, D, "v")
+    rows = _NewRows(qp[0], kp[0], vp[0], qp[1], qp[2], kp[1], kp[2], vp[1], vp[2], T)
+    return (C.byref(rows), None if rope is None else C.byref(rope._c), _dev(positions, torch.int32, "positions", (B, T), optional=True),
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True),
+            _dev(q_out, torch.bfloat16, "q_out", (B, T, Hq, D), optional=True))
+
+
+def rk_rope_append(geom: Geom, q, k, v, rope: Optional[Rope], K, V, seq_lens, q_out, new_lens=None, positions=None,
+                   pred=None, pred_val: int = 0, stream=None) -> None:
+    """q bf16 [B, T, Hq, D] (or None, with q_out), k, v [B, T, Hkv, D], the heads of a token side by side (any strides between tokens and
+    sequences); K, V: the full cache; q_out bf16 [B, T, Hq, D] (may be q)."""
+    rows, r, pos, lens, new, qo = _new_rows(geom, q, k, v, rope, positions, seq_lens, new_lens, q_out)
+    dev = _same_device(k, q, v, None if rope is None else rope.table, K, V, seq_lens, q_out, new_lens, positions, pred)
+    _launch("rk_rope_append", dev, stream, C.byref(geom.c()), rows, r, pos, _kv(geom, K, V, "cache"), lens, new, qo,
+            _dev(pred, torch.int32, "pred", (geom.batch,), optional=True), int(pred_val))
+
+
+def rk_rope_append_q8(geom: Geom, q, k, v, rope: Optional[Rope], cache: Kv8, seq_lens, q_out, new_lens=None, positions=None,
+                      pred=None, pred_val: int = 0, stream=None) -> None:
+    """rk_rope_append into a cache of 8 bits."""
+    rows, r, pos, lens, new, qo = _new_rows(geom, q, k, v, rope, positions, seq_lens, new_lens, q_out)
+    dev = _same_device(k, q, v, None if rope is None else rope.table, _cache8(geom, cache), seq_lens, q_out, new_lens, positions, pred)
+    _launch("rk_rope_append_q8", dev, stream, C.byref(geom.c()), rows, r, pos, C.byref(cache._c), lens, new, qo,
+            _dev(pred, torch.int32, "pred", (geom.batch,), optional=True), int(pred_val))
+
+
+def _cache8(geom: Geom, cache: Kv8) -> torch.Tensor:
+    """One tensor of the cache, once it is known to be of this geometry."""
+    if not isinstance(cache, Kv8):
+        raise ValueError("cache must be a Kv8")
+    g = cache.geom
+    if (g.batch, g.n_kv_heads, g.head_dim) != (geom.batch, geom.n_kv_heads, geom.head_dim):
+        raise ValueError("the cache is of another geometry")
+    return cache.k
