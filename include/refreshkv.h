@@ -658,6 +658,22 @@ int rk_rope_append_q8(const rk_geom* geom, const rk_new_rows* rows, const rk_rop
                       const rk_kv8* cache, const int32_t* seq_lens, const int32_t* new_lens, void* q_out,
                       const int32_t* pred, int32_t pred_val, void* stream);
 
+/* rk_full_attn over a cache of 8 bits: half the bytes of the step that is bound by them.  The scores, weights and output of
+ * rk_full_attn over the rows that the cache stands for (any scales; scores and sums in fp32, the weights that multiply V kept to 2^-17).
+ * Rows of the block that is not full are taken from the tail, so seq_lens must be what the cache was filled to.  `weights` (optional) go to
+ * rk_topk_select as those of rk_full_attn do.  Arguments as in rk_full_attn; workspace of rk_workspace_bytes(geom, max_len, ..). */
+int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8* full, const int32_t* seq_lens, int32_t max_len,
+                    void* out, float* weights, int64_t w_stride, float* lse,
+                    const int32_t* pred, int32_t pred_val,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* rk_gather_small_kv out of a cache of 8 bits into a bf16 small cache: small.k[b,g,i,:] = the row idx[b,g,i] as the cache stands for it,
+ * rounded to bf16 (exact where the scale is a power of two; bit copies from the tail).  Slots whose idx is outside
+ * [0, seq_lens[b]) are left untouched.  seq_lens is required; tail_start (optional) <- seq_lens. */
+int rk_gather_small_kv_q8(const rk_geom* geom, const rk_kv8* full, const int32_t* idx, int32_t k, rk_kv small,
+                          const int32_t* seq_lens, int32_t* tail_start,
+                          const int32_t* pred, int32_t pred_val, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

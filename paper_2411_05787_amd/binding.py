@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(HERE, "librefreshkv.so")
 EXPORTS = ["rk_version", "rk_status_string", "rk_workspace_bytes", "rk_workspace_init",
            "rk_full_attn", "rk_full_attn_scores", "rk_topk_select", "rk_full_attn_select", "rk_full_attn_pool", "rk_full_attn_deferred", "rk_select_pooled", "rk_score_select", "rk_window_select", "rk_gather_small_kv", "rk_partial_attn", "rk_partial_attn_static", "rk_partial_attn_static_bytes", "rk_partial_attn_fixed", "rk_partial_attn_lazy", "rk_gather_attn", "rk_partial_attn_triggered", "rk_decode_step", "rk_decode_step_overlapped", "rk_refresh_batched", "rk_decode_step_batched",
            "rk_query_sim", "rk_mark_refresh", "rk_calibration_copy", "rk_calibration_read", "rk_debug_set_slice_spin", "rk_h2o_append", "rk_h2o_update", "rk_h2o_step",
-           "rk_rope_table", "rk_rope_append", "rk_rope_append_q8"]
+           "rk_rope_table", "rk_rope_append", "rk_rope_append_q8", "rk_full_attn_q8", "rk_gather_small_kv_q8"]
 
 RK_AGG_MAX, RK_AGG_MEAN, RK_AGG_FIRST = 0, 1, 2
 
@@ -167,6 +167,10 @@ def _load(path: str = LIB_PATH) -> C.CDLL:
     l.rk_rope_append.restype = C.c_int
     l.rk_rope_append_q8.argtypes = [G, C.POINTER(_NewRows), C.POINTER(_Rope), P, C.POINTER(_Kv8), P, P, P, P, I32, P]
     l.rk_rope_append_q8.restype = C.c_int
+    l.rk_full_attn_q8.argtypes = [G, P, C.POINTER(_Kv8), P, I32, P, P, I64, P, P, I32, P, SZ, P]
+    l.rk_full_attn_q8.restype = C.c_int
+    l.rk_gather_small_kv_q8.argtypes = [G, C.POINTER(_Kv8), P, I32, _Kv, P, P, P, I32, P]
+    l.rk_gather_small_kv_q8.restype = C.c_int
     return l
 
 
@@ -887,3 +891,31 @@ def _cache8(geom: Geom, cache: Kv8) -> torch.Tensor:
     if (g.batch, g.n_kv_heads, g.head_dim) != (geom.batch, geom.n_kv_heads, geom.head_dim):
         raise ValueError("the cache is of another geometry")
     return cache.k
+
+
+def rk_full_attn_q8(geom: Geom, q, cache: Kv8, seq_lens, max_len: int, out, weights=None, lse=None, pred=None, pred_val: int = 0,
+                    workspace: Workspace = None, stream=None) -> None:
+    """rk_full_attn over a cache of 8 bits."""
+    B, Hq, D = geom.batch, geom.n_q_heads, geom.head_dim
+    dev = _same_device(_cache8(geom, cache), q, seq_lens, out, weights, lse, pred)
+    if max_len > cache.capacity:
+        raise ValueError("max_len %d exceeds the cache capacity %d" % (max_len, cache.capacity))
+    w_stride = 0
+    if weights is not None:
+        if weights.dim() != 3 or weights.shape[0] != B or weights.shape[1] != Hq or weights.shape[2] < max_len:
+            raise ValueError("weights must be [batch, n_q_heads, >= max_len]")
+        w_stride = weights.shape[2]
+    _launch("rk_full_attn_q8", dev, stream, C.byref(geom.c()), _dev(q, torch.bfloat16, "q", (B, Hq, D)), C.byref(cache._c),
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), int(max_len), _dev(out, torch.bfloat16, "out", (B, Hq, D)),
+            _dev(weights, torch.float32, "weights", optional=True), w_stride, _dev(lse, torch.float32, "lse", (B, Hq), optional=True),
+            _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val), workspace.ptr, workspace.nbytes)
+
+
+def rk_gather_small_kv_q8(geom: Geom, cache: Kv8, idx, k: int, small_K, small_V, seq_lens, tail_start=None, pred=None, pred_val: int = 0,
+                          stream=None) -> None:
+    """rk_gather_small_kv out of a cache of 8 bits."""
+    B, Hkv = geom.batch, geom.n_kv_heads
+    dev = _same_device(_cache8(geom, cache), idx, small_K, small_V, seq_lens, tail_start, pred)
+    _launch("rk_gather_small_kv_q8", dev, stream, C.byref(geom.c()), C.byref(cache._c), _dev(idx, torch.int32, "idx", (B, Hkv, k)), int(k),
+            _kv(geom, small_K, small_V, "small", min_rows=k), _dev(seq_lens, torch.int32, "seq_lens", (B,)),
+            _dev(tail_start, torch.int32, "tail_start", (B,), optional=True), _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val))

@@ -44,79 +44,6 @@
 
 namespace rk {
 
-// Work split of the split kernels.  The rows of a (sequence, KV head) are cut into tiles of 32;
-// tile t belongs to wavefront t % 4 of workgroup (t / 4) % nch, so workgroup c starts at row
-// 128 c and the tiles go round the nch * 4 wavefronts of the launch: every wavefront gets the
-// same number of tiles, give or take one, whatever the length, and at any moment the launch
-// streams one contiguous stretch of the cache.  Workgroups whose first row is past the end do
-// nothing; the others each leave one partial result (the merge takes any subsets of the rows).
-__device__ __forceinline__ int active_workgroups(int n_rows, int nch) {
-    return max(1, min(nch, (n_rows + kSplitWaves * kTileRows - 1) / (kSplitWaves * kTileRows)));
-}
-
-// Ragged batches.  With nch workgroups for every sequence, whatever its length, a launch that is
-// resident as a whole takes as long as its longest sequence.  Score-emitting launches over
-// 2..kRaggedMaxBatch sequences therefore share the nch * batch workgroups of a KV head out in
-// proportion to the lengths: sequence i gets a_i = 1 + its share of the other nch * batch - batch by
-// the largest-remainder rule (at least one, at most one per 128 rows and share_cap; the a_i add up
-// to no more than there are), and workgroup z * nch + x of the grid is number (that minus the a_j before it) of
-// the sequence it falls into; those past the sum do nothing.  Every workgroup derives the same a_i from
-// seq_lens: exact arithmetic (fp64 on whole numbers below 2^46), one wavefront, lane i for sequence i.  All of
-// the launch waits for it before its first request, so it keeps to the data-parallel operand path and scalar
-// registers (64-bit integer division and shuffles through LDS took 0.6 us longer).
-// The kernels that read the partial results do not repeat it: the first workgroup of every (sequence, KV head)
-// of such a launch leaves their number in its counter line (kCountWord).  16 ragged sequences of 10k rows, us per launch: output merge
-// 7.8 -> 6.2, pooling of 4 layers 54 -> 45.
-__device__ __forceinline__ int clamped_len(int raw, int cap, int max_rows) { return min(max(min(raw, cap), 0), max_rows); }
-__device__ __forceinline__ double lane_of(double v, int lane) {          // (lane: the same in all lanes)
-    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
-}
-
-// Lane i < batch: a_i.  Other lanes: 0.  Called by whole wavefronts.  APPEND: the rows kept so far and one more.
-template <bool APPEND>
-__device__ __forceinline__ int ragged_share_lane(const AttnParams& p, const int32_t* seq_lens) {
-    const int lane = threadIdx.x & 63, batch = p.ragged_batch, nch = p.nch, share_cap = p.share_cap;
-    const int raw = lane < batch ? seq_lens[lane] : 0;
-    const int len = lane >= batch ? 0 : APPEND ? min(min(max(raw, 0), p.cap1 - 1) + 1, p.n_sel) : clamped_len(raw, p.cap2, p.max_rows2);
-    const double total = wave_sum((double)len);
-    int a = 1;
-    if (total > 0.0) {
-        const int spare = nch * batch - batch;                 // at most kMaxChunks * kRaggedMaxBatch
-        const double num = (double)spare * (double)len;
-        double fl = floor(num / total);
-        double rem = fma(-fl, total, num);                     // exact; the quotient may have been rounded across a whole number
-        if (rem < 0.0) { fl -= 1.0; rem += total; }
-        if (rem >= total) { fl += 1.0; rem -= total; }
-        // what the floors leave over goes, one each, to the largest remainders (ties: lower sequence first)
-        const int left = spare - (int)wave_sum(fl);            // 0 <= left < batch
-        int rank = 0;
-        for (int j = 0; j < batch; ++j) {
-            const double rj = lane_of(rem, j);
-            rank += (rj > rem || (rj == rem && j < lane)) ? 1 : 0;
-        }
-        a += (int)fl + (rank < left ? 1 : 0);
-    }
-    a = min(a, min(share_cap, max(1, (len + kSplitWaves * kTileRows - 1) / (kSplitWaves * kTileRows))));
-    return lane < batch ? a : 0;
-}
-
-// Sequence, number within it and share of the workgroup at `slot` (b < 0: none).
-struct RaggedSlot { int b, c, nchunks; };
-template <bool APPEND>
-__device__ __forceinline__ RaggedSlot ragged_slot(const AttnParams& p, const int32_t* seq_lens, int slot) {
-    const int a = ragged_share_lane<APPEND>(p, seq_lens);
-    const int incl = (int)wave_inclusive_scan((uint32_t)a);
-    const int before = incl - a;
-    const unsigned long long hit = __ballot(a > 0 && before <= slot && slot < incl);
-    RaggedSlot r{-1, 0, 0};
-    if (hit != 0) {
-        r.b = __ffsll(hit) - 1;
-        r.c = slot - __builtin_amdgcn_readlane(before, r.b);
-        r.nchunks = __builtin_amdgcn_readlane(a, r.b);
-    }
-    return r;
-}
-
 __device__ __forceinline__ void coherent_store2(float* p, float a, float b) {
     const uint64_t v = (uint64_t)__float_as_uint(a) | ((uint64_t)__float_as_uint(b) << 32);
     __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -1496,7 +1423,9 @@ __device__ __forceinline__ void block_head_lse(const AttnParams& p, int G, int64
     const double L64 = block_sum_f64<4>((double)wgt * (double)l, reinterpret_cast<double*>(s.red));
     if (tid == 0) {
         float hi = -INFINITY, lo = 0.f;
-        if (L64 > 0.0 && fp32_log) {
+        if (p.keep_nan != 0 && L64 != L64) {
+            hi = (float)L64;
+        } else if (L64 > 0.0 && fp32_log) {
             hi = M + __logf((float)L64);
         } else if (L64 > 0.0) {
             const double l64 = (double)M + log(L64);
@@ -1544,7 +1473,7 @@ __device__ __forceinline__ void block_head_out(const AttnParams& p, int G, int b
     __syncthreads();
     if (tid < kD) {
         const float L = (float)s.L64;
-        const float o = L > 0.f ? (s.acc[0][tid] + s.acc[1][tid] + s.acc[2][tid] + s.acc[3][tid]) / L : 0.f;
+        const float o = L > 0.f || (p.keep_nan != 0 && L != L) ? (s.acc[0][tid] + s.acc[1][tid] + s.acc[2][tid] + s.acc[3][tid]) / L : 0.f;
         p.out[((int64_t)b * p.Hq + h) * kD + tid] = f32_to_bf16(o);
     }
     if (tid == 0) p.lse[(int64_t)b * p.Hq + h] = s.lse[0];
@@ -2005,11 +1934,7 @@ int full_attn_stage(const rk_geom* geom, const void* q, rk_kv full, const int32_
                   : launch_split<true, false>(p, geom->batch, G, nchunk_grid, st);
     }
     if (rc != RK_OK || scores_only) return rc;
-    if (!fused) {
-        dim3 grid(1 + (max_len + kNormTile - 1) / kNormTile, geom->n_q_heads, geom->batch);
-        hipLaunchKernelGGL(merge_normalise_kernel, grid, dim3(256), 0, st, p, G);
-        return launch_status();
-    }
+    if (!fused) return merge_weights_stage(p, geom->batch, max_len, st);
     if (defer_pool) {            // only the output is finished now; pool_batched_stage does the rest later
         if (merge_inside) return rc;
         p.weights = nullptr;
@@ -2028,6 +1953,13 @@ int full_attn_stage(const rk_geom* geom, const void* q, rk_kv full, const int32_
         case 8: return launch_finish_pool<8>(p, geom->batch, max_len, ws, pool_half, agg, st);
         default: return RK_ERR_UNSUPPORTED;
     }
+}
+
+// The launch that ends a step whose split kernel left raw scores in p.weights (or none) and partial results: merge, lse, weights.
+int merge_weights_stage(const AttnParams& p, int batch, int32_t max_len, hipStream_t st) {
+    const dim3 grid(p.weights ? 1 + (max_len + kNormTile - 1) / kNormTile : 1, p.Hq, batch);
+    hipLaunchKernelGGL(merge_normalise_kernel, grid, dim3(256), 0, st, p, p.Hq / p.Hkv);
+    return launch_status();
 }
 
 // The attention of an H2O step: raw scores to ws.scores, partial results to ws.part_ml / part_o, n_attend[b] set.

@@ -35,6 +35,7 @@ struct AttnParams {
     int32_t* mark_tail; int32_t* mark_count;  // the gather inside the step only: tail_start <- seq_lens, refreshes counted (may be NULL)
     int32_t ragged_batch;              // != 0 (= batch): workgroups are shared out by length, see ragged_share_lane
     int32_t share_cap;                 // ... at most this many to a sequence
+    int32_t keep_nan;                  // the merge leaves NaN where the sums are NaN (0: zeros, as the steps over bf16 caches have it)
     int32_t* n_attend;                 // APPEND only: [B], rows attended over, for the kernel that follows
     int32_t slice_merge;               // TAGGED: every workgroup merges a slice of the output (all workgroups of the launch are resident together)
     int32_t slice_spin;                // ... re-reading rows still in flight at most this often before it leaves its slice to the last one
@@ -45,9 +46,86 @@ struct AttnParams {
 __attribute__((visibility("hidden")))
 int launch_partial_tile(const AttnParams& p, int batch, int G, const TileForm& form, bool trig, const int32_t* idx, hipStream_t st);
 
+// The launch that merges a split kernel's partial results and turns the raw scores in p.weights (may be NULL) into weights.
+__attribute__((visibility("hidden")))
+int merge_weights_stage(const AttnParams& p, int batch, int32_t max_len, hipStream_t st);
+
 constexpr int kSplitWaves = 4, kTileRows = 32;
 constexpr int kNoTailWg = 0xff;                   // top byte of the kernel argument s_b_and_tail: no workgroup for the tail rows
 constexpr int kHeadsFirst = 0xfe;                 // ... (launches over the full cache only) grid x = KV head, y = sequence, z = chunk
+
+// Work split of the split kernels.  The rows of a (sequence, KV head) are cut into tiles of 32;
+// tile t belongs to wavefront t % 4 of workgroup (t / 4) % nch, so workgroup c starts at row
+// 128 c and the tiles go round the nch * 4 wavefronts of the launch: every wavefront gets the
+// same number of tiles, give or take one, whatever the length, and at any moment the launch
+// streams one contiguous stretch of the cache.  Workgroups whose first row is past the end do
+// nothing; the others each leave one partial result (the merge takes any subsets of the rows).
+__device__ __forceinline__ int active_workgroups(int n_rows, int nch) {
+    return max(1, min(nch, (n_rows + kSplitWaves * kTileRows - 1) / (kSplitWaves * kTileRows)));
+}
+
+// Ragged batches.  With nch workgroups for every sequence, whatever its length, a launch that is
+// resident as a whole takes as long as its longest sequence.  Score-emitting launches over
+// 2..kRaggedMaxBatch sequences therefore share the nch * batch workgroups of a KV head out in
+// proportion to the lengths: sequence i gets a_i = 1 + its share of the other nch * batch - batch by
+// the largest-remainder rule (at least one, at most one per 128 rows and share_cap; the a_i add up
+// to no more than there are), and workgroup z * nch + x of the grid is number (that minus the a_j before it) of
+// the sequence it falls into; those past the sum do nothing.  Every workgroup derives the same a_i from
+// seq_lens: exact arithmetic (fp64 on whole numbers below 2^46), one wavefront, lane i for sequence i.  All of
+// the launch waits for it before its first request, so it keeps to the data-parallel operand path and scalar
+// registers (64-bit integer division and shuffles through LDS took 0.6 us longer).
+// The kernels that read the partial results do not repeat it: the first workgroup of every (sequence, KV head)
+// of such a launch leaves their number in its counter line (kCountWord).  16 ragged sequences of 10k rows, us per launch: output merge
+// 7.8 -> 6.2, pooling of 4 layers 54 -> 45.
+__device__ __forceinline__ int clamped_len(int raw, int cap, int max_rows) { return min(max(min(raw, cap), 0), max_rows); }
+__device__ __forceinline__ double lane_of(double v, int lane) {          // (lane: the same in all lanes)
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+
+// Lane i < batch: a_i.  Other lanes: 0.  Called by whole wavefronts.  APPEND: the rows kept so far and one more.
+template <bool APPEND>
+__device__ __forceinline__ int ragged_share_lane(const AttnParams& p, const int32_t* seq_lens) {
+    const int lane = threadIdx.x & 63, batch = p.ragged_batch, nch = p.nch, share_cap = p.share_cap;
+    const int raw = lane < batch ? seq_lens[lane] : 0;
+    const int len = lane >= batch ? 0 : APPEND ? min(min(max(raw, 0), p.cap1 - 1) + 1, p.n_sel) : clamped_len(raw, p.cap2, p.max_rows2);
+    const double total = wave_sum((double)len);
+    int a = 1;
+    if (total > 0.0) {
+        const int spare = nch * batch - batch;                 // at most kMaxChunks * kRaggedMaxBatch
+        const double num = (double)spare * (double)len;
+        double fl = floor(num / total);
+        double rem = fma(-fl, total, num);                     // exact; the quotient may have been rounded across a whole number
+        if (rem < 0.0) { fl -= 1.0; rem += total; }
+        if (rem >= total) { fl += 1.0; rem -= total; }
+        // what the floors leave over goes, one each, to the largest remainders (ties: lower sequence first)
+        const int left = spare - (int)wave_sum(fl);            // 0 <= left < batch
+        int rank = 0;
+        for (int j = 0; j < batch; ++j) {
+            const double rj = lane_of(rem, j);
+            rank += (rj > rem || (rj == rem && j < lane)) ? 1 : 0;
+        }
+        a += (int)fl + (rank < left ? 1 : 0);
+    }
+    a = min(a, min(share_cap, max(1, (len + kSplitWaves * kTileRows - 1) / (kSplitWaves * kTileRows))));
+    return lane < batch ? a : 0;
+}
+
+// Sequence, number within it and share of the workgroup at `slot` (b < 0: none).
+struct RaggedSlot { int b, c, nchunks; };
+template <bool APPEND>
+__device__ __forceinline__ RaggedSlot ragged_slot(const AttnParams& p, const int32_t* seq_lens, int slot) {
+    const int a = ragged_share_lane<APPEND>(p, seq_lens);
+    const int incl = (int)wave_inclusive_scan((uint32_t)a);
+    const int before = incl - a;
+    const unsigned long long hit = __ballot(a > 0 && before <= slot && slot < incl);
+    RaggedSlot r{-1, 0, 0};
+    if (hit != 0) {
+        r.b = __ffsll(hit) - 1;
+        r.c = slot - __builtin_amdgcn_readlane(before, r.b);
+        r.nchunks = __builtin_amdgcn_readlane(a, r.b);
+    }
+    return r;
+}
 
 // All global stores this thread issued so far are acknowledged once this returns.
 __device__ __forceinline__ void wait_stores_acknowledged() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }

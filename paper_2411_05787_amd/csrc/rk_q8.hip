@@ -1,0 +1,211 @@
+// rk_full_attn_q8 and rk_gather_small_kv_q8: the full step and the refresh over a cache of 8 bits.
+//
+// The step streams 256 bytes of a KV head's row instead of 512 and is bound by that: what the matrix cores and the conversions take
+// fits behind it.  The scale of a block of rows multiplies its scores (K) and its weights (V), never the rows.  Split, work shares of
+// ragged batches, the layout of the partial results and the kernel that merges them and normalises the weights are those of the step over
+// the bf16 cache (rk_attn_common.h).
+#include "rk_cols.h"
+
+namespace rk {
+
+struct Q8Rows { const uint8_t *k, *v; const float *ks, *vs; const uint16_t *kt, *vt; int64_t s_b; int32_t s_h, blocks, shift; };
+
+// Tiles of a sequence of len rows (of which the call looks at the first n): those of whole blocks, then those of the tail.
+template <int FORMAT, bool EMIT>
+__global__ __launch_bounds__(kColWaves * 64, 2)
+void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
+    const int g = blockIdx.y;
+    int b = blockIdx.z, c = blockIdx.x, nchunks = 0;
+    if (p.ragged_batch != 0) {
+        const RaggedSlot slot = ragged_slot<false>(p, p.seq_lens, (int)(blockIdx.z * gridDim.x + blockIdx.x));
+        if (slot.b < 0) return;
+        b = slot.b; c = slot.c; nchunks = slot.nchunks;
+    }
+    if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
+    const int len = min(max(p.seq_lens[b], 0), p.cap2), n = min(len, p.max_rows2);
+    if (p.ragged_batch == 0) {
+        nchunks = active_workgroups(n, p.nch);
+        if (c >= nchunks) return;
+    }
+    const int G = p.Hq / p.Hkv;
+    const int64_t bg = (int64_t)b * p.Hkv + g;
+    if (p.ragged_batch != 0 && c == 0 && threadIdx.x == 0) store_chunks(p.counters, bg, nchunks);
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, gr = lane >> 4;
+    const int full = len >> c8.shift << c8.shift, main_rows = min(n, full);
+    const int main_tiles = (main_rows + kTileRows - 1) / kTileRows, tiles = main_tiles + (n - main_rows + kTileRows - 1) / kTileRows;
+    const uint8_t* k = c8.k + b * c8.s_b + (int64_t)g * c8.s_h;
+    const uint8_t* v = c8.v + b * c8.s_b + (int64_t)g * c8.s_h;
+    const float* ks = c8.ks + bg * c8.blocks;
+    const float* vs = c8.vs + bg * c8.blocks;
+
+    bf16x8 q[4];                              // (columns beyond the group repeat its last head: they are never looked at)
+    const uint16_t* qr = p.q + ((int64_t)b * p.Hq + g * G + min(col, G - 1)) * kD;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qr + operand_dim<true>(s, gr));
+
+    ColState st;
+    st.clear();
+    float* wrow = EMIT ? p.weights + ((int64_t)b * p.Hq + g * G + min(col, G - 1)) * p.w_stride : nullptr;
+    // scores of rows first .. first + 31, the first `rows` of which exist
+    auto finish_scores = [&](float (&s)[2][4], int first, int rows, float k0, float k1) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[x][i] *= x ? k1 : k0;
+            const int r = 16 * x + 4 * gr;
+            if (EMIT && col < G) {
+                float* to = wrow + first + r;
+                if (p.w_vec != 0 && r + 4 <= rows) {
+                    *reinterpret_cast<float4*>(to) = make_float4(s[x][0], s[x][1], s[x][2], s[x][3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (r + i < rows) to[i] = s[x][i];
+                }
+            }
+            if (rows < kTileRows) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[x][i] = r + i < rows ? s[x][i] : -INFINITY;
+            }
+        }
+        tile_softmax(st, s);
+    };
+    const int t0 = c * kColWaves + w, step = nchunks * kColWaves;
+    TileRows<FORMAT> rows;
+    int t = t0;
+    if (t < main_tiles) {
+        request_keys<FORMAT, true, true>(rows, k, (int64_t)t * kTileRows, main_rows - 1);
+        request_values<FORMAT, true>(rows, v, (int64_t)t * kTileRows, main_rows - 1);
+    }
+    for (; t < main_tiles; t += step) {
+        const int first = t * kTileRows, second = min(first + 16, main_rows - 1);
+        const float k0 = ks[first >> c8.shift] * p.scale, k1 = ks[second >> c8.shift] * p.scale;
+        const float v0 = vs[first >> c8.shift], v1 = vs[second >> c8.shift];
+        float s[2][4];
+        tile_scores<FORMAT>(rows, q, s);
+        const bool more = t + step < main_tiles;
+        if (more) request_keys<FORMAT, true, true>(rows, k, (int64_t)(t + step) * kTileRows, main_rows - 1);
+        finish_scores(s, first, main_rows - first, k0, k1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { s[0][i] *= v0; s[1][i] = main_rows - first > 16 ? s[1][i] * v1 : 0.f; }
+        bf16x8 hi, lo;
+        weight_operands(s, hi, lo);
+        tile_output<FORMAT>(rows, st, hi, lo);
+        if (more) request_values<FORMAT, true>(rows, v, (int64_t)(t + step) * kTileRows, main_rows - 1);
+    }
+    for (; t < tiles; t += step) {            // the block that is not full: bf16
+        const int at = (t - main_tiles) * kTileRows, left = n - main_rows - at;
+        const uint16_t* kt = c8.kt + (bg << c8.shift) * kD;
+        const uint16_t* vt = c8.vt + (bg << c8.shift) * kD;
+        TileRows<kBf16> x;
+        request_keys<kBf16, false, true>(x, kt, at, n - main_rows - 1);
+        request_values<kBf16, false>(x, vt, at, n - main_rows - 1);
+        float s[2][4];
+        tile_scores<kBf16>(x, q, s);
+        finish_scores(s, main_rows + at, left, p.scale, p.scale);
+        bf16x8 hi, lo;
+        weight_operands(s, hi, lo);
+        tile_output<kBf16>(x, st, hi, lo);
+    }
+
+    __shared__ __attribute__((aligned(16))) ColMergeLds lds;
+    float* po = p.part_o + (bg * p.max_chunks + c) * G * kD;
+    float* ml = p.part_ml + (bg * kMaxChunks + c) * G * 2;
+    merge_columns(lds, st, G,
+                  [&](int x, int d, float o0, float o1) { *reinterpret_cast<float2*>(po + x * kD + d) = make_float2(o0, o1); },
+                  [&](int x, float m, float l) { *reinterpret_cast<float2*>(ml + 2 * x) = make_float2(m, l); });
+}
+
+// rk_gather_small_kv out of a cache of 8 bits: 16 lanes to a row.
+constexpr int kGatherRows8 = 16;
+template <int FORMAT>
+__global__ __launch_bounds__(256)
+void gather_q8_kernel(const rk_kv8 c8, uint16_t* __restrict__ sk, uint16_t* __restrict__ sv, int64_t ss_b, int64_t ss_h,
+                      const int32_t* __restrict__ idx, int32_t k, int32_t Hkv, const int32_t* __restrict__ seq_lens,
+                      int32_t* __restrict__ tail_start, const int32_t* pred, int32_t pred_val) {
+    const int g = blockIdx.y, b = blockIdx.z;
+    if (pred != nullptr && pred[b] != pred_val) return;
+    const int raw = seq_lens[b];
+    if (tail_start != nullptr && blockIdx.x == 0 && g == 0 && threadIdx.x == 0) tail_start[b] = raw;
+    const int i = blockIdx.x * kGatherRows8 + (threadIdx.x >> 4);
+    if (i >= k) return;
+    const int64_t bg = (int64_t)b * Hkv + g;
+    const int j = idx[bg * k + i], len = (int)min((int64_t)max(raw, 0), c8.capacity), full = len / c8.block * c8.block;
+    if (j < 0 || j >= len) return;
+    const int seg = (threadIdx.x & 15) * 8;
+    const int64_t to = (int64_t)b * ss_b + (int64_t)g * ss_h + (int64_t)i * kD + seg;
+    u32x4 row[2];
+    if (j >= full) {
+        const int64_t at = (bg * c8.block + (j - full)) * kD + seg;
+        row[0] = *reinterpret_cast<const u32x4*>((const uint16_t*)c8.k_tail + at);
+        row[1] = *reinterpret_cast<const u32x4*>((const uint16_t*)c8.v_tail + at);
+    } else {
+        const int64_t at = (int64_t)b * c8.stride_b + (int64_t)g * c8.stride_h + (int64_t)j * kD + seg;
+        const int64_t block = bg * (c8.capacity / c8.block) + j / c8.block;
+        const uint2 w[2] = {*reinterpret_cast<const uint2*>((const uint8_t*)c8.k + at), *reinterpret_cast<const uint2*>((const uint8_t*)c8.v + at)};
+        const float scale[2] = {c8.k_scale[block], c8.v_scale[block]};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            // (a value of the format has at most 8 bits: its product with a power of two is a bf16, with another scale it is rounded)
+            const uint32_t v[4] = {pair_of<FORMAT, false>(w[x].x), pair_of<FORMAT, true>(w[x].x), pair_of<FORMAT, false>(w[x].y), pair_of<FORMAT, true>(w[x].y)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) row[x][e] = pack_bf16(bf16_lo(v[e]) * scale[x], bf16_hi(v[e]) * scale[x]);
+        }
+    }
+    *reinterpret_cast<u32x4*>(sk + to) = row[0];
+    *reinterpret_cast<u32x4*>(sv + to) = row[1];
+}
+
+}  // namespace rk
+
+using namespace rk;
+
+extern "C" int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8* full, const int32_t* seq_lens, int32_t max_len,
+                               void* out, float* weights, int64_t w_stride, float* lse, const int32_t* pred, int32_t pred_val,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_geom(geom);
+    if (rc != RK_OK) return rc;
+    if (!q || !out || !seq_lens || max_len <= 0 || !aligned16(q) || ((uintptr_t)out & 1u)) return RK_ERR_INVALID_ARG;
+    if ((rc = check_kv8(full)) != RK_OK) return rc;
+    if (weights && (w_stride < max_len || ((uintptr_t)weights & 3u))) return RK_ERR_INVALID_ARG;
+    Workspace ws;
+    if ((rc = check_workspace(geom, max_len, 0, workspace, workspace_bytes, &ws)) != RK_OK) return rc;
+    const int G = geom->n_q_heads / geom->n_kv_heads;
+    AttnParams p{};
+    p.q = (const uint16_t*)q;
+    p.seq_lens = seq_lens; p.max_rows2 = max_len; p.cap2 = (int32_t)full->capacity;
+    p.nch = emit_split_workgroups(geom, max_len);
+    p.Hq = geom->n_q_heads; p.Hkv = geom->n_kv_heads;
+    p.scale = geom->scale;
+    p.out = (uint16_t*)out;
+    p.weights = weights; p.w_stride = w_stride; p.w_vec = weights && w_stride % 4 == 0 && aligned16(weights) ? 1 : 0;
+    p.lse = lse ? lse : ws.lse;
+    p.pred = pred; p.pred_val = pred_val;
+    p.counters = ws.counters; p.part_ml = ws.part_ml; p.part_o = ws.part_o; p.max_chunks = ws.max_chunks;
+    p.ragged_batch = ragged_batch_of(geom); p.share_cap = kMaxChunks;
+    p.keep_nan = 1;                           // (a block that held one has NaN as its scale)
+    const Q8Rows rows{(const uint8_t*)full->k, (const uint8_t*)full->v, full->k_scale, full->v_scale, (const uint16_t*)full->k_tail,
+                      (const uint16_t*)full->v_tail, full->stride_b, (int32_t)full->stride_h, (int32_t)(full->capacity / full->block),
+                      full->block == 16 ? 4 : full->block == 32 ? 5 : full->block == 64 ? 6 : 7};
+    const dim3 grid(p.nch, geom->n_kv_heads, geom->batch);
+    const bool e4m3 = full->format == RK_Q8_E4M3;
+    auto kernel = e4m3 ? (weights ? q8_attn_kernel<RK_Q8_E4M3, true> : q8_attn_kernel<RK_Q8_E4M3, false>)
+                       : (weights ? q8_attn_kernel<RK_Q8_INT8, true> : q8_attn_kernel<RK_Q8_INT8, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(kColWaves * 64), 0, (hipStream_t)stream, p, rows);
+    if ((rc = launch_status()) != RK_OK) return rc;
+    return merge_weights_stage(p, geom->batch, max_len, (hipStream_t)stream);
+}
+
+extern "C" int rk_gather_small_kv_q8(const rk_geom* geom, const rk_kv8* full, const int32_t* idx, int32_t k, rk_kv small,
+                                     const int32_t* seq_lens, int32_t* tail_start, const int32_t* pred, int32_t pred_val, void* stream) {
+    int rc = check_geom(geom);
+    if (rc != RK_OK) return rc;
+    if (!idx || k <= 0 || !seq_lens) return RK_ERR_INVALID_ARG;
+    if ((rc = check_kv8(full)) != RK_OK) return rc;
+    if ((rc = check_kv(small)) != RK_OK) return rc;
+    if (small.capacity < k) return RK_ERR_INVALID_ARG;
+    auto kernel = full->format == RK_Q8_E4M3 ? gather_q8_kernel<RK_Q8_E4M3> : gather_q8_kernel<RK_Q8_INT8>;
+    hipLaunchKernelGGL(kernel, dim3((k + kGatherRows8 - 1) / kGatherRows8, geom->n_kv_heads, geom->batch), dim3(256), 0, (hipStream_t)stream,
+                       *full, (uint16_t*)small.k, (uint16_t*)small.v, small.stride_b, small.stride_h, idx, k, geom->n_kv_heads, seq_lens,
+                       tail_start, pred, pred_val);
+    return launch_status();
+}
