@@ -674,6 +674,43 @@ int rk_gather_small_kv_q8(const rk_geom* geom, const rk_kv8* full, const int32_t
                           const int32_t* seq_lens, int32_t* tail_start,
                           const int32_t* pred, int32_t pred_val, void* stream);
 
+/* ---- attention of new tokens ---------------------------------------------------------------- */
+
+/* What rk_prompt_attn does with the scores (a NULL pointer to it: the plain causal step).
+ *   cap     > 0: the score x = scale * <q, k> becomes cap * tanh(x / cap);  0: as it is
+ *   slopes  device fp32 [n_q_heads] or NULL: minus slopes[h] * |position of the token - row|, after the cap
+ *   first, end  device int32 [batch, n_new] or NULL: token i of sequence b sees the rows first[b,i] <= j < end[b,i] of the cache.  NULL: from
+ *           row 0, and up to its own row.  Packed documents: first = the row where the token's document starts.  A prefix that sees itself
+ *           both ways: end = the larger of the token's row + 1 and the prefix's end.  A window: first = the token's row - width + 1.
+ *           first == end (or beyond): the token sees nothing. */
+typedef struct rk_prompt_scores {
+    float cap;
+    const float* slopes;
+    const int32_t* first;
+    const int32_t* end;
+} rk_prompt_scores;
+
+/* Bytes of scratch that rk_prompt_attn needs for up to n_new new tokens per sequence and up to max_len rows (256-byte aligned
+ * device memory; nothing in it needs to be initialised, and nothing is kept there between calls).  Host-only; 0: invalid. */
+size_t rk_prompt_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t max_len);
+
+/* Attention of the new tokens of each sequence over its rows in the cache, their own among them (rk_rope_append has put them there): a whole
+ * prompt, a chunk of one behind what is cached already, drafted tokens, or a decode step's single token.
+ * Tokens are numbered and placed as in rk_rope_append: sequence b has n = new_lens[b] of them (clamped to [0, n_new]; NULL: n_new), entry i is
+ * row and position p = seq_lens[b] - n + i.  For query head h (KV head g = h / G), over the rows j that the token sees, j < min(seq_lens[b],
+ * max_len, capacity):
+ *     s[j] = scale * <q[b,i,h,:], K[b,g,j,:]>   (capped, less the bias)
+ *     out[b,i,h,:] = sum_j softmax(s)[j] * V[b,g,j,:]          lse[b,i,h] = log sum_j exp(s[j])
+ *   q    bf16, row (b, i, h) at q + b * q_stride_b + i * q_stride_t + h * 128; 16-byte aligned, strides multiples of 8
+ *   out  bf16 [batch, n_new, n_q_heads, 128] contiguous, 16-byte aligned;  lse fp32 [batch, n_new, n_q_heads] or NULL
+ * A token that sees no row gets out = 0 and lse = -inf; entries beyond n are left as they were.  Rows that a token does not see have no part in its
+ * result, whatever they hold (infinities and NaN included; one that it sees makes its output infinite or NaN).  With more than 16 / G new tokens the softmax weights enter the product with V as
+ * bf16 (sums in fp32), with fewer to 2^-17. */
+int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, rk_kv cache,
+                   const int32_t* seq_lens, const int32_t* new_lens, int32_t max_len, const rk_prompt_scores* scores,
+                   void* out, float* lse, const int32_t* pred, int32_t pred_val,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

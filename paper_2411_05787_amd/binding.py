@@ -19,7 +19,8 @@ LIB_PATH = os.path.join(HERE, "librefreshkv.so")
 EXPORTS = ["rk_version", "rk_status_string", "rk_workspace_bytes", "rk_workspace_init",
            "rk_full_attn", "rk_full_attn_scores", "rk_topk_select", "rk_full_attn_select", "rk_full_attn_pool", "rk_full_attn_deferred", "rk_select_pooled", "rk_score_select", "rk_window_select", "rk_gather_small_kv", "rk_partial_attn", "rk_partial_attn_static", "rk_partial_attn_static_bytes", "rk_partial_attn_fixed", "rk_partial_attn_lazy", "rk_gather_attn", "rk_partial_attn_triggered", "rk_decode_step", "rk_decode_step_overlapped", "rk_refresh_batched", "rk_decode_step_batched",
            "rk_query_sim", "rk_mark_refresh", "rk_calibration_copy", "rk_calibration_read", "rk_debug_set_slice_spin", "rk_h2o_append", "rk_h2o_update", "rk_h2o_step",
-           "rk_rope_table", "rk_rope_append", "rk_rope_append_q8", "rk_full_attn_q8", "rk_gather_small_kv_q8"]
+           "rk_rope_table", "rk_rope_append", "rk_rope_append_q8", "rk_full_attn_q8", "rk_gather_small_kv_q8",
+           "rk_prompt_workspace_bytes", "rk_prompt_attn"]
 
 RK_AGG_MAX, RK_AGG_MEAN, RK_AGG_FIRST = 0, 1, 2
 
@@ -80,6 +81,10 @@ class _Kv8(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_tail", C.c_void_p),
                 ("v_tail", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("capacity", C.c_int64),
                 ("block", C.c_int32), ("format", C.c_int32)]
+
+
+class _PromptScores(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("first", C.c_void_p), ("end", C.c_void_p)]
 
 
 STEP_KINDS = {1: "full", 2: "partial", 3: "both"}
@@ -171,6 +176,10 @@ def _load(path: str = LIB_PATH) -> C.CDLL:
     l.rk_full_attn_q8.restype = C.c_int
     l.rk_gather_small_kv_q8.argtypes = [G, C.POINTER(_Kv8), P, I32, _Kv, P, P, P, I32, P]
     l.rk_gather_small_kv_q8.restype = C.c_int
+    l.rk_prompt_workspace_bytes.restype = SZ
+    l.rk_prompt_workspace_bytes.argtypes = [G, I32, I32]
+    l.rk_prompt_attn.argtypes = [G, P, I64, I64, I32, _Kv, P, P, I32, C.POINTER(_PromptScores), P, P, P, I32, P, SZ, P]
+    l.rk_prompt_attn.restype = C.c_int
     return l
 
 
@@ -919,3 +928,41 @@ def rk_gather_small_kv_q8(geom: Geom, cache: Kv8, idx, k: int, small_K, small_V,
     _launch("rk_gather_small_kv_q8", dev, stream, C.byref(geom.c()), C.byref(cache._c), _dev(idx, torch.int32, "idx", (B, Hkv, k)), int(k),
             _kv(geom, small_K, small_V, "small", min_rows=k), _dev(seq_lens, torch.int32, "seq_lens", (B,)),
             _dev(tail_start, torch.int32, "tail_start", (B,), optional=True), _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val))
+
+
+def rk_prompt_workspace_bytes(geom: Geom, n_new: int, max_len: int) -> int:
+    n = int(lib.rk_prompt_workspace_bytes(C.byref(geom.c()), int(n_new), int(max_len)))
+    if n == 0:
+        raise RkError("rk_prompt_workspace_bytes", -1)
+    return n
+
+
+class PromptWorkspace:
+    """Scratch of rk_prompt_attn for up to n_new new tokens per sequence and max_len rows; nothing in it outlives a call."""
+
+    def __init__(self, geom: Geom, n_new: int, max_len: int, device="cuda"):
+        self.geom, self.n_new, self.max_len = geom, int(n_new), int(max_len)
+        self.nbytes = rk_prompt_workspace_bytes(geom, n_new, max_len)
+        self.buf = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
+        self.ptr = (self.buf.data_ptr() + 255) // 256 * 256
+
+
+def rk_prompt_attn(geom: Geom, q, K, V, seq_lens, max_len: int, out, new_lens=None, first=None, end=None, cap: float = 0.0, slopes=None,
+                   lse=None, pred=None, pred_val: int = 0, workspace: PromptWorkspace = None, stream=None) -> None:
+    """q bf16 [B, T, Hq, D], the heads of a token side by side (any strides between tokens and sequences); out bf16 [B, T, Hq, D];
+    first, end int32 [B, T]; slopes fp32 [Hq]; lse fp32 [B, T, Hq]."""
+    B, Hq, D = geom.batch, geom.n_q_heads, geom.head_dim
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be [batch, n_new, n_q_heads, head_dim]")
+    T = q.shape[1]
+    dev = _same_device(q, K, V, seq_lens, out, new_lens, first, end, slopes, lse, pred, None if workspace is None else workspace.buf)
+    qp, sb, st = _rows(q, B, T, Hq, D, "q")
+    if max_len > K.shape[2]:
+        raise ValueError("max_len %d exceeds the cache capacity %d" % (max_len, K.shape[2]))
+    scores = _PromptScores(float(cap), _dev(slopes, torch.float32, "slopes", (Hq,), optional=True),
+                           _dev(first, torch.int32, "first", (B, T), optional=True), _dev(end, torch.int32, "end", (B, T), optional=True))
+    ws, nb = (None, 0) if workspace is None else (workspace.ptr, workspace.nbytes)
+    _launch("rk_prompt_attn", dev, stream, C.byref(geom.c()), qp, sb, st, T, _kv(geom, K, V, "cache"),
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(max_len),
+            C.byref(scores), _dev(out, torch.bfloat16, "out", (B, T, Hq, D)), _dev(lse, torch.float32, "lse", (B, T, Hq), optional=True),
+            _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val), ws, nb)

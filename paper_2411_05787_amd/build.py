@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librefreshkv.so")
 BIND = os.path.join(HERE, "_rkbind.so")               # argument marshalling of the short calls (csrc/rk_bind.cpp), linked against LIB
 SOURCES = ["rk_api.hip", "rk_attn.hip", "rk_partial.hip", "rk_topk.hip", "rk_gather.hip", "rk_query_sim.hip", "rk_step.hip",
-           "rk_window.hip", "rk_h2o.hip", "rk_rope.hip", "rk_q8.hip"]
+           "rk_window.hip", "rk_h2o.hip", "rk_rope.hip", "rk_q8.hip", "rk_prompt.hip"]
 # Packed fp32 VALU forms are switched off for every device compilation of this library.
 HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
