@@ -1,9 +1,8 @@
 // Rotary positions of new tokens, and their rows into the full cache: rk_rope_table, rk_rope_append, rk_rope_append_q8.
 //
 // A pass reads every new row once and writes it once; there is nothing to reuse but a token's cosines and sines, which all of its
-// heads share.  Eight lanes take a row of 256 bytes, two chunks of eight dims each: in the half layout chunk c and its partner
-// c + rot_dim / 16, which hold the two halves of eight pairs; in the interleaved one, and among the dims that are not turned, two
-// neighbouring chunks.  So a pair never leaves its lane, a turn needs no exchange, and q_out may be q.
+// heads share.  Eight lanes take a row of 256 bytes, two chunks of eight dims each: in the half layout the two halves of eight pairs, in the
+// interleaved one any.  So a pair never leaves its lane, a turn needs no exchange, and q_out may be q.
 #include "rk_q8.h"
 
 namespace rk {
@@ -19,21 +18,46 @@ struct RopeParams {
     uint16_t *ck, *cv; int64_t c_b, c_h; int32_t capacity;       // the bf16 cache
     rk_kv8 c8;                                                   // the one of 8 bits
     const int32_t* pred; int32_t pred_val;
-    int32_t team_rows, teams_per_token;       // rows of a token that eight lanes take one after the other
+    int32_t rows_per_token;                   // that token_row takes
     int32_t block_wgs;                        // 8 bits: workgroups ahead of those with q rows
 };
 
-// Eight pairs' cosines and sines, and the two chunks that they turn.  Products and sums are rounded one by one: what is quantised
-// later must not depend on which of them a compiler fuses.
-struct Turn { float c[8], s[8]; };
+// Products and sums are rounded one by one: what is quantised later must not depend on which of them a compiler fuses.
 __device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) {
 #pragma clang fp contract(off)
     const float x = a * c, y = b * s, z = b * c, w = a * s;
     a = x - y;
     b = z + w;
 }
-// Chunks of a lane: the half layout's pairs are (lo[i], hi[i]); the interleaved one's neighbours within lo, then within hi.
-__device__ __forceinline__ void turn_chunks(u32x4& lo, u32x4& hi, const Turn& t, bool interleaved) {
+
+// What lane c of the eight has of a row: the dims where its two chunks start, 64 or rot / 2 apart, so that the eight lanes' chunks lie side by
+// side.  Half layout: lo and hi are the halves of eight pairs, or both are not turned.  Interleaved: each is four pairs, or is not turned.
+struct LaneDims { int lo, hi; bool turn_lo, turn_hi; };
+__device__ __forceinline__ LaneDims lane_dims(int c, const RopeParams& p) {
+    const int pairs = p.rot >> 4;             // lanes whose chunks are turned in the half layout
+    if (p.interleaved) return {c * 8, 64 + c * 8, c * 8 < p.rot, 64 + c * 8 < p.rot};
+    if (c < pairs) return {c * 8, (p.rot >> 1) + c * 8, true, true};
+    return {(c + pairs) * 8, 64 + c * 8, false, false};
+}
+// Cosines and sines of a lane's eight pairs: pairs lo .. lo + 7 of the half layout, lo / 2 .. + 3 and hi / 2 .. + 3 of the interleaved one.
+struct Turn { float c[8], s[8]; };
+__device__ __forceinline__ void load_turn(Turn& t, const RopeParams& p, int pos, const LaneDims& d) {
+    const bool known = (uint32_t)pos < (uint32_t)p.max_pos;
+    const float* row = p.table + (int64_t)(known ? pos : 0) * p.rot;
+    const int a = p.interleaved ? d.lo >> 1 : d.lo, b = p.interleaved ? d.hi >> 1 : d.lo + 4;
+    float4 x[4] = {};
+    if (d.turn_lo) { x[0] = *reinterpret_cast<const float4*>(row + a); x[2] = *reinterpret_cast<const float4*>(row + (p.rot >> 1) + a); }
+    if (d.turn_hi) { x[1] = *reinterpret_cast<const float4*>(row + b); x[3] = *reinterpret_cast<const float4*>(row + (p.rot >> 1) + b); }
+    const float nan = __uint_as_float(0x7fc00000u);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        t.c[4 * i] = x[i].x; t.c[4 * i + 1] = x[i].y; t.c[4 * i + 2] = x[i].z; t.c[4 * i + 3] = x[i].w;
+        t.s[4 * i] = x[2 + i].x; t.s[4 * i + 1] = x[2 + i].y; t.s[4 * i + 2] = x[2 + i].z; t.s[4 * i + 3] = x[2 + i].w;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { t.c[i] = known ? t.c[i] : nan; t.s[i] = known ? t.s[i] : nan; }
+}
+__device__ __forceinline__ void turn_chunks(u32x4& lo, u32x4& hi, const Turn& t, const LaneDims& d, bool interleaved) {
     float a[8], b[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -52,37 +76,9 @@ __device__ __forceinline__ void turn_chunks(u32x4& lo, u32x4& hi, const Turn& t,
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        lo[i] = pack_bf16(a[2 * i], a[2 * i + 1]);
-        hi[i] = pack_bf16(b[2 * i], b[2 * i + 1]);
+        if (d.turn_lo) lo[i] = pack_bf16(a[2 * i], a[2 * i + 1]);
+        if (d.turn_hi) hi[i] = pack_bf16(b[2 * i], b[2 * i + 1]);
     }
-}
-
-// What lane c of the eight has of a row: the element where each of its chunks starts, whether they are turned, and the place of
-// their cosines among the token's.
-struct LaneDims { int lo, hi, at; bool turned; };
-__device__ __forceinline__ LaneDims lane_dims(int c, const RopeParams& p) {
-    const int pairs = p.rot >> 4;             // lanes whose chunks are turned
-    LaneDims d;
-    d.turned = p.table != nullptr && c < pairs;
-    const bool half = d.turned && !p.interleaved;
-    d.lo = half ? c * 8 : c * 16;             // (dims that are not turned start at rot = 16 * pairs)
-    d.hi = half ? c * 8 + (p.rot >> 1) : c * 16 + 8;
-    d.at = c * 8;
-    return d;
-}
-// (by eight floats each: rot is a multiple of 16)
-__device__ __forceinline__ void load_turn(Turn& t, const RopeParams& p, int pos, const LaneDims& d) {
-    if (!d.turned) return;
-    if ((uint32_t)pos >= (uint32_t)p.max_pos) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t.c[i] = t.s[i] = __uint_as_float(0x7fc00000u);
-        return;
-    }
-    const float4* row = reinterpret_cast<const float4*>(p.table + (int64_t)pos * p.rot + d.at);
-    const float4* sin = reinterpret_cast<const float4*>(p.table + (int64_t)pos * p.rot + (p.rot >> 1) + d.at);
-    const float4 c0 = row[0], c1 = row[1], s0 = sin[0], s1 = sin[1];
-    t.c[0] = c0.x; t.c[1] = c0.y; t.c[2] = c0.z; t.c[3] = c0.w; t.c[4] = c1.x; t.c[5] = c1.y; t.c[6] = c1.z; t.c[7] = c1.w;
-    t.s[0] = s0.x; t.s[1] = s0.y; t.s[2] = s0.z; t.s[3] = s0.w; t.s[4] = s1.x; t.s[5] = s1.y; t.s[6] = s1.z; t.s[7] = s1.w;
 }
 
 // New tokens of a sequence, and the cache row of the first of them (it may lie outside the cache).
@@ -95,48 +91,38 @@ __device__ __forceinline__ int position_of(const RopeParams& p, int b, int i, in
     return p.positions != nullptr ? p.positions[(int64_t)b * p.n_new + i] : (int)min(max(start + i, (int64_t)-1), (int64_t)INT32_MAX);
 }
 
-// Rows of one token, ROWS at a time by eight lanes: q heads (turned, to q_out), then with the bf16 cache k heads (turned) and v heads
-// (copied).  ROWS = 8 where the launch is large: the lanes then share one read of the token's cosines and sines among eight rows.
-template <int ROWS, bool Q8>
-__device__ __forceinline__ void token_rows(const RopeParams& p, int b, uint32_t team) {
-    const int c = threadIdx.x & 7;
-    const int i = (int)(team / (uint32_t)p.teams_per_token), part = (int)(team - (uint32_t)i * (uint32_t)p.teams_per_token);
+// Eight lanes, one row of a token: q heads (turned, to q_out), then with the bf16 cache k heads (turned) and v heads (copied).  Sharing a
+// token's cosines and sines among several rows of a lane saves reads that hit in L2 and costs registers and coalescing: 8192 tokens of 48
+// heads take 39.1 us with one row to eight lanes (204 MB, 5.2 TB/s, the rate of a plain copy), 44.9 with two or four, 47.4 with eight; one
+// token 2.8, 3.4 and (four) 4.2.
+template <bool Q8>
+__device__ __forceinline__ void token_row(const RopeParams& p, int b, uint32_t team) {
+    const int i = (int)(team / (uint32_t)p.rows_per_token), r = (int)(team - (uint32_t)i * (uint32_t)p.rows_per_token);
     const NewTokens nt = new_tokens(p, b);
     if (i >= nt.n) return;
-    const int n_q = p.q != nullptr ? p.Hq : 0, total = n_q + (Q8 ? 0 : 2 * p.Hkv), r0 = part * ROWS;
+    const int n_q = p.q != nullptr ? p.Hq : 0;
     const int64_t at = nt.start + i;
-    const bool in_cache = at >= 0 && at < p.capacity;
-    const LaneDims d = lane_dims(c, p);
-    Turn t;
-    load_turn(t, p, position_of(p, b, i, nt.start), d);
-    u32x4 lo[ROWS], hi[ROWS];
-    uint16_t* to[ROWS];
-#pragma unroll
-    for (int x = 0; x < ROWS; ++x) {
-        const int r = r0 + x;
-        to[x] = nullptr;
-        if (r >= total) continue;
-        const uint16_t* from;
-        if (r < n_q) {
-            from = p.q + (int64_t)b * p.q_b + (int64_t)i * p.q_t + (int64_t)r * kD;
-            to[x] = p.q_out + (((int64_t)b * p.n_new + i) * p.Hq + r) * kD;
-        } else {
-            if (Q8 || !in_cache) continue;
-            const int h = r - n_q, g = h < p.Hkv ? h : h - p.Hkv;
-            from = h < p.Hkv ? p.k + (int64_t)b * p.k_b + (int64_t)i * p.k_t + (int64_t)g * kD
-                             : p.v + (int64_t)b * p.v_b + (int64_t)i * p.v_t + (int64_t)g * kD;
-            to[x] = (h < p.Hkv ? p.ck : p.cv) + (int64_t)b * p.c_b + (int64_t)g * p.c_h + at * kD;
-        }
-        lo[x] = *reinterpret_cast<const u32x4*>(from + d.lo);
-        hi[x] = *reinterpret_cast<const u32x4*>(from + d.hi);
+    const LaneDims d = lane_dims(threadIdx.x & 7, p);
+    const uint16_t* from;
+    uint16_t* to;
+    if (r < n_q) {
+        from = p.q + (int64_t)b * p.q_b + (int64_t)i * p.q_t + (int64_t)r * kD;
+        to = p.q_out + (((int64_t)b * p.n_new + i) * p.Hq + r) * kD;
+    } else {
+        if (Q8 || at < 0 || at >= p.capacity) return;
+        const bool key = r < n_q + p.Hkv;
+        const int g = r - n_q - (key ? 0 : p.Hkv);
+        from = (key ? p.k + (int64_t)b * p.k_b + (int64_t)i * p.k_t : p.v + (int64_t)b * p.v_b + (int64_t)i * p.v_t) + (int64_t)g * kD;
+        to = (key ? p.ck : p.cv) + (int64_t)b * p.c_b + (int64_t)g * p.c_h + at * kD;
     }
-#pragma unroll
-    for (int x = 0; x < ROWS; ++x) {
-        if (to[x] == nullptr) continue;
-        if (d.turned && r0 + x < n_q + p.Hkv) turn_chunks(lo[x], hi[x], t, p.interleaved != 0);
-        *reinterpret_cast<u32x4*>(to[x] + d.lo) = lo[x];
-        *reinterpret_cast<u32x4*>(to[x] + d.hi) = hi[x];
+    u32x4 lo = *reinterpret_cast<const u32x4*>(from + d.lo), hi = *reinterpret_cast<const u32x4*>(from + d.hi);
+    if (p.table != nullptr && r < n_q + p.Hkv) {
+        Turn t;
+        load_turn(t, p, position_of(p, b, i, nt.start), d);
+        turn_chunks(lo, hi, t, d, p.interleaved != 0);
     }
+    *reinterpret_cast<u32x4*>(to + d.lo) = lo;
+    *reinterpret_cast<u32x4*>(to + d.hi) = hi;
 }
 
 // ---- blocks of the cache of 8 bits ----
@@ -170,12 +156,11 @@ __device__ __forceinline__ uint2 quantise8(const u32x4 x, float inv) {
     return make_uint2(o[0], o[1]);
 }
 
-// One workgroup: block number start / block + x of one (sequence, KV head), keys or values.  32 rows at a time by eight lanes each, all
+// One workgroup: block number start / block + x of one (sequence, KV head), keys or values.  PASSES times 32 rows by eight lanes each, all
 // rows held in registers until their largest magnitude is known.  The first block's workgroup also has the rows that stay in the
 // tail when they belong to a later block: it has read the tail's old rows by then.
-template <int FORMAT>
+template <int FORMAT, int PASSES>
 __device__ __forceinline__ void append_block(const RopeParams& p, int b, int x, int g, bool values) {
-    constexpr int PASSES = kQ8MaxBlock / 32;
     const NewTokens nt = new_tokens(p, b);
     if (nt.n == 0) return;
     const int blk = p.c8.block;
@@ -193,10 +178,10 @@ __device__ __forceinline__ void append_block(const RopeParams& p, int b, int x, 
         from += (int64_t)g * kD;
         lo = *reinterpret_cast<const u32x4*>(from + d.lo);
         hi = *reinterpret_cast<const u32x4*>(from + d.hi);
-        if (!values && d.turned) {
+        if (!values && p.table != nullptr) {
             Turn t;
             load_turn(t, p, position_of(p, b, i, nt.start), d);
-            turn_chunks(lo, hi, t, p.interleaved != 0);
+            turn_chunks(lo, hi, t, d, p.interleaved != 0);
         }
     };
     auto rows_to_tail = [&](int64_t block_first) {       // the new rows of the last block
@@ -251,23 +236,22 @@ __device__ __forceinline__ void append_block(const RopeParams& p, int b, int x, 
     if (x == 0 && partial && last != number) rows_to_tail(last * blk);       // (behind the barrier: the old rows have been read)
 }
 
-template <int ROWS>
 __global__ __launch_bounds__(256) void rope_append_kernel(const RopeParams p) {
     const int b = blockIdx.y;
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
-    token_rows<ROWS, false>(p, b, blockIdx.x * 32 + (threadIdx.x >> 3));
+    token_row<false>(p, b, blockIdx.x * 32 + (threadIdx.x >> 3));
 }
 
-template <int ROWS, int FORMAT>
+template <int FORMAT, int PASSES>
 __global__ __launch_bounds__(256) void rope_append_q8_kernel(const RopeParams p) {
     const int b = blockIdx.y;
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
     if ((int)blockIdx.x < p.block_wgs) {
         const int kv = blockIdx.x % (2 * p.Hkv);
-        append_block<FORMAT>(p, b, blockIdx.x / (2 * p.Hkv), kv >> 1, (kv & 1) != 0);
+        append_block<FORMAT, PASSES>(p, b, blockIdx.x / (2 * p.Hkv), kv >> 1, (kv & 1) != 0);
         return;
     }
-    token_rows<ROWS, true>(p, b, (blockIdx.x - (uint32_t)p.block_wgs) * 32 + (threadIdx.x >> 3));
+    token_row<true>(p, b, (blockIdx.x - (uint32_t)p.block_wgs) * 32 + (threadIdx.x >> 3));
 }
 
 // One workgroup per position.
@@ -318,11 +302,6 @@ static RopeParams rope_params(const rk_geom* geom, const rk_new_rows* rows, cons
     return p;
 }
 
-// Rows that eight lanes take one after the other: 8 where that leaves the chip full, one where a call is a few tokens.
-static int rows_per_team(const rk_geom* geom, const rk_new_rows* rows, int rows_per_token) {
-    return (int64_t)geom->batch * rows->n_new * rows_per_token >= 8 * 32 * 4 * kComputeUnits ? 8 : 1;
-}
-
 }  // namespace rk
 
 using namespace rk;
@@ -344,14 +323,10 @@ extern "C" int rk_rope_append(const rk_geom* geom, const rk_new_rows* rows, cons
     if ((rc = check_kv(cache)) != RK_OK) return rc;
     RopeParams p = rope_params(geom, rows, rope, positions, seq_lens, new_lens, q_out, pred, pred_val);
     p.ck = (uint16_t*)cache.k; p.cv = (uint16_t*)cache.v; p.c_b = cache.stride_b; p.c_h = cache.stride_h; p.capacity = (int32_t)cache.capacity;
-    const int per_token = (rows->q ? p.Hq : 0) + 2 * p.Hkv;
-    p.team_rows = rows_per_team(geom, rows, per_token);
-    p.teams_per_token = (per_token + p.team_rows - 1) / p.team_rows;
-    const int64_t wgs = ((int64_t)p.n_new * p.teams_per_token + 31) / 32;
+    p.rows_per_token = (rows->q ? p.Hq : 0) + 2 * p.Hkv;
+    const int64_t wgs = ((int64_t)p.n_new * p.rows_per_token + 31) / 32;
     if (wgs * 32 > INT32_MAX) return RK_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)wgs, geom->batch);
-    if (p.team_rows == 8) hipLaunchKernelGGL(rope_append_kernel<8>, grid, dim3(256), 0, (hipStream_t)stream, p);
-    else                  hipLaunchKernelGGL(rope_append_kernel<1>, grid, dim3(256), 0, (hipStream_t)stream, p);
+    hipLaunchKernelGGL(rope_append_kernel, dim3((unsigned)wgs, geom->batch), dim3(256), 0, (hipStream_t)stream, p);
     return launch_status();
 }
 
@@ -363,21 +338,15 @@ extern "C" int rk_rope_append_q8(const rk_geom* geom, const rk_new_rows* rows, c
     if ((rc = check_kv8(cache)) != RK_OK) return rc;
     RopeParams p = rope_params(geom, rows, rope, positions, seq_lens, new_lens, q_out, pred, pred_val);
     p.c8 = *cache;
-    const int per_token = rows->q ? p.Hq : 0;
-    p.team_rows = rows_per_team(geom, rows, per_token);
-    p.teams_per_token = per_token ? (per_token + p.team_rows - 1) / p.team_rows : 1;
+    p.rows_per_token = rows->q ? p.Hq : 0;
     const int64_t blocks = ((int64_t)p.n_new + p.c8.block - 2) / p.c8.block + 1;       // that n_new rows can touch
-    const int64_t block_wgs = blocks * 2 * p.Hkv, q_wgs = per_token ? ((int64_t)p.n_new * p.teams_per_token + 31) / 32 : 0;
+    const int64_t block_wgs = blocks * 2 * p.Hkv, q_wgs = ((int64_t)p.n_new * p.rows_per_token + 31) / 32;
     if (block_wgs + q_wgs * 32 > INT32_MAX) return RK_ERR_UNSUPPORTED;
     p.block_wgs = (int32_t)block_wgs;
-    const dim3 grid((unsigned)(block_wgs + q_wgs), geom->batch);
-    hipStream_t st = (hipStream_t)stream;
-    if (cache->format == RK_Q8_E4M3) {
-        if (p.team_rows == 8) hipLaunchKernelGGL((rope_append_q8_kernel<8, RK_Q8_E4M3>), grid, dim3(256), 0, st, p);
-        else                  hipLaunchKernelGGL((rope_append_q8_kernel<1, RK_Q8_E4M3>), grid, dim3(256), 0, st, p);
-    } else {
-        if (p.team_rows == 8) hipLaunchKernelGGL((rope_append_q8_kernel<8, RK_Q8_INT8>), grid, dim3(256), 0, st, p);
-        else                  hipLaunchKernelGGL((rope_append_q8_kernel<1, RK_Q8_INT8>), grid, dim3(256), 0, st, p);
-    }
+    const bool e4m3 = cache->format == RK_Q8_E4M3;
+    auto kernel = cache->block == 128 ? (e4m3 ? rope_append_q8_kernel<RK_Q8_E4M3, 4> : rope_append_q8_kernel<RK_Q8_INT8, 4>)
+                  : cache->block == 64 ? (e4m3 ? rope_append_q8_kernel<RK_Q8_E4M3, 2> : rope_append_q8_kernel<RK_Q8_INT8, 2>)
+                                       : (e4m3 ? rope_append_q8_kernel<RK_Q8_E4M3, 1> : rope_append_q8_kernel<RK_Q8_INT8, 1>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(block_wgs + q_wgs), geom->batch), dim3(256), 0, (hipStream_t)stream, p);
     return launch_status();
 }
