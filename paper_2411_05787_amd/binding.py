@@ -191,6 +191,7 @@ except ImportError as _e:                  # not built (build.py), or for anothe
     class _native:
         """Takes no call: None sends each through the checks below."""
         setup = rk_partial_attn = rk_partial_attn_fixed = rk_gather_small_kv = rk_h2o_step = rk_full_attn = staticmethod(lambda *a: None)
+        rk_rope_append = rk_rope_append_q8 = rk_full_attn_q8 = rk_gather_small_kv_q8 = rk_prompt_attn = setup
 
     warnings.warn("short calls are marshalled in Python and take the host about 4 us more: %s" % _e, RuntimeWarning)
 
@@ -289,7 +290,7 @@ def _stream(stream) -> int:
     return int(stream)
 
 
-_native.setup(_stream, _raw_stream, _device, _Geom, _H2oState)
+_native.setup(_stream, _raw_stream, _device, _Geom, _H2oState, _Rope, _Kv8)
 
 
 def workspace_bytes(geom: Geom, max_len: int, max_k: int) -> int:
@@ -759,7 +760,7 @@ class Rope:
         if table.dim() != 2:
             raise ValueError("table must be [max_pos, rot_dim]")
         self.table, self.interleaved = table, bool(interleaved)
-        self.rot_dim = table.shape[1]
+        self.rot_dim, self.device_index = table.shape[1], table.device.index
         self._c = _Rope(_dev(table, torch.float32, "table"), table.shape[0], table.shape[1], int(self.interleaved))
 
 
@@ -811,7 +812,7 @@ class Kv8:
                        _dev(v_scale, torch.float32, "v_scale", (B, H, cap // block)),
                        _dev(k_tail, torch.bfloat16, "k_tail", (B, H, block, D)), _dev(v_tail, torch.bfloat16, "v_tail", (B, H, block, D)),
                        k.stride(0), k.stride(1), cap, block, Q8_FORMATS[k.dtype])
-        _same_device(k, v, k_scale, v_scale, k_tail, v_tail)
+        self.device_index = _same_device(k, v, k_scale, v_scale, k_tail, v_tail).index
 
     @classmethod
     def empty(cls, geom: Geom, capacity: int, block: int = 32, dtype=torch.float8_e4m3fn, device="cuda") -> "Kv8":
@@ -877,6 +878,9 @@ def rk_rope_append(geom: Geom, q, k, v, rope: Optional[Rope], K, V, seq_lens, q_
                    pred=None, pred_val: int = 0, stream=None) -> None:
     """q bf16 [B, T, Hq, D] (or None, with q_out), k, v [B, T, Hkv, D], the heads of a token side by side (any strides between tokens and
     sequences); K, V: the full cache; q_out bf16 [B, T, Hq, D] (may be q)."""
+    rc = _native.rk_rope_append(geom, q, k, v, rope, K, V, seq_lens, q_out, new_lens, positions, pred, pred_val, stream)
+    if rc is not None:
+        return _check("rk_rope_append", rc)
     rows, r, pos, lens, new, qo = _new_rows(geom, q, k, v, rope, positions, seq_lens, new_lens, q_out)
     dev = _same_device(k, q, v, None if rope is None else rope.table, K, V, seq_lens, q_out, new_lens, positions, pred)
     _launch("rk_rope_append", dev, stream, C.byref(geom.c()), rows, r, pos, _kv(geom, K, V, "cache"), lens, new, qo,
@@ -886,6 +890,9 @@ def rk_rope_append(geom: Geom, q, k, v, rope: Optional[Rope], K, V, seq_lens, q_
 def rk_rope_append_q8(geom: Geom, q, k, v, rope: Optional[Rope], cache: Kv8, seq_lens, q_out, new_lens=None, positions=None,
                       pred=None, pred_val: int = 0, stream=None) -> None:
     """rk_rope_append into a cache of 8 bits."""
+    rc = _native.rk_rope_append_q8(geom, q, k, v, rope, cache, seq_lens, q_out, new_lens, positions, pred, pred_val, stream)
+    if rc is not None:
+        return _check("rk_rope_append_q8", rc)
     rows, r, pos, lens, new, qo = _new_rows(geom, q, k, v, rope, positions, seq_lens, new_lens, q_out)
     dev = _same_device(k, q, v, None if rope is None else rope.table, _cache8(geom, cache), seq_lens, q_out, new_lens, positions, pred)
     _launch("rk_rope_append_q8", dev, stream, C.byref(geom.c()), rows, r, pos, C.byref(cache._c), lens, new, qo,
@@ -905,6 +912,9 @@ def _cache8(geom: Geom, cache: Kv8) -> torch.Tensor:
 def rk_full_attn_q8(geom: Geom, q, cache: Kv8, seq_lens, max_len: int, out, weights=None, lse=None, pred=None, pred_val: int = 0,
                     workspace: Workspace = None, stream=None) -> None:
     """rk_full_attn over a cache of 8 bits."""
+    rc = _native.rk_full_attn_q8(geom, q, cache, seq_lens, max_len, out, weights, lse, pred, pred_val, workspace, stream)
+    if rc is not None:
+        return _check("rk_full_attn_q8", rc)
     B, Hq, D = geom.batch, geom.n_q_heads, geom.head_dim
     dev = _same_device(_cache8(geom, cache), q, seq_lens, out, weights, lse, pred)
     if max_len > cache.capacity:
@@ -923,6 +933,9 @@ def rk_full_attn_q8(geom: Geom, q, cache: Kv8, seq_lens, max_len: int, out, weig
 def rk_gather_small_kv_q8(geom: Geom, cache: Kv8, idx, k: int, small_K, small_V, seq_lens, tail_start=None, pred=None, pred_val: int = 0,
                           stream=None) -> None:
     """rk_gather_small_kv out of a cache of 8 bits."""
+    rc = _native.rk_gather_small_kv_q8(geom, cache, idx, k, small_K, small_V, seq_lens, tail_start, pred, pred_val, stream)
+    if rc is not None:
+        return _check("rk_gather_small_kv_q8", rc)
     B, Hkv = geom.batch, geom.n_kv_heads
     dev = _same_device(_cache8(geom, cache), idx, small_K, small_V, seq_lens, tail_start, pred)
     _launch("rk_gather_small_kv_q8", dev, stream, C.byref(geom.c()), C.byref(cache._c), _dev(idx, torch.int32, "idx", (B, Hkv, k)), int(k),
@@ -951,6 +964,9 @@ def rk_prompt_attn(geom: Geom, q, K, V, seq_lens, max_len: int, out, new_lens=No
                    lse=None, pred=None, pred_val: int = 0, workspace: PromptWorkspace = None, stream=None) -> None:
     """q bf16 [B, T, Hq, D], the heads of a token side by side (any strides between tokens and sequences); out bf16 [B, T, Hq, D];
     first, end int32 [B, T]; slopes fp32 [Hq]; lse fp32 [B, T, Hq]."""
+    rc = _native.rk_prompt_attn(geom, q, K, V, seq_lens, max_len, out, new_lens, first, end, cap, slopes, lse, pred, pred_val, workspace, stream)
+    if rc is not None:
+        return _check("rk_prompt_attn", rc)
     B, Hq, D = geom.batch, geom.n_q_heads, geom.head_dim
     if not isinstance(q, torch.Tensor) or q.dim() != 4:
         raise ValueError("q must be [batch, n_new, n_q_heads, head_dim]")
