@@ -33,35 +33,44 @@ template <> struct TileRows<RK_Q8_INT8> { u32x4 k[2][2]; uint2 v[8]; };
 // Row of the tile that slot e of lane group g of the second product is.
 __device__ __forceinline__ int slot_row(int e, int g) { return (e >> 2) * 16 + 4 * g + (e & 3); }
 
-// Requests the rows first .. first + 31 (never one beyond `last`) of k, v: base pointers of the (sequence, KV head).
-template <int FORMAT, bool STREAM, bool BYTES>
-__device__ __forceinline__ void request_keys(TileRows<FORMAT>& t, const void* k, int64_t first, int64_t last) {
+// Requests the rows at..at + 31 of k, v (base pointers of the (sequence, KV head), the same in the whole wavefront), of which `left` exist (any number, also none): the
+// tile is a buffer of its own, so that a lane's place in it is worked out once for all tiles and rows past the end read as zeros without traffic.
+// All are streamed: see load_rows16.
+constexpr int kStreamAux = 2;                 // cache-policy operand of buffer loads: nt
+template <int FORMAT>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_buffer(const void* base, int at, int left) {
+    constexpr int row = FORMAT == kBf16 ? kD * 2 : kD;
+    int rows = min(left, kTileRows);
+    asm("" : "+s"(rows));                     // (scalar minimum and maximum, one after the other)
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>((const uint8_t*)base + (int64_t)at * row), 0, max(rows, 0) * row, 0x00020000);
+}
+template <int FORMAT, bool BYTES>
+__device__ __forceinline__ void request_keys(TileRows<FORMAT>& t, const void* k, int at, int left) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const __amdgpu_buffer_rsrc_t r = tile_buffer<FORMAT>(k, at, left);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        const int64_t r = min(first + 16 * x + n, last);
         if constexpr (FORMAT == kBf16) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) t.k[x][s] = load_rows16<STREAM>((const uint16_t*)k + r * kD + operand_dim<BYTES>(s, g));
+            for (int s = 0; s < 4; ++s)
+                t.k[x][s] = __builtin_amdgcn_raw_buffer_load_b128(r, (16 * x + n) * (kD * 2) + operand_dim<BYTES>(s, g) * 2, 0, kStreamAux);
         } else {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) t.k[x][s] = load_rows16<STREAM>((const uint16_t*)((const uint8_t*)k + r * kD + 64 * s + 16 * g));
+            for (int s = 0; s < 2; ++s) t.k[x][s] = __builtin_amdgcn_raw_buffer_load_b128(r, (16 * x + n) * kD + 64 * s + 16 * g, 0, kStreamAux);
         }
     }
 }
-template <int FORMAT, bool STREAM>
-__device__ __forceinline__ void request_values(TileRows<FORMAT>& t, const void* v, int64_t first, int64_t last) {
+template <int FORMAT>
+__device__ __forceinline__ void request_values(TileRows<FORMAT>& t, const void* v, int at, int left) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const __amdgpu_buffer_rsrc_t r = tile_buffer<FORMAT>(v, at, left);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int64_t r = min(first + slot_row(e, g), last);
         if constexpr (FORMAT == kBf16) {
-            t.v[e] = load_rows16<STREAM>((const uint16_t*)v + r * kD + 8 * n);
+            t.v[e] = __builtin_amdgcn_raw_buffer_load_b128(r, slot_row(e, g) * (kD * 2) + 16 * n, 0, kStreamAux);
         } else {
-            typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-            const u32x2* p = reinterpret_cast<const u32x2*>((const uint8_t*)v + r * kD + 8 * n);
-            const u32x2 x = STREAM ? __builtin_nontemporal_load(p) : *p;
-            t.v[e] = make_uint2(x.x, x.y);
+            const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, slot_row(e, g) * kD + 8 * n, 0, kStreamAux);
+            t.v[e] = make_uint2(x[0], x[1]);
         }
     }
 }
@@ -103,6 +112,18 @@ __device__ __forceinline__ void value_operands(const TileRows<FORMAT>& t, int h,
             o[0][j] = pair_of<FORMAT, false>(w0); o[1][j] = pair_of<FORMAT, true>(w0);
             o[2][j] = pair_of<FORMAT, false>(w1); o[3][j] = pair_of<FORMAT, true>(w1);
         }
+    }
+}
+
+// The queries' operands are here once this returns.  Called behind the first tile's requests: left to itself the compiler finds them still on their way
+// where the loop begins, and every round of the loop then waits for all that is in flight (18.4 -> 15.2 us for 32777 rows of 8 bits).
+__device__ __forceinline__ void queries_here(bf16x8 (&q)[4]) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        u32x4 x = __builtin_bit_cast(u32x4, q[s]);
+        asm volatile("" : "+v"(x));
+        q[s] = __builtin_bit_cast(bf16x8, x);
     }
 }
 

@@ -299,6 +299,7 @@ void prompt_cols_kernel(const PromptParams p) {
     const uint16_t* qr = p.q + (int64_t)b * p.q_b + (int64_t)me.token * p.q_t + (int64_t)me.head * kD;
 #pragma unroll
     for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qr + operand_dim<false>(s, gr));
+    __builtin_amdgcn_sched_barrier(0);
     const ScoreForm form = score_form(p);
     const float slope2 = MODS && p.slopes != nullptr ? p.slopes[me.head] * kLog2e : 0.f;
     const uint16_t* k = p.k + (int64_t)b * p.s_b + (int64_t)g * p.s_h;
@@ -309,17 +310,17 @@ void prompt_cols_kernel(const PromptParams p) {
     TileRows<kBf16> rows;
     const int step = p.splits * kColWaves;
     int t = split * kColWaves + w;
-    auto first_of = [&](int x) { return (int64_t)lo + (int64_t)x * kTileRows; };
+    auto first_of = [&](int x) { return lo + x * kTileRows; };        // (past the rows there are by a round at most: see check_kv)
     if (t < tiles) {
-        request_keys<kBf16, true, false>(rows, k, first_of(t), hi - 1);
-        request_values<kBf16, true>(rows, v, first_of(t), hi - 1);
+        request_keys<kBf16, false>(rows, k, first_of(t), hi - first_of(t));
+        request_values<kBf16>(rows, v, first_of(t), hi - first_of(t));
     }
+    queries_here(q);
     for (; t < tiles; t += step) {
-        const int j0 = (int)first_of(t);
+        const int j0 = first_of(t);
         float s[2][4];
         tile_scores<kBf16>(rows, q, s);
-        const bool more = t + step < tiles;
-        if (more) request_keys<kBf16, true, false>(rows, k, first_of(t + step), hi - 1);
+        request_keys<kBf16, false>(rows, k, first_of(t + step), hi - first_of(t + step));       // (past the last tile: nothing)
         const bool masked = j0 < in_lo || (int64_t)j0 + kTileRows > in_hi;
         auto sees = [&](int j) { return j >= me.lo && j < me.hi; };
 #pragma unroll
@@ -359,7 +360,7 @@ void prompt_cols_kernel(const PromptParams p) {
                 }
             }
         }
-        if (more) request_values<kBf16, true>(rows, v, first_of(t + step), hi - 1);
+        request_values<kBf16>(rows, v, first_of(t + step), hi - first_of(t + step));
     }
 
     __shared__ __attribute__((aligned(16))) ColMergeLds lds;

@@ -22,7 +22,7 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
         b = slot.b; c = slot.c; nchunks = slot.nchunks;
     }
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
-    const int len = min(max(p.seq_lens[b], 0), p.cap2), n = min(len, p.max_rows2);
+    const int len = __builtin_amdgcn_readfirstlane(min(max(p.seq_lens[b], 0), p.cap2)), n = min(len, p.max_rows2);
     if (p.ragged_batch == 0) {
         nchunks = active_workgroups(n, p.nch);
         if (c >= nchunks) return;
@@ -42,6 +42,7 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
     const uint16_t* qr = p.q + ((int64_t)b * p.Hq + g * G + min(col, G - 1)) * kD;
 #pragma unroll
     for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qr + operand_dim<true>(s, gr));
+    __builtin_amdgcn_sched_barrier(0);
 
     ColState st;
     st.clear();
@@ -52,53 +53,69 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
         for (int x = 0; x < 2; ++x) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[x][i] *= x ? k1 : k0;
-            const int r = 16 * x + 4 * gr;
-            if (EMIT && col < G) {
-                float* to = wrow + first + r;
-                if (p.w_vec != 0 && r + 4 <= rows) {
-                    *reinterpret_cast<float4*>(to) = make_float4(s[x][0], s[x][1], s[x][2], s[x][3]);
-                } else {
+        }
+        if (EMIT && col < G) {
+            float* to = wrow + first + 4 * gr;
+            if (p.w_vec != 0 && rows >= kTileRows) {      // (the same for the whole wavefront)
+                *reinterpret_cast<float4*>(to) = make_float4(s[0][0], s[0][1], s[0][2], s[0][3]);
+                *reinterpret_cast<float4*>(to + 16) = make_float4(s[1][0], s[1][1], s[1][2], s[1][3]);
+            } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) if (r + i < rows) to[i] = s[x][i];
-                }
-            }
-            if (rows < kTileRows) {
+                for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[x][i] = r + i < rows ? s[x][i] : -INFINITY;
+                    for (int i = 0; i < 4; ++i) if (16 * x + 4 * gr + i < rows) to[16 * x + i] = s[x][i];
             }
+        }
+        if (rows < kTileRows) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[x][i] = 16 * x + 4 * gr + i < rows ? s[x][i] : -INFINITY;
         }
         tile_softmax(st, s);
     };
     const int t0 = c * kColWaves + w, step = nchunks * kColWaves;
     TileRows<FORMAT> rows;
+    // the scales of a tile's two blocks of 16 rows, requested with its rows
+    struct Scales { float k0, k1, v0, v1; };
+    auto request_scales = [&](int t) {
+        const int x = min(t * kTileRows, main_rows - 1) >> c8.shift, y = min(t * kTileRows + 16, main_rows - 1) >> c8.shift;
+        typedef const __attribute__((address_space(4))) float* Scalar;      // (nothing writes them meanwhile: scalar loads)
+        return Scales{((Scalar)ks)[x], ((Scalar)ks)[y], ((Scalar)vs)[x], ((Scalar)vs)[y]};
+    };
+    Scales sc{};
     int t = t0;
     if (t < main_tiles) {
-        request_keys<FORMAT, true, true>(rows, k, (int64_t)t * kTileRows, main_rows - 1);
-        request_values<FORMAT, true>(rows, v, (int64_t)t * kTileRows, main_rows - 1);
+        request_keys<FORMAT, true>(rows, k, t * kTileRows, main_rows - t * kTileRows);
+        request_values<FORMAT>(rows, v, t * kTileRows, main_rows - t * kTileRows);
+        sc = request_scales(t);
     }
+    queries_here(q);
+    // The next tile's rows are requested as soon as the registers of this one's are consumed, past the last tile as well (nothing then): a
+    // request that is not always made would leave the compiler to wait for all that are in flight.
     for (; t < main_tiles; t += step) {
-        const int first = t * kTileRows, second = min(first + 16, main_rows - 1);
-        const float k0 = ks[first >> c8.shift] * p.scale, k1 = ks[second >> c8.shift] * p.scale;
-        const float v0 = vs[first >> c8.shift], v1 = vs[second >> c8.shift];
+        const int first = t * kTileRows;
         float s[2][4];
         tile_scores<FORMAT>(rows, q, s);
-        const bool more = t + step < main_tiles;
-        if (more) request_keys<FORMAT, true, true>(rows, k, (int64_t)(t + step) * kTileRows, main_rows - 1);
-        finish_scores(s, first, main_rows - first, k0, k1);
+        const int next = (t + step) * kTileRows;      // (no more than 2 kMaxChunks * kMinChunk beyond the rows there are: see check_kv8)
+        request_keys<FORMAT, true>(rows, k, next, main_rows - next);
+        const Scales now = sc;
+        sc = request_scales(t + step);
+        finish_scores(s, first, main_rows - first, now.k0 * p.scale, now.k1 * p.scale);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { s[0][i] *= v0; s[1][i] = main_rows - first > 16 ? s[1][i] * v1 : 0.f; }
+        for (int i = 0; i < 4; ++i) { s[0][i] *= now.v0; s[1][i] *= now.v1; }      // (rows that are not there: 0, and the last row's scale)
         bf16x8 hi, lo;
         weight_operands(s, hi, lo);
         tile_output<FORMAT>(rows, st, hi, lo);
-        if (more) request_values<FORMAT, true>(rows, v, (int64_t)(t + step) * kTileRows, main_rows - 1);
+        request_values<FORMAT>(rows, v, next, main_rows - next);
     }
     for (; t < tiles; t += step) {            // the block that is not full: bf16
         const int at = (t - main_tiles) * kTileRows, left = n - main_rows - at;
         const uint16_t* kt = c8.kt + (bg << c8.shift) * kD;
         const uint16_t* vt = c8.vt + (bg << c8.shift) * kD;
         TileRows<kBf16> x;
-        request_keys<kBf16, false, true>(x, kt, at, n - main_rows - 1);
-        request_values<kBf16, false>(x, vt, at, n - main_rows - 1);
+        request_keys<kBf16, true>(x, kt, at, left);
+        request_values<kBf16>(x, vt, at, left);
         float s[2][4];
         tile_scores<kBf16>(x, q, s);
         finish_scores(s, main_rows + at, left, p.scale, p.scale);
@@ -169,7 +186,6 @@ extern "C" int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8*
     if (weights && (w_stride < max_len || ((uintptr_t)weights & 3u))) return RK_ERR_INVALID_ARG;
     Workspace ws;
     if ((rc = check_workspace(geom, max_len, 0, workspace, workspace_bytes, &ws)) != RK_OK) return rc;
-    const int G = geom->n_q_heads / geom->n_kv_heads;
     AttnParams p{};
     p.q = (const uint16_t*)q;
     p.seq_lens = seq_lens; p.max_rows2 = max_len; p.cap2 = (int32_t)full->capacity;
