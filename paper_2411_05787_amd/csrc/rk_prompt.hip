@@ -59,9 +59,7 @@ struct ScoreForm { float scale2, inner, cap2; bool capped; };
 __device__ __forceinline__ ScoreForm score_form(const PromptParams& p) {
     return {p.scale * kLog2e, p.cap > 0.f ? p.scale / p.cap * (2.f * kLog2e) : 0.f, p.cap * kLog2e, p.cap > 0.f};
 }
-template <bool MODS>
 __device__ __forceinline__ float score_of(float x, const ScoreForm& f, float slope2, int far) {
-    if constexpr (!MODS) return x * f.scale2;
     float s = x * f.scale2;
     if (f.capped) s = f.cap2 - 2.f * f.cap2 * __builtin_amdgcn_rcpf(fast_exp2(x * f.inner) + 1.f);
     return fmaf(-slope2, fabsf((float)far), s);
@@ -121,7 +119,12 @@ void prompt_tile_kernel(const PromptParams p) {
     const uint16_t* qr = p.q + (int64_t)b * p.q_b + (int64_t)me.token * p.q_t + (int64_t)me.head * kD;
 #pragma unroll
     for (int s = 0; s < 8; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s + 8 * h);
-    const ScoreForm form = score_form(p);
+    ScoreForm form = score_form(p);
+    if (!MODS && form.scale2 < 0.f) {         // raw products are compared below: their order has to be the scores'
+        form.scale2 = -form.scale2;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[s]) ^ 0x80008000u);
+    }
     const float slope2 = MODS && p.slopes != nullptr ? p.slopes[me.head] * kLog2e : 0.f;
     __syncthreads();
     const int lo = min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])), hi = max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3]));
@@ -139,15 +142,18 @@ void prompt_tile_kernel(const PromptParams p) {
     // staging: thread -> chunk of 16 bytes c of rows r16 + 16 i.  K: chunk c of row r lies at c ^ (r & 15); V: at c ^ 2 (r & 7), so that the
     // transposing reads of four rows of 16 dims fall on different banks.
     const int c = tid & 15, r16 = tid >> 4;
-    const uint16_t* kb_ = p.k + (int64_t)b * p.s_b + (int64_t)g * p.s_h + c * 8;
-    const uint16_t* vb_ = p.v + (int64_t)b * p.s_b + (int64_t)g * p.s_h + c * 8;
+    const uint16_t* k_rows = p.k + (int64_t)b * p.s_b + (int64_t)g * p.s_h;
+    const uint16_t* v_rows = p.v + (int64_t)b * p.s_b + (int64_t)g * p.s_h;
     u32x4 kr[4], vr[4];
+    // (a tile is a buffer of its own: rows past `hi` read as zeros, which no row sees)
     auto request = [&](int t) {
+        const int at = lo + t * kPromptTile, bytes = min(hi - at, kPromptTile) * (kD * 2);
+        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(k_rows) + (int64_t)at * kD, 0, bytes, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(v_rows) + (int64_t)at * kD, 0, bytes, 0x00020000);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t r = min((int64_t)lo + (int64_t)t * kPromptTile + r16 + 16 * i, (int64_t)hi - 1);
-            kr[i] = *reinterpret_cast<const u32x4*>(kb_ + r * kD);
-            vr[i] = *reinterpret_cast<const u32x4*>(vb_ + r * kD);
+            kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, tid * 16, i * 4096, 0);
+            vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, tid * 16, i * 4096, 0);
         }
     };
     const int k_to = r16 * 256 + ((c ^ r16) << 4), v_to = r16 * 256 + ((c ^ (2 * (r16 & 7))) << 4);
@@ -187,18 +193,26 @@ void prompt_tile_kernel(const PromptParams p) {
                 s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[k], s[x], 0, 0, 0);
             }
         }
+        auto row_of = [&](int x, int r) { return j0 + 32 * x + 8 * (r >> 2) + 4 * h + (r & 3); };
+        if constexpr (MODS) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[x][r] = score_of(s[x][r], form, slope2, me.pos - row_of(x, r));
+        }
+        if (masked) {
+            asm volatile("" ::: "memory");    // (a branch: most tiles have nothing to mask)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) { const int j = row_of(x, r); s[x][r] = j >= me.lo && j < me.hi ? s[x][r] : -INFINITY; }
+        }
         float mx = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int j = j0 + 32 * x + 8 * (r >> 2) + 4 * h + (r & 3);
-                float v = score_of<MODS>(s[x][r], form, slope2, me.pos - j);
-                if (masked) v = j >= me.lo && j < me.hi ? v : -INFINITY;
-                s[x][r] = v;
-                mx = fmaxf(mx, v);
-            }
-        }
+            for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(s[x][r], s[x][r + 1]), mx);
+        if constexpr (!MODS) mx *= form.scale2;
         mx = max_xor32(mx);
         // The maximum that weights are taken against follows the true one only when that has grown by more than 8: weights stay below 2^8, and the output
         // is rescaled a few times in all.
@@ -220,7 +234,8 @@ void prompt_tile_kernel(const PromptParams p) {
                 u32x4 u;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float a = fast_exp2(s[x][8 * y + 2 * e] - ref), bb = fast_exp2(s[x][8 * y + 2 * e + 1] - ref);
+                    const float s0 = s[x][8 * y + 2 * e], s1 = s[x][8 * y + 2 * e + 1];
+                    const float a = fast_exp2(MODS ? s0 - ref : fmaf(s0, form.scale2, -ref)), bb = fast_exp2(MODS ? s1 - ref : fmaf(s1, form.scale2, -ref));
                     l += a + bb;
                     u[e] = pack_bf16(a, bb);          // (8 bits a weight: its rounding is as large as the output's own and not common to the rows)
                 }
@@ -324,14 +339,16 @@ void prompt_cols_kernel(const PromptParams p) {
         const bool masked = j0 < in_lo || (int64_t)j0 + kTileRows > in_hi;
         auto sees = [&](int j) { return j >= me.lo && j < me.hi; };
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = j0 + 16 * x + 4 * gr + i;
-                // (natural units, as the columns' running state has them)
-                const float z = score_of<MODS>(s[x][i], form, slope2, me.pos - j) * (1.f / kLog2e);
-                s[x][i] = !masked || sees(j) ? z : -INFINITY;
-            }
+            for (int i = 0; i < 4; ++i)       // (natural units, as the columns' running state has them)
+                s[x][i] = MODS ? score_of(s[x][i], form, slope2, me.pos - (j0 + 16 * x + 4 * gr + i)) * (1.f / kLog2e) : s[x][i] * p.scale;
+        if (masked) {
+            asm volatile("" ::: "memory");    // (a branch: most tiles have nothing to mask)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[x][i] = sees(j0 + 16 * x + 4 * gr + i) ? s[x][i] : -INFINITY;
         }
         tile_softmax(st, s);
         bf16x8 ph, pl;
@@ -502,7 +519,7 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
         p.part_o = (float*)workspace;
         p.part_ml = p.part_o + rows * kD;
     }
-    const bool mods = p.cap > 0.f || p.slopes != nullptr;
+    const bool mods = p.cap > 0.f || p.slopes != nullptr || p.scale == 0.f;      // (a scale of 0: masked products would be 0 times infinity)
     hipStream_t st = (hipStream_t)stream;
     if (plan.cols) {
         auto kernel = mods ? prompt_cols_kernel<true> : prompt_cols_kernel<false>;
