@@ -105,15 +105,17 @@ void prompt_tile_kernel(const PromptParams p) {
     const bool real = row < n_rows;
     const Query me = query_of(p, tok, b, g, min(row, n_rows - 1));
 
-    __shared__ __attribute__((aligned(16))) unsigned char sK[kPromptTile * kD * 2], sV[kPromptTile * kD * 2];
-    __shared__ int sLo[4], sHi[4], sInLo[4], sInHi[4], sBad;
+    // two tiles of K and V: one is worked on while the next is written
+    constexpr int kHalf = kPromptTile * kD * 2;
+    __shared__ __attribute__((aligned(16))) unsigned char sK[2 * kHalf], sV[2 * kHalf];
+    __shared__ int sLo[4], sHi[4], sInLo[4], sInHi[4], sBad[2];
 
     // ranges: of the wavefront's rows together, and what all of them see
     const bool some = real && me.lo < me.hi;
     const int w_lo = wave_min(some ? me.lo : INT32_MAX), w_hi = wave_max_i(some ? me.hi : INT32_MIN);
     const int in_lo = wave_max_i(real ? me.lo : INT32_MIN), in_hi = wave_min(real ? me.hi : INT32_MAX);
     if (lane == 0) { sLo[w] = w_lo; sHi[w] = w_hi; sInLo[w] = in_lo; sInHi[w] = in_hi; }
-    if (tid == 0) sBad = -1;
+    if (tid == 0) sBad[0] = sBad[1] = -1;
 
     bf16x8 q[8];
     const uint16_t* qr = p.q + (int64_t)b * p.q_b + (int64_t)me.token * p.q_t + (int64_t)me.head * kD;
@@ -161,26 +163,25 @@ void prompt_tile_kernel(const PromptParams p) {
     const int i16 = lane & 15, q4 = (lane >> 4) & 1;
     const int v_from = (4 * h + (i16 >> 2)) * 256 + (((2 * q4 + ((i16 & 3) >> 1)) ^ (2 * (4 * h + (i16 >> 2)))) << 4) + (i16 & 1) * 8;
 
-    if (t0 < t1) request(t0);
-    for (int t = t0; t < t1; ++t) {
-        __syncthreads();
-        const int j0 = lo + t * kPromptTile;
-        if (j0 < all_lo || (int64_t)j0 + kPromptTile > all_hi) {
+    auto write = [&](int t) {                 // the requested tile, number t, to its half of the LDS
+        const int j0 = lo + t * kPromptTile, half = (t & 1) * kHalf;
+        if (j0 < all_lo || j0 + kPromptTile > all_hi) {
             if (has_non_finite(vr[0]) || has_non_finite(vr[1]) || has_non_finite(vr[2]) || has_non_finite(vr[3])) {
-                sBad = t;
+                sBad[t & 1] = t;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) drop_non_finite(vr[i]);
             }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<u32x4*>(sK + k_to + i * 4096) = kr[i];
-            *reinterpret_cast<u32x4*>(sV + v_to + i * 4096) = vr[i];
+            *reinterpret_cast<u32x4*>(sK + half + k_to + i * 4096) = kr[i];
+            *reinterpret_cast<u32x4*>(sV + half + v_to + i * 4096) = vr[i];
         }
-        __syncthreads();
-        if (t + 1 < t1) request(t + 1);
-        if (j0 >= w_hi || (int64_t)j0 + kPromptTile <= w_lo) continue;
-        const bool masked = j0 < in_lo || (int64_t)j0 + kPromptTile > in_hi;
+    };
+    auto work = [&](int t) {
+        const int j0 = lo + t * kPromptTile, half = (t & 1) * kHalf;
+        if (j0 >= w_hi || j0 + kPromptTile <= w_lo) return;
+        const bool masked = j0 < in_lo || j0 + kPromptTile > in_hi;
         // ---- S^T: rows j0 + 32 x + 8 (r / 4) + 4 h + r % 4 of column n ----
         f32x16 s[2];
 #pragma unroll
@@ -189,7 +190,7 @@ void prompt_tile_kernel(const PromptParams p) {
             for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8*>(sK + (k_from ^ (k << 5)) + x * 8192);
+                const bf16x8 a = *reinterpret_cast<const bf16x8*>(sK + half + (k_from ^ (k << 5)) + x * 8192);
                 s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[k], s[x], 0, 0, 0);
             }
         }
@@ -226,34 +227,51 @@ void prompt_tile_kernel(const PromptParams p) {
                 for (int r = 0; r < 16; ++r) o[d][r] *= a;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        bf16x8 pw[4];
+        // ---- weights, and O^T += V^T P^T, 16 rows at a time: slot e of half h is row 8 (e / 4) + 4 h + e % 4 of them ----
+        auto value = [&](int y, int d) {
+            const unsigned char* at = sV + half + (v_from ^ (d << 6)) + y * 4096;
+            const v4s v0 = lds_read_tr16(reinterpret_cast<const uint16_t*>(at)), v1 = lds_read_tr16(reinterpret_cast<const uint16_t*>(at + 2048));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        float part[4];
+        auto weights = [&](int y) {
+            u32x4 u;
+            part[y] = 0.f;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+            for (int e = 0; e < 4; ++e) {
+                const float s0 = s[y >> 1][8 * (y & 1) + 2 * e], s1 = s[y >> 1][8 * (y & 1) + 2 * e + 1];
+                const float a = fast_exp2(MODS ? s0 - ref : fmaf(s0, form.scale2, -ref)), bb = fast_exp2(MODS ? s1 - ref : fmaf(s1, form.scale2, -ref));
+                part[y] += a + bb;
+                u[e] = pack_bf16(a, bb);              // (8 bits a weight: its rounding is as large as the output's own and not common to the rows)
+            }
+            return __builtin_bit_cast(bf16x8, u);
+        };
+        bf16x8 v[2][4], pw[2];
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                u32x4 u;
+        for (int d = 0; d < 4; ++d) v[0][d] = value(0, d);
+        pw[0] = weights(0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float s0 = s[x][8 * y + 2 * e], s1 = s[x][8 * y + 2 * e + 1];
-                    const float a = fast_exp2(MODS ? s0 - ref : fmaf(s0, form.scale2, -ref)), bb = fast_exp2(MODS ? s1 - ref : fmaf(s1, form.scale2, -ref));
-                    l += a + bb;
-                    u[e] = pack_bf16(a, bb);          // (8 bits a weight: its rounding is as large as the output's own and not common to the rows)
+        for (int y = 0; y < 4; ++y) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (y < 3) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d) v[(y + 1) & 1][d] = value(y + 1, d);
+                pw[(y + 1) & 1] = weights(y + 1);
+            }
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[y & 1][d], pw[y & 1], o[d], 0, 0, 0);
+            if (y < 3) {                      // a matrix instruction, then what fits beside it: transposing reads and the next 16 rows' weights
+                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x402, 9, 0);
                 }
-                pw[2 * x + y] = __builtin_bit_cast(bf16x8, u);
             }
         }
-        // ---- O^T += V^T P^T: slot e of half h is row 8 (e / 4) + 4 h + e % 4 of 16 ----
-        auto value = [&](int y, int d) {
-            const unsigned char* at = sV + (v_from ^ (d << 6)) + y * 4096;
-            const v4s v0 = lds_read_tr16(reinterpret_cast<const uint16_t*>(at)), v1 = lds_read_tr16(reinterpret_cast<const uint16_t*>(at + 2048));
-            return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value(y, d)), pw[y], o[d], 0, 0, 0);
-        if (sBad == t) {
+        __builtin_amdgcn_sched_barrier(0);
+        l += (part[0] + part[1]) + (part[2] + part[3]);
+        if (sBad[t & 1] == t) {
             const uint16_t* from = p.v + (int64_t)b * p.s_b + (int64_t)g * p.s_h + 4 * h;
             for (int j = max(j0, me.lo); j < j0 + kPromptTile && j < me.hi; ++j) {
 #pragma unroll
@@ -266,6 +284,18 @@ void prompt_tile_kernel(const PromptParams p) {
                     }
             }
         }
+    };
+    if (t0 < t1) {
+        request(t0);
+        write(t0);
+        if (t0 + 1 < t1) request(t0 + 1);
+        __syncthreads();
+    }
+    for (int t = t0; t < t1; ++t) {
+        work(t);
+        if (t + 1 < t1) write(t + 1);
+        if (t + 2 < t1) request(t + 2);
+        lds_barrier();
     }
     // ---- lane (n, h) has dims 32 d + 8 (r / 4) + 4 h + r % 4 of row n ----
     l = sum_xor32(l);
