@@ -54,15 +54,19 @@ __device__ __forceinline__ int wave_min(int v) {
 }
 __device__ __forceinline__ int wave_max_i(int v) { return ~wave_min(~v); }
 
-// Raw product -> score in units of ln 2.  tanh(x) = 1 - 2 / (e^2x + 1): right at both ends, off by 2^-23 of the cap between.
-struct ScoreForm { float scale2, inner, cap2; bool capped; };
-__device__ __forceinline__ ScoreForm score_form(const PromptParams& p) {
-    return {p.scale * kLog2e, p.cap > 0.f ? p.scale / p.cap * (2.f * kLog2e) : 0.f, p.cap * kLog2e, p.cap > 0.f};
+// Raw product x -> score = a * bend(x) + b, in units of ln 2 or 1 / `unit` of that.  Without a cap bend(x) = x; with one, cap tanh(y / cap) =
+// 2 cap / (1 + e^(-2 y / cap)) - cap, right at both ends and off by 2^-22 of the cap between: one exponential and one reciprocal, and the
+// product and sum around them become part of the multiply-add ahead of the weight's exponential.
+struct ScoreForm { float a, b, inner; };
+template <bool CAP>
+__device__ __forceinline__ ScoreForm score_form(const PromptParams& p, float unit) {
+    if constexpr (CAP) return {2.f * p.cap * unit, -p.cap * unit, p.scale / p.cap * (-2.f * kLog2e)};
+    return {p.scale * unit, 0.f, 0.f};
 }
-__device__ __forceinline__ float score_of(float x, const ScoreForm& f, float slope2, int far) {
-    float s = x * f.scale2;
-    if (f.capped) s = f.cap2 - 2.f * f.cap2 * __builtin_amdgcn_rcpf(fast_exp2(x * f.inner) + 1.f);
-    return fmaf(-slope2, fabsf((float)far), s);
+template <bool CAP>
+__device__ __forceinline__ float bend(float x, const ScoreForm& f) {
+    if constexpr (CAP) return __builtin_amdgcn_rcpf(fast_exp2(x * f.inner) + 1.f);
+    return x;
 }
 
 // Infinities and NaN of V in a tile of which a row sees a part.  A weight of 0 times one of them would be NaN in rows that do not see it, so such
@@ -85,7 +89,8 @@ __device__ __forceinline__ float only_non_finite(float v) { return (__float_as_u
 // ---- 128 rows to a workgroup ----
 constexpr int kPromptRows = 128, kPromptTile = 64;
 
-template <bool MODS>
+// SLOPE: scores are worked out one by one, not in the weights' exponents.
+template <bool CAP, bool SLOPE>
 __global__ __launch_bounds__(256, 2)
 void prompt_tile_kernel(const PromptParams p) {
     // Workgroups go round the 8 dies; each die takes one stretch of (sequence, KV head) pairs, so that a pair's rows are read by one L2, the
@@ -121,13 +126,13 @@ void prompt_tile_kernel(const PromptParams p) {
     const uint16_t* qr = p.q + (int64_t)b * p.q_b + (int64_t)me.token * p.q_t + (int64_t)me.head * kD;
 #pragma unroll
     for (int s = 0; s < 8; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s + 8 * h);
-    ScoreForm form = score_form(p);
-    if (!MODS && form.scale2 < 0.f) {         // raw products are compared below: their order has to be the scores'
-        form.scale2 = -form.scale2;
+    ScoreForm form = score_form<CAP>(p, kLog2e);
+    if (!SLOPE && form.a < 0.f) {             // raw products are compared below: their order has to be the scores'
+        form.a = -form.a;
 #pragma unroll
         for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[s]) ^ 0x80008000u);
     }
-    const float slope2 = MODS && p.slopes != nullptr ? p.slopes[me.head] * kLog2e : 0.f;
+    const float slope2 = SLOPE && p.slopes != nullptr ? p.slopes[me.head] * kLog2e : 0.f;
     __syncthreads();
     const int lo = min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])), hi = max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3]));
     const int all_lo = max(max(sInLo[0], sInLo[1]), max(sInLo[2], sInLo[3])), all_hi = min(min(sInHi[0], sInHi[1]), min(sInHi[2], sInHi[3]));
@@ -195,11 +200,15 @@ void prompt_tile_kernel(const PromptParams p) {
             }
         }
         auto row_of = [&](int x, int r) { return j0 + 32 * x + 8 * (r >> 2) + 4 * h + (r & 3); };
-        if constexpr (MODS) {
+        if constexpr (CAP || SLOPE) {
+            const float far0 = (float)(me.pos - j0 - 4 * h);       // (distances beyond 2^24 to 2^-24 of themselves)
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[x][r] = score_of(s[x][r], form, slope2, me.pos - row_of(x, r));
+                for (int r = 0; r < 16; ++r) {
+                    s[x][r] = bend<CAP>(s[x][r], form);
+                    if constexpr (SLOPE) s[x][r] = fmaf(-slope2, fabsf(far0 - (float)(32 * x + 8 * (r >> 2) + (r & 3))), fmaf(s[x][r], form.a, form.b));
+                }
         }
         if (masked) {
             asm volatile("" ::: "memory");    // (a branch: most tiles have nothing to mask)
@@ -213,7 +222,7 @@ void prompt_tile_kernel(const PromptParams p) {
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(s[x][r], s[x][r + 1]), mx);
-        if constexpr (!MODS) mx *= form.scale2;
+        if constexpr (!SLOPE) mx = fmaf(mx, form.a, form.b);
         mx = max_xor32(mx);
         // The maximum that weights are taken against follows the true one only when that has grown by more than 8: weights stay below 2^8, and the output
         // is rescaled a few times in all.
@@ -226,7 +235,7 @@ void prompt_tile_kernel(const PromptParams p) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= a;
         }
-        const float ref = m == -INFINITY ? 0.f : m;
+        const float ref = m == -INFINITY ? 0.f : m, from = form.b - ref;
         // ---- weights, and O^T += V^T P^T, 16 rows at a time: slot e of half h is row 8 (e / 4) + 4 h + e % 4 of them ----
         auto value = [&](int y, int d) {
             const unsigned char* at = sV + half + (v_from ^ (d << 6)) + y * 4096;
@@ -240,7 +249,7 @@ void prompt_tile_kernel(const PromptParams p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float s0 = s[y >> 1][8 * (y & 1) + 2 * e], s1 = s[y >> 1][8 * (y & 1) + 2 * e + 1];
-                const float a = fast_exp2(MODS ? s0 - ref : fmaf(s0, form.scale2, -ref)), bb = fast_exp2(MODS ? s1 - ref : fmaf(s1, form.scale2, -ref));
+                const float a = fast_exp2(SLOPE ? s0 - ref : fmaf(s0, form.a, from)), bb = fast_exp2(SLOPE ? s1 - ref : fmaf(s1, form.a, from));
                 part[y] += a + bb;
                 u[e] = pack_bf16(a, bb);              // (8 bits a weight: its rounding is as large as the output's own and not common to the rows)
             }
@@ -324,7 +333,7 @@ void prompt_tile_kernel(const PromptParams p) {
 }
 
 // ---- up to 16 rows in all ----
-template <bool MODS>
+template <bool CAP, bool SLOPE>
 __global__ __launch_bounds__(kColWaves * 64, 2)
 void prompt_cols_kernel(const PromptParams p) {
     const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
@@ -345,8 +354,8 @@ void prompt_cols_kernel(const PromptParams p) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qr + operand_dim<false>(s, gr));
     __builtin_amdgcn_sched_barrier(0);
-    const ScoreForm form = score_form(p);
-    const float slope2 = MODS && p.slopes != nullptr ? p.slopes[me.head] * kLog2e : 0.f;
+    const ScoreForm form = score_form<CAP>(p, 1.f);       // (natural units, as the columns' running state has them)
+    const float slope = SLOPE && p.slopes != nullptr ? p.slopes[me.head] : 0.f;
     const uint16_t* k = p.k + (int64_t)b * p.s_b + (int64_t)g * p.s_h;
     const uint16_t* v = p.v + (int64_t)b * p.s_b + (int64_t)g * p.s_h;
 
@@ -368,11 +377,14 @@ void prompt_cols_kernel(const PromptParams p) {
         request_keys<kBf16, false>(rows, k, first_of(t + step), hi - first_of(t + step));       // (past the last tile: nothing)
         const bool masked = j0 < in_lo || (int64_t)j0 + kTileRows > in_hi;
         auto sees = [&](int j) { return j >= me.lo && j < me.hi; };
+        const float far0 = (float)(me.pos - j0 - 4 * gr);
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)       // (natural units, as the columns' running state has them)
-                s[x][i] = MODS ? score_of(s[x][i], form, slope2, me.pos - (j0 + 16 * x + 4 * gr + i)) * (1.f / kLog2e) : s[x][i] * p.scale;
+            for (int i = 0; i < 4; ++i) {
+                s[x][i] = fmaf(bend<CAP>(s[x][i], form), form.a, form.b);
+                if constexpr (SLOPE) s[x][i] = fmaf(-slope, fabsf(far0 - (float)(16 * x + i)), s[x][i]);
+            }
         if (masked) {
             asm volatile("" ::: "memory");    // (a branch: most tiles have nothing to mask)
 #pragma unroll
@@ -549,13 +561,16 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
         p.part_o = (float*)workspace;
         p.part_ml = p.part_o + rows * kD;
     }
-    const bool mods = p.cap > 0.f || p.slopes != nullptr || p.scale == 0.f;      // (a scale of 0: masked products would be 0 times infinity)
+    // (a scale of 0 goes with the slopes: masked products would be 0 times infinity in a weight's exponent)
+    const bool cap = p.cap > 0.f, slope = p.slopes != nullptr || (p.scale == 0.f && !cap);
     hipStream_t st = (hipStream_t)stream;
     if (plan.cols) {
-        auto kernel = mods ? prompt_cols_kernel<true> : prompt_cols_kernel<false>;
+        auto kernel = cap ? (slope ? prompt_cols_kernel<true, true> : prompt_cols_kernel<true, false>)
+                          : (slope ? prompt_cols_kernel<false, true> : prompt_cols_kernel<false, false>);
         hipLaunchKernelGGL(kernel, dim3(plan.splits, geom->n_kv_heads, geom->batch), dim3(kColWaves * 64), 0, st, p);
     } else {
-        auto kernel = mods ? prompt_tile_kernel<true> : prompt_tile_kernel<false>;
+        auto kernel = cap ? (slope ? prompt_tile_kernel<true, true> : prompt_tile_kernel<true, false>)
+                          : (slope ? prompt_tile_kernel<false, true> : prompt_tile_kernel<false, false>);
         const int64_t total = pairs * plan.row_tiles * plan.splits;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((total + 7) / 8 * 8)), dim3(256), 0, st, p);
     }
