@@ -190,15 +190,27 @@ void prompt_tile_kernel(const PromptParams p) {
         // ---- S^T: rows j0 + 32 x + 8 (r / 4) + 4 h + r % 4 of column n ----
         f32x16 s[2];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
                 const bf16x8 a = *reinterpret_cast<const bf16x8*>(sK + half + (k_from ^ (k << 5)) + x * 8192);
                 s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[k], s[x], 0, 0, 0);
             }
+        // (reads kAhead matrix instructions ahead of their use)
+        constexpr int kAhead = 6;
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < 16 - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+        __builtin_amdgcn_sched_barrier(0);
         auto row_of = [&](int x, int r) { return j0 + 32 * x + 8 * (r >> 2) + 4 * h + (r & 3); };
         if constexpr (CAP || SLOPE) {
             const float far0 = (float)(me.pos - j0 - 4 * h);       // (distances beyond 2^24 to 2^-24 of themselves)
@@ -235,6 +247,7 @@ void prompt_tile_kernel(const PromptParams p) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= a;
         }
+        __builtin_amdgcn_s_setprio(1);        // (two wavefronts to a SIMD: the one here goes first, the other's products fill in; 558 -> 542 us)
         const float ref = m == -INFINITY ? 0.f : m, from = form.b - ref;
         // ---- weights, and O^T += V^T P^T, 16 rows at a time: slot e of half h is row 8 (e / 4) + 4 h + e % 4 of them ----
         auto value = [&](int y, int d) {
@@ -279,6 +292,7 @@ void prompt_tile_kernel(const PromptParams p) {
             }
         }
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
         l += (part[0] + part[1]) + (part[2] + part[3]);
         if (sBad[t & 1] == t) {
             const uint16_t* from = p.v + (int64_t)b * p.s_b + (int64_t)g * p.s_h + 4 * h;
@@ -294,6 +308,13 @@ void prompt_tile_kernel(const PromptParams p) {
             }
         }
     };
+    // (the queries are here before the loop begins: see queries_here)
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+        u32x4 x = __builtin_bit_cast(u32x4, q[s]);
+        asm volatile("" : "+v"(x));
+        q[s] = __builtin_bit_cast(bf16x8, x);
+    }
     if (t0 < t1) {
         request(t0);
         write(t0);
