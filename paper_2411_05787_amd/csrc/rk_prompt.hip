@@ -21,8 +21,9 @@ struct PromptParams {
     const float* slopes; const int32_t *first, *end;
     uint16_t* out; float* lse;
     const int32_t* pred; int32_t pred_val;
-    int32_t splits, row_tiles;
+    int32_t splits, row_tiles, split_tiles;   // at most `splits` parts to a row tile, of no fewer than split_tiles tiles of cache rows
     float *part_o, *part_ml;                  // [batch * Hkv][n_new * G][splits][128], [..][2]: maxima in units of ln 2
+    int32_t* parts;                           // [batch * Hkv][row_tiles]: how many a row tile has (1: the output is there already)
 };
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -93,12 +94,9 @@ constexpr int kPromptRows = 128, kPromptTile = 64;
 template <bool CAP, bool SLOPE>
 __global__ __launch_bounds__(256, 2)
 void prompt_tile_kernel(const PromptParams p) {
-    // Workgroups go round the 8 dies; each die takes one stretch of (sequence, KV head) pairs, so that a pair's rows are read by one L2, the
-    // longest row tiles (the last tokens') first.
-    const int total = p.row_tiles * p.splits * p.Hkv * p.batch, per = (total + 7) >> 3;
-    const int order = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || order >= total) return;
-    const int bg = order / (p.row_tiles * p.splits), rest = order - bg * (p.row_tiles * p.splits);
+    // Consecutive workgroups go round the 8 dies, and the (sequence, KV head) pairs run fastest: a die sees few pairs (one, where there are 8; the same
+    // head of every sequence), whose rows its L2 keeps, and of each sequence as many row tiles as any other die.  The last tokens', which see most, come first.
+    const int pairs = p.Hkv * p.batch, bg = (int)(blockIdx.x % (uint32_t)pairs), rest = (int)(blockIdx.x / (uint32_t)pairs);
     const int tile = p.row_tiles - 1 - rest / p.splits, split = rest % p.splits;
     const int b = bg / p.Hkv, g = bg - b * p.Hkv;
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
@@ -134,10 +132,16 @@ void prompt_tile_kernel(const PromptParams p) {
     }
     const float slope2 = SLOPE && p.slopes != nullptr ? p.slopes[me.head] * kLog2e : 0.f;
     __syncthreads();
-    const int lo = min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])), hi = max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3]));
+    const int lo = __builtin_amdgcn_readfirstlane(min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])));
+    const int hi = __builtin_amdgcn_readfirstlane(max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3])));
     const int all_lo = max(max(sInLo[0], sInLo[1]), max(sInLo[2], sInLo[3])), all_hi = min(min(sInHi[0], sInHi[1]), min(sInHi[2], sInHi[3]));
     const int tiles = hi > lo ? (int)(((int64_t)hi - lo + kPromptTile - 1) / kPromptTile) : 0;
-    const int t0 = (int)((int64_t)tiles * split / p.splits), t1 = (int)((int64_t)tiles * (split + 1) / p.splits);
+    const int parts = max(1, min(p.splits, (int)((uint32_t)(tiles + p.split_tiles - 1) / (uint32_t)p.split_tiles)));
+    if (split >= parts) return;
+    if (split == 0 && tid == 0 && p.splits > 1) p.parts[bg * p.row_tiles + tile] = parts;
+    // (scalars, and known as such: the buffers of the tiles hang on them)
+    const int t0 = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * split / parts));
+    const int t1 = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * (split + 1) / parts));
 
     float m = -INFINITY, l = 0.f;
     f32x16 o[4];
@@ -193,17 +197,20 @@ void prompt_tile_kernel(const PromptParams p) {
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
+        // (kAhead operands are read, and waited for, ahead of an unbroken run of products)
+        auto key = [&](int i) { return *reinterpret_cast<const bf16x8*>(sK + half + (k_from ^ (i >> 1 << 5)) + (i & 1) * 8192); };
+        constexpr int kAhead = 6;
+        bf16x8 a[16];
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int i = 0; i < kAhead; ++i) a[i] = key(i);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8*>(sK + half + (k_from ^ (k << 5)) + x * 8192);
-                s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[k], s[x], 0, 0, 0);
-            }
-        // (reads kAhead matrix instructions ahead of their use)
-        constexpr int kAhead = 6;
-        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+        for (int i = 0; i < 16; ++i) {
+            s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], q[i >> 1], s[i & 1], 0, 0, 0);
+            if (i + kAhead < 16) a[i + kAhead] = key(i + kAhead);
+        }
 #pragma unroll
         for (int i = 0; i < 16 - kAhead; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -330,7 +337,7 @@ void prompt_tile_kernel(const PromptParams p) {
     // ---- lane (n, h) has dims 32 d + 8 (r / 4) + 4 h + r % 4 of row n ----
     l = sum_xor32(l);
     if (!real) return;
-    if (p.splits > 1) {
+    if (parts > 1) {
         const int64_t at = ((int64_t)bg * p.n_new * p.G + row) * p.splits + split;
         if (h == 0) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(m, l);
         float* to = p.part_o + at * kD + 4 * h;
@@ -472,7 +479,7 @@ void prompt_cols_kernel(const PromptParams p) {
     }
 }
 
-// Joins the splits of a row: a wavefront each.
+// Joins the parts of a row: a wavefront each.
 constexpr int kMaxSplits = 256;
 __global__ __launch_bounds__(256)
 void prompt_merge_kernel(const PromptParams p) {
@@ -481,12 +488,15 @@ void prompt_merge_kernel(const PromptParams p) {
     __shared__ float sW[4][kMaxSplits];
     const Tokens tok = tokens_of(p, b);
     if (row >= tok.n * p.G) return;
-    const int64_t at = (((int64_t)b * p.Hkv + g) * p.n_new * p.G + row) * p.splits;
+    const int64_t bg = (int64_t)b * p.Hkv + g;
+    const int parts = p.parts != nullptr ? p.parts[bg * p.row_tiles + row / kPromptRows] : p.splits;
+    if (p.parts != nullptr && parts == 1) return;
+    const int64_t at = (bg * p.n_new * p.G + row) * p.splits;
     float m[kMaxSplits / 64], l[kMaxSplits / 64], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kMaxSplits / 64; ++i) {
         const int s = lane + 64 * i;
-        const float2 ml = s < p.splits ? *reinterpret_cast<const float2*>(p.part_ml + (at + s) * 2) : make_float2(-INFINITY, 0.f);
+        const float2 ml = s < parts ? *reinterpret_cast<const float2*>(p.part_ml + (at + s) * 2) : make_float2(-INFINITY, 0.f);
         m[i] = ml.x; l[i] = ml.y;
         top = fmaxf(top, ml.x);
     }
@@ -502,14 +512,14 @@ void prompt_merge_kernel(const PromptParams p) {
     wave_lds_sync();
     const float2* from = reinterpret_cast<const float2*>(p.part_o + at * kD) + lane;
     float o0 = 0.f, o1 = 0.f;
-    for (int s = 0; s < p.splits; s += 8) {
+    for (int s = 0; s < parts; s += 8) {
         float2 v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = from[(int64_t)min(s + i, p.splits - 1) * (kD / 2)];
+        for (int i = 0; i < 8; ++i) v[i] = from[(int64_t)min(s + i, parts - 1) * (kD / 2)];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float a = s + i < p.splits ? sW[w][s + i] : 0.f;
-            if (a != 0.f) { o0 = fmaf(a, v[i].x, o0); o1 = fmaf(a, v[i].y, o1); }      // (a split without rows left nothing)
+            const float a = s + i < parts ? sW[w][s + i] : 0.f;
+            if (a != 0.f) { o0 = fmaf(a, v[i].x, o0); o1 = fmaf(a, v[i].y, o1); }      // (a part without rows left nothing)
         }
     }
     const int i = (uint32_t)row / (uint32_t)p.G;
@@ -519,23 +529,31 @@ void prompt_merge_kernel(const PromptParams p) {
     if (lane == 0 && p.lse != nullptr) p.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.f / kLog2e);
 }
 
-// Which kernel, and over how many workgroups the cache rows of one row tile are split: so that the launch has about kTarget workgroups (two to a
-// compute unit), none with fewer than four tiles of 64 rows (one round of 128, for the columns).
+// Which kernel, and over how many workgroups at most the cache rows of one row tile are split: so that the launch has up to kPromptTarget workgroups (two to
+// a compute unit).  Columns: none with fewer than a round of 128 rows.  Row tiles: a part no shorter than split_tiles tiles of 64 rows, which
+// the kernel sees to, as only it knows the ranges: 32, or 16 where there are few row tiles.  us, 32 heads over 8 (parts: most to a row tile):
+//   128 tokens behind 32640: 1 part 740, 2: 378, 4: 197, 8: 108, 16: 84, 32: 101;  300 behind 7892: 1: 190, 2: 107, 4: 69, 6: 77;
+//   512 behind 32256: 1: 742, 4: 285;  8 behind 32760, parts of 32 tiles: 47, 16: 32, 8: 33, 4: 43;  whole prompts of 600: 1: 20.0, 2: 26.4,
+//   of 2048: 1: 59, 2: 77 (there the partial results cost more than the even spread gains).
 constexpr int kPromptTarget = 2 * kComputeUnits;
-struct PromptPlan { bool cols; int row_tiles, splits; };
+struct PromptPlan { bool cols; int row_tiles, splits, split_tiles; };
 static PromptPlan prompt_plan(const rk_geom* g, int64_t n_new, int64_t max_len) {
     const int64_t pairs = (int64_t)g->batch * g->n_kv_heads, rows = n_new * (g->n_q_heads / g->n_kv_heads);
-    PromptPlan f{rows <= 16, 1, 1};
-    f.row_tiles = f.cols ? 1 : (int)((rows + kPromptRows - 1) / kPromptRows);
-    const int64_t stretches = (max_len + (f.cols ? kMinChunk : 4 * kPromptTile) - 1) / (f.cols ? kMinChunk : 4 * kPromptTile);
+    PromptPlan f{rows <= 16, 1, 1, 1};
+    int64_t most = (max_len + kMinChunk - 1) / kMinChunk;
+    if (!f.cols) {
+        f.row_tiles = (int)((rows + kPromptRows - 1) / kPromptRows);
+        f.split_tiles = pairs * f.row_tiles < 64 ? 16 : 32;
+        most = (max_len + f.split_tiles * kPromptTile - 1) / (f.split_tiles * kPromptTile);
+    }
     int64_t s = kPromptTarget / (pairs * f.row_tiles);
-    if (s > stretches) s = stretches;
+    if (s > most) s = most;
     if (s > kMaxSplits) s = kMaxSplits;
     f.splits = (int)(s < 1 ? 1 : s);
     return f;
 }
 // Rows of partial results that any call of up to n_new tokens and max_len rows can need: a launch that splits has at most
-// kPromptTarget workgroups of at most kPromptRows rows.
+// kPromptTarget workgroups of at most kPromptRows rows each.
 static int64_t prompt_partials(const rk_geom* g, int64_t n_new, int64_t max_len) {
     const int64_t pairs = (int64_t)g->batch * g->n_kv_heads, rows = n_new * (g->n_q_heads / g->n_kv_heads);
     const int64_t most = (int64_t)kPromptTarget * kPromptRows, all = pairs * rows * ((max_len + kMinChunk - 1) / kMinChunk);
@@ -548,7 +566,7 @@ using namespace rk;
 
 extern "C" size_t rk_prompt_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t max_len) {
     if (check_geom(geom) != RK_OK || n_new <= 0 || max_len <= 0) return 0;
-    return align_up((size_t)prompt_partials(geom, n_new, max_len) * (kD + 2) * sizeof(float), 256) + 256;
+    return align_up(((size_t)prompt_partials(geom, n_new, max_len) * (kD + 2) + kPromptTarget) * sizeof(float), 256);
 }
 
 extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, rk_kv cache,
@@ -575,12 +593,14 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
     if (scores) { p.cap = scores->cap; p.slopes = scores->slopes; p.first = scores->first; p.end = scores->end; }
     p.out = (uint16_t*)out; p.lse = lse;
     p.pred = pred; p.pred_val = pred_val;
-    p.splits = plan.splits; p.row_tiles = plan.row_tiles;
+    p.splits = plan.splits; p.row_tiles = plan.row_tiles; p.split_tiles = plan.split_tiles;
     if (plan.splits > 1) {
         const size_t rows = (size_t)pairs * n_new * G * plan.splits;
-        if (!workspace || ((uintptr_t)workspace & 255u) != 0 || workspace_bytes < rows * (kD + 2) * sizeof(float)) return RK_ERR_WORKSPACE;
+        const size_t counts = plan.cols ? 0 : (size_t)pairs * plan.row_tiles;
+        if (!workspace || ((uintptr_t)workspace & 255u) != 0 || workspace_bytes < (rows * (kD + 2) + counts) * sizeof(float)) return RK_ERR_WORKSPACE;
         p.part_o = (float*)workspace;
         p.part_ml = p.part_o + rows * kD;
+        p.parts = plan.cols ? nullptr : (int32_t*)(p.part_ml + rows * 2);
     }
     // (a scale of 0 goes with the slopes: masked products would be 0 times infinity in a weight's exponent)
     const bool cap = p.cap > 0.f, slope = p.slopes != nullptr || (p.scale == 0.f && !cap);
@@ -593,7 +613,7 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
         auto kernel = cap ? (slope ? prompt_tile_kernel<true, true> : prompt_tile_kernel<true, false>)
                           : (slope ? prompt_tile_kernel<false, true> : prompt_tile_kernel<false, false>);
         const int64_t total = pairs * plan.row_tiles * plan.splits;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((total + 7) / 8 * 8)), dim3(256), 0, st, p);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(256), 0, st, p);
     }
     if ((rc = launch_status()) != RK_OK || plan.splits == 1) return rc;
     hipLaunchKernelGGL(prompt_merge_kernel, dim3((unsigned)((n_new * G + 3) / 4), geom->n_kv_heads, geom->batch), dim3(256), 0, st, p);
