@@ -22,8 +22,12 @@ struct PromptParams {
     uint16_t* out; float* lse;
     const int32_t* pred; int32_t pred_val;
     int32_t splits, row_tiles, split_tiles;   // at most `splits` parts to a row tile, of no fewer than split_tiles tiles of cache rows
-    float *part_o, *part_ml;                  // [batch * Hkv][n_new * G][splits][128], [..][2]: maxima in units of ln 2
-    int32_t* parts;                           // [batch * Hkv][row_tiles]: how many a row tile has (1: the output is there already)
+    // partial results, [..][128] and their (maximum in units of ln 2, sum): of row tiles [batch * Hkv][n_new * G][splits], of columns
+    // [Hkv][splits * batch][n_new * G]
+    float *part_o, *part_ml;
+    int32_t* parts;                           // of row tiles [batch * Hkv][row_tiles]: how many (1: the output is there already); of columns
+                                              // [batch * Hkv][2]: the first one's number and how many
+    int32_t cols, ragged;                     // ragged != 0 (= batch): the columns' workgroups are shared out by length
 };
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -89,6 +93,7 @@ __device__ __forceinline__ float only_non_finite(float v) { return (__float_as_u
 
 // ---- 128 rows to a workgroup ----
 constexpr int kPromptRows = 128, kPromptTile = 64;
+constexpr int kMaxSplits = 256;
 
 // SLOPE: scores are worked out one by one, not in the weights' exponents.
 template <bool CAP, bool SLOPE>
@@ -364,11 +369,21 @@ void prompt_tile_kernel(const PromptParams p) {
 template <bool CAP, bool SLOPE>
 __global__ __launch_bounds__(kColWaves * 64, 2)
 void prompt_cols_kernel(const PromptParams p) {
-    const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+    const int g = blockIdx.y, slot = (int)(blockIdx.z * gridDim.x + blockIdx.x);
+    int b = blockIdx.z, split = blockIdx.x, parts = p.splits;
+    if (p.ragged != 0) {                      // (sequences by their lengths: what the ranges leave of them is not known here)
+        AttnParams a;
+        a.ragged_batch = p.ragged; a.nch = p.splits; a.share_cap = kMaxSplits; a.cap2 = p.cap_rows; a.max_rows2 = p.max_len;
+        const RaggedSlot r = ragged_slot<false>(a, p.seq_lens, slot);
+        if (r.b < 0) return;
+        b = r.b; split = r.c; parts = r.nchunks;
+    }
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
     const Tokens tok = tokens_of(p, b);
     const int n_rows = tok.n * p.G;
     if (n_rows == 0) return;
+    const int64_t bg = (int64_t)b * p.Hkv + g;
+    if (p.splits > 1 && split == 0 && threadIdx.x == 0) { p.parts[2 * bg] = slot; p.parts[2 * bg + 1] = parts; }
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, gr = lane >> 4;
     const bool real = col < n_rows;
     const Query me = query_of(p, tok, b, g, min(col, n_rows - 1));
@@ -390,7 +405,7 @@ void prompt_cols_kernel(const PromptParams p) {
     ColState st;
     st.clear();
     TileRows<kBf16> rows;
-    const int step = p.splits * kColWaves;
+    const int step = parts * kColWaves;
     int t = split * kColWaves + w;
     auto first_of = [&](int x) { return lo + x * kTileRows; };        // (past the rows there are by a round at most: see check_kv)
     if (t < tiles) {
@@ -452,14 +467,14 @@ void prompt_cols_kernel(const PromptParams p) {
 
     __shared__ __attribute__((aligned(16))) ColMergeLds lds;
     __shared__ float sInv[16];
-    const int64_t bg = (int64_t)b * p.Hkv + g;
     if (p.splits > 1) {
+        const int64_t at = ((int64_t)g * p.splits * p.batch + slot) * p.n_new * p.G;
         merge_columns(lds, st, n_rows,
                       [&](int x, int d, float o0, float o1) {
-                          *reinterpret_cast<float2*>(p.part_o + ((bg * p.n_new * p.G + x) * p.splits + split) * kD + d) = make_float2(o0, o1);
+                          *reinterpret_cast<float2*>(p.part_o + (at + x) * kD + d) = make_float2(o0, o1);
                       },
                       [&](int x, float m, float l) {
-                          *reinterpret_cast<float2*>(p.part_ml + ((bg * p.n_new * p.G + x) * p.splits + split) * 2) = make_float2(m * kLog2e, l);
+                          *reinterpret_cast<float2*>(p.part_ml + (at + x) * 2) = make_float2(m * kLog2e, l);
                       });
         return;
     }
@@ -480,7 +495,6 @@ void prompt_cols_kernel(const PromptParams p) {
 }
 
 // Joins the parts of a row: a wavefront each.
-constexpr int kMaxSplits = 256;
 __global__ __launch_bounds__(256)
 void prompt_merge_kernel(const PromptParams p) {
     const int g = blockIdx.y, b = blockIdx.z, w = threadIdx.x >> 6, lane = threadIdx.x & 63, row = blockIdx.x * 4 + w;
@@ -489,14 +503,16 @@ void prompt_merge_kernel(const PromptParams p) {
     const Tokens tok = tokens_of(p, b);
     if (row >= tok.n * p.G) return;
     const int64_t bg = (int64_t)b * p.Hkv + g;
-    const int parts = p.parts != nullptr ? p.parts[bg * p.row_tiles + row / kPromptRows] : p.splits;
-    if (p.parts != nullptr && parts == 1) return;
-    const int64_t at = (bg * p.n_new * p.G + row) * p.splits;
+    const int rows = p.n_new * p.G, parts = p.cols ? p.parts[2 * bg + 1] : p.parts[bg * p.row_tiles + row / kPromptRows];
+    if (!p.cols && parts == 1) return;
+    // part s of this row is at + s * step
+    const int64_t at = p.cols ? ((int64_t)g * p.splits * p.batch + p.parts[2 * bg]) * rows + row : (bg * rows + row) * p.splits;
+    const int step = p.cols ? rows : 1;
     float m[kMaxSplits / 64], l[kMaxSplits / 64], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kMaxSplits / 64; ++i) {
         const int s = lane + 64 * i;
-        const float2 ml = s < parts ? *reinterpret_cast<const float2*>(p.part_ml + (at + s) * 2) : make_float2(-INFINITY, 0.f);
+        const float2 ml = s < parts ? *reinterpret_cast<const float2*>(p.part_ml + (at + (int64_t)s * step) * 2) : make_float2(-INFINITY, 0.f);
         m[i] = ml.x; l[i] = ml.y;
         top = fmaxf(top, ml.x);
     }
@@ -515,7 +531,7 @@ void prompt_merge_kernel(const PromptParams p) {
     for (int s = 0; s < parts; s += 8) {
         float2 v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = from[(int64_t)min(s + i, parts - 1) * (kD / 2)];
+        for (int i = 0; i < 8; ++i) v[i] = from[(int64_t)min(s + i, parts - 1) * step * (kD / 2)];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float a = s + i < parts ? sW[w][s + i] : 0.f;
@@ -596,11 +612,13 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
     p.splits = plan.splits; p.row_tiles = plan.row_tiles; p.split_tiles = plan.split_tiles;
     if (plan.splits > 1) {
         const size_t rows = (size_t)pairs * n_new * G * plan.splits;
-        const size_t counts = plan.cols ? 0 : (size_t)pairs * plan.row_tiles;
+        const size_t counts = (size_t)pairs * (plan.cols ? 2 : plan.row_tiles);
         if (!workspace || ((uintptr_t)workspace & 255u) != 0 || workspace_bytes < (rows * (kD + 2) + counts) * sizeof(float)) return RK_ERR_WORKSPACE;
         p.part_o = (float*)workspace;
         p.part_ml = p.part_o + rows * kD;
-        p.parts = plan.cols ? nullptr : (int32_t*)(p.part_ml + rows * 2);
+        p.parts = (int32_t*)(p.part_ml + rows * 2);
+        p.cols = plan.cols ? 1 : 0;
+        p.ragged = plan.cols ? ragged_batch_of(geom) : 0;
     }
     // (a scale of 0 goes with the slopes: masked products would be 0 times infinity in a weight's exponent)
     const bool cap = p.cap > 0.f, slope = p.slopes != nullptr || (p.scale == 0.f && !cap);
