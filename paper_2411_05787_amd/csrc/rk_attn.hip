@@ -1423,9 +1423,7 @@ __device__ __forceinline__ void block_head_lse(const AttnParams& p, int G, int64
     const double L64 = block_sum_f64<4>((double)wgt * (double)l, reinterpret_cast<double*>(s.red));
     if (tid == 0) {
         float hi = -INFINITY, lo = 0.f;
-        if (p.keep_nan != 0 && L64 != L64) {
-            hi = (float)L64;
-        } else if (L64 > 0.0 && fp32_log) {
+        if (L64 > 0.0 && fp32_log) {
             hi = M + __logf((float)L64);
         } else if (L64 > 0.0) {
             const double l64 = (double)M + log(L64);
@@ -1473,7 +1471,7 @@ __device__ __forceinline__ void block_head_out(const AttnParams& p, int G, int b
     __syncthreads();
     if (tid < kD) {
         const float L = (float)s.L64;
-        const float o = L > 0.f || (p.keep_nan != 0 && L != L) ? (s.acc[0][tid] + s.acc[1][tid] + s.acc[2][tid] + s.acc[3][tid]) / L : 0.f;
+        const float o = L > 0.f ? (s.acc[0][tid] + s.acc[1][tid] + s.acc[2][tid] + s.acc[3][tid]) / L : 0.f;
         p.out[((int64_t)b * p.Hq + h) * kD + tid] = f32_to_bf16(o);
     }
     if (tid == 0) p.lse[(int64_t)b * p.Hq + h] = s.lse[0];
@@ -1934,7 +1932,11 @@ int full_attn_stage(const rk_geom* geom, const void* q, rk_kv full, const int32_
                   : launch_split<true, false>(p, geom->batch, G, nchunk_grid, st);
     }
     if (rc != RK_OK || scores_only) return rc;
-    if (!fused) return merge_weights_stage(p, geom->batch, max_len, st);
+    if (!fused) {
+        dim3 grid(1 + (max_len + kNormTile - 1) / kNormTile, geom->n_q_heads, geom->batch);
+        hipLaunchKernelGGL(merge_normalise_kernel, grid, dim3(256), 0, st, p, G);
+        return launch_status();
+    }
     if (defer_pool) {            // only the output is finished now; pool_batched_stage does the rest later
         if (merge_inside) return rc;
         p.weights = nullptr;
@@ -1953,13 +1955,6 @@ int full_attn_stage(const rk_geom* geom, const void* q, rk_kv full, const int32_
         case 8: return launch_finish_pool<8>(p, geom->batch, max_len, ws, pool_half, agg, st);
         default: return RK_ERR_UNSUPPORTED;
     }
-}
-
-// The launch that ends a step whose split kernel left raw scores in p.weights (or none) and partial results: merge, lse, weights.
-int merge_weights_stage(const AttnParams& p, int batch, int32_t max_len, hipStream_t st) {
-    const dim3 grid(p.weights ? 1 + (max_len + kNormTile - 1) / kNormTile : 1, p.Hq, batch);
-    hipLaunchKernelGGL(merge_normalise_kernel, grid, dim3(256), 0, st, p, p.Hq / p.Hkv);
-    return launch_status();
 }
 
 // The attention of an H2O step: raw scores to ws.scores, partial results to ws.part_ml / part_o, n_attend[b] set.

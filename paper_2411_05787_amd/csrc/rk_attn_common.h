@@ -35,7 +35,6 @@ struct AttnParams {
     int32_t* mark_tail; int32_t* mark_count;  // the gather inside the step only: tail_start <- seq_lens, refreshes counted (may be NULL)
     int32_t ragged_batch;              // != 0 (= batch): workgroups are shared out by length, see ragged_share_lane
     int32_t share_cap;                 // ... at most this many to a sequence
-    int32_t keep_nan;                  // the merge leaves NaN where the sums are NaN (0: zeros, as the steps over bf16 caches have it)
     int32_t* n_attend;                 // APPEND only: [B], rows attended over, for the kernel that follows
     int32_t slice_merge;               // TAGGED: every workgroup merges a slice of the output (all workgroups of the launch are resident together)
     int32_t slice_spin;                // ... re-reading rows still in flight at most this often before it leaves its slice to the last one
@@ -45,10 +44,6 @@ struct AttnParams {
 // idx given: the gather inside the step.
 __attribute__((visibility("hidden")))
 int launch_partial_tile(const AttnParams& p, int batch, int G, const TileForm& form, bool trig, const int32_t* idx, hipStream_t st);
-
-// The launch that merges a split kernel's partial results and turns the raw scores in p.weights (may be NULL) into weights.
-__attribute__((visibility("hidden")))
-int merge_weights_stage(const AttnParams& p, int batch, int32_t max_len, hipStream_t st);
 
 constexpr int kSplitWaves = 4, kTileRows = 32;
 constexpr int kNoTailWg = 0xff;                   // top byte of the kernel argument s_b_and_tail: no workgroup for the tail rows

@@ -2,13 +2,20 @@
 //
 // The step streams 256 bytes of a KV head's row instead of 512 and is bound by that: what the matrix cores and the conversions take
 // fits behind it.  The scale of a block of rows multiplies its scores (K) and its weights (V), never the rows.  Split, work shares of
-// ragged batches, the layout of the partial results and the kernel that merges them and normalises the weights are those of the step over
-// the bf16 cache (rk_attn_common.h).
+// ragged batches and the layout of the partial results are those of the step over the bf16 cache (rk_attn_common.h).
 #include "rk_cols.h"
 
 namespace rk {
 
 struct Q8Rows { const uint8_t *k, *v; const float *ks, *vs; const uint16_t *kt, *vt; int64_t s_b; int32_t s_h, blocks, shift; };
+
+// Workgroups per (sequence, KV head): with the scores returned as the step over the bf16 cache has it, without them one to a compute unit, as
+// no stores come between the requests.  us by workgroups in all (256 / 512 / 768 / 1024), 32 heads over 8, e4m3: with weights 32777 rows 21.0 /
+// 21.3 / 22.4 / 24.3, 65536 37.4 / 34.4 / 34.9 / 34.6, 131072 71.7 / 70.4 / 68.0 / 65.4, without 65536 26.5 / 26.6 / 28.2 / 28.7, 4 sequences of
+// 32768 45.0 / 46.7 / 47.2 / 47.6, 16 ragged ones of up to 16384, 28 over 4, int8 36.2 / 35.6 / 35.7 / 38.9.
+static int q8_split_workgroups(const rk_geom* g, int32_t max_len, bool weights) {
+    return split_workgroups(max_len, (int64_t)g->batch * g->n_kv_heads, kMaxChunks, weights ? emit_split_target(g, max_len) : kComputeUnits);
+}
 
 // Tiles of a sequence of len rows (of which the call looks at the first n): those of whole blocks, then those of the tail.
 template <int FORMAT, bool EMIT>
@@ -46,6 +53,8 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
 
     ColState st;
     st.clear();
+    // (where scores are returned: this lane's row of them, and where it has 16 bytes of a whole tile's line of 128)
+    float* wline = EMIT ? p.weights + ((int64_t)b * p.Hq + g * G + (col >= G ? min(col - G, G - 1) : col)) * p.w_stride + (col >= G ? 16 : 0) : nullptr;
     float* wrow = EMIT ? p.weights + ((int64_t)b * p.Hq + g * G + min(col, G - 1)) * p.w_stride : nullptr;
     // scores of rows first .. first + 31, the first `rows` of which exist
     auto finish_scores = [&](float (&s)[2][4], int first, int rows, float k0, float k1) {
@@ -54,17 +63,22 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[x][i] *= x ? k1 : k0;
         }
-        if (EMIT && col < G) {
-            float* to = wrow + first + 4 * gr;
-            if (p.w_vec != 0 && rows >= kTileRows) {      // (the same for the whole wavefront)
-                *reinterpret_cast<float4*>(to) = make_float4(s[0][0], s[0][1], s[0][2], s[0][3]);
-                *reinterpret_cast<float4*>(to + 16) = make_float4(s[1][0], s[1][1], s[1][2], s[1][3]);
-            } else {
+        if (EMIT && p.w_vec != 0 && rows >= kTileRows) {      // (the same for the whole wavefront)
+            // the second block's scores to the lanes behind the group's: whole lines of 128 bytes leave in one store
+            const int from = (lane & 48) + (col >= G ? col - G : col);
+            float4 v;
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) if (16 * x + 4 * gr + i < rows) to[16 * x + i] = s[x][i];
+            for (int i = 0; i < 4; ++i) {
+                const float up = __int_as_float(__builtin_amdgcn_ds_bpermute(from * 4, __float_as_int(s[1][i])));
+                (&v.x)[i] = col < G ? s[0][i] : up;
             }
+            if (col < 2 * G) *reinterpret_cast<float4*>(wline + first + 4 * gr) = v;
+        } else if (EMIT && col < G) {
+            float* to = wrow + first + 4 * gr;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (16 * x + 4 * gr + i < rows) to[16 * x + i] = s[x][i];
         }
         if (rows < kTileRows) {
 #pragma unroll
@@ -132,6 +146,121 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
                   [&](int x, float m, float l) { *reinterpret_cast<float2*>(ml + 2 * x) = make_float2(m, l); });
 }
 
+// The launch behind it.  Workgroups x < G: the output of query head x of the group, four wavefronts with every fourth partial result each.  The
+// others: kWeightTile positions of all G heads, raw scores -> weights in place, requested before the log-sum-exps that they wait for are worked
+// out, by a wavefront each.  Every wavefront that needs a head's statistics reduces them by itself, without a barrier.
+constexpr int kWeightTile = 1024, kOutRound = 16;
+struct HeadStats { float M; double L; };
+// a[i]: what partial result lane + 64 i weighs.
+__device__ __forceinline__ HeadStats head_stats(const AttnParams& p, int G, int64_t bg, int gi, int nchunks, float (&a)[kMaxChunks / 64]) {
+    const float* ml = p.part_ml + (bg * kMaxChunks * G + gi) * 2;
+    const int lane = threadIdx.x & 63;
+    float2 t[kMaxChunks / 64];
+#pragma unroll
+    for (int i = 0; i < kMaxChunks / 64; ++i)
+        t[i] = lane + 64 * i < nchunks ? *reinterpret_cast<const float2*>(ml + (int64_t)(lane + 64 * i) * G * 2) : make_float2(-INFINITY, 0.f);
+    float m = fmaxf(fmaxf(t[0].x, t[1].x), fmaxf(t[2].x, t[3].x));
+    m = wave_max(m);
+    double l = 0.0;
+#pragma unroll
+    for (int i = 0; i < kMaxChunks / 64; ++i) {
+        a[i] = t[i].x == -INFINITY ? 0.f : fast_exp2((t[i].x - m) * kLog2e);
+        l += (double)a[i] * (double)t[i].y;
+    }
+    return {m, wave_sum(l)};
+}
+// log-sum-exp as hi + lo (no rows: -inf; a NaN among the sums: NaN).
+__device__ __forceinline__ float2 head_lse(const HeadStats& s) {
+    if (s.L == 0.0) return make_float2(-INFINITY, 0.f);
+    const double x = (double)s.M + log(s.L);
+    const float hi = (float)x;
+    return make_float2(hi, (float)(x - (double)hi));
+}
+static_assert(kMaxChunks == 256, "statistics in four registers to a lane");
+
+__global__ __launch_bounds__(256)
+void q8_finish_kernel(const AttnParams p) {
+    const int x = blockIdx.x, g = blockIdx.y, b = blockIdx.z, G = p.Hq / p.Hkv;
+    if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
+    const int len = clamped_len(p.seq_lens[b], p.cap2, p.max_rows2), j0 = (x - G) * kWeightTile;
+    if (x >= G && j0 >= len) return;
+    const int64_t bg = (int64_t)b * p.Hkv + g;
+    const int nchunks = p.ragged_batch != 0 ? stored_chunks(p.counters, bg) : active_workgroups(len, p.nch);
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t head0 = (int64_t)b * p.Hq + g * G;
+    if (x >= G) {
+        __shared__ float2 sLse[RK_MAX_GROUP];
+        float* rows = p.weights + head0 * p.w_stride + j0;
+        const int n = len - j0;
+        float v[RK_MAX_GROUP][4];
+        const bool vec = p.w_vec != 0 && n >= kWeightTile;
+#pragma unroll
+        for (int gi = 0; gi < RK_MAX_GROUP; ++gi) {
+            if (gi >= G) break;
+            const float* row = rows + gi * p.w_stride;
+            if (vec) {
+                const float4 f = *reinterpret_cast<const float4*>(row + 4 * tid);
+                v[gi][0] = f.x; v[gi][1] = f.y; v[gi][2] = f.z; v[gi][3] = f.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[gi][i] = tid + 256 * i < n ? row[tid + 256 * i] : 0.f;
+            }
+        }
+        for (int gi = w; gi < G; gi += 4) {
+            float a[kMaxChunks / 64];
+            const float2 lse = head_lse(head_stats(p, G, bg, gi, nchunks, a));
+            if (lane == 0) sLse[gi] = lse;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int gi = 0; gi < RK_MAX_GROUP; ++gi) {
+            if (gi >= G) break;
+            float* row = rows + gi * p.w_stride;
+            const float nl = -sLse[gi].x, ll = sLse[gi].y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[gi][i] = weight_of(v[gi][i], nl, ll);
+            if (vec) {
+                *reinterpret_cast<float4*>(row + 4 * tid) = make_float4(v[gi][0], v[gi][1], v[gi][2], v[gi][3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (tid + 256 * i < n) row[tid + 256 * i] = v[gi][i];
+            }
+        }
+        return;
+    }
+    __shared__ float sW[4][kMaxChunks];
+    __shared__ float2 sOut[4][64];
+    const float2* po = reinterpret_cast<const float2*>(p.part_o + (bg * p.max_chunks * G + x) * kD) + lane;
+    float2 v[kOutRound];
+    auto request = [&](int c0) {
+#pragma unroll
+        for (int u = 0; u < kOutRound; ++u) v[u] = po[(int64_t)min(c0 + 4 * u, nchunks - 1) * G * (kD / 2)];
+    };
+    request(w);
+    float a[kMaxChunks / 64];
+    const HeadStats st = head_stats(p, G, bg, x, nchunks, a);
+#pragma unroll
+    for (int i = 0; i < kMaxChunks / 64; ++i) sW[w][lane + 64 * i] = a[i];
+    wave_lds_sync();
+    float o0 = 0.f, o1 = 0.f;
+    for (int c0 = w; c0 < nchunks; c0 += 4 * kOutRound) {
+        if (c0 != w) request(c0);
+#pragma unroll
+        for (int u = 0; u < kOutRound; ++u) {
+            const float wc = c0 + 4 * u < nchunks ? sW[w][c0 + 4 * u] : 0.f;
+            o0 = fmaf(wc, v[u].x, o0); o1 = fmaf(wc, v[u].y, o1);
+        }
+    }
+    sOut[w][lane] = make_float2(o0, o1);
+    __syncthreads();
+    if (w != 0) return;
+    const float inv = st.L == 0.0 ? 0.f : 1.f / (float)st.L;
+    uint16_t* out = p.out + (head0 + x) * kD + 2 * lane;
+    out[0] = f32_to_bf16((sOut[0][lane].x + sOut[1][lane].x + sOut[2][lane].x + sOut[3][lane].x) * inv);      // (out is 2-byte aligned)
+    out[1] = f32_to_bf16((sOut[0][lane].y + sOut[1][lane].y + sOut[2][lane].y + sOut[3][lane].y) * inv);
+    if (lane == 0 && p.lse != nullptr) p.lse[head0 + x] = head_lse(st).x;
+}
+
 // rk_gather_small_kv out of a cache of 8 bits: 16 lanes to a row.
 constexpr int kGatherRows8 = 16;
 template <int FORMAT>
@@ -189,16 +318,15 @@ extern "C" int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8*
     AttnParams p{};
     p.q = (const uint16_t*)q;
     p.seq_lens = seq_lens; p.max_rows2 = max_len; p.cap2 = (int32_t)full->capacity;
-    p.nch = emit_split_workgroups(geom, max_len);
+    p.nch = q8_split_workgroups(geom, max_len, weights != nullptr);
     p.Hq = geom->n_q_heads; p.Hkv = geom->n_kv_heads;
     p.scale = geom->scale;
     p.out = (uint16_t*)out;
     p.weights = weights; p.w_stride = w_stride; p.w_vec = weights && w_stride % 4 == 0 && aligned16(weights) ? 1 : 0;
-    p.lse = lse ? lse : ws.lse;
+    p.lse = lse;
     p.pred = pred; p.pred_val = pred_val;
     p.counters = ws.counters; p.part_ml = ws.part_ml; p.part_o = ws.part_o; p.max_chunks = ws.max_chunks;
     p.ragged_batch = ragged_batch_of(geom); p.share_cap = kMaxChunks;
-    p.keep_nan = 1;                           // (a block that held one has NaN as its scale)
     const Q8Rows rows{(const uint8_t*)full->k, (const uint8_t*)full->v, full->k_scale, full->v_scale, (const uint16_t*)full->k_tail,
                       (const uint16_t*)full->v_tail, full->stride_b, (int32_t)full->stride_h, (int32_t)(full->capacity / full->block),
                       full->block == 16 ? 4 : full->block == 32 ? 5 : full->block == 64 ? 6 : 7};
@@ -208,7 +336,9 @@ extern "C" int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8*
                        : (weights ? q8_attn_kernel<RK_Q8_INT8, true> : q8_attn_kernel<RK_Q8_INT8, false>);
     hipLaunchKernelGGL(kernel, grid, dim3(kColWaves * 64), 0, (hipStream_t)stream, p, rows);
     if ((rc = launch_status()) != RK_OK) return rc;
-    return merge_weights_stage(p, geom->batch, max_len, (hipStream_t)stream);
+    const int tiles = weights ? (max_len + kWeightTile - 1) / kWeightTile : 0;
+    hipLaunchKernelGGL(q8_finish_kernel, dim3(geom->n_q_heads / geom->n_kv_heads + tiles, geom->n_kv_heads, geom->batch), dim3(256), 0, (hipStream_t)stream, p);
+    return launch_status();
 }
 
 extern "C" int rk_gather_small_kv_q8(const rk_geom* geom, const rk_kv8* full, const int32_t* idx, int32_t k, rk_kv small,
