@@ -24,6 +24,15 @@
  *   rk_query_sim        the query-similarity test that decides whether a full step is
  *                       needed          (Section 2.2, "Deciding when to decode with full cache")
  *
+ * and what a decode step needs around it:
+ *
+ *   rk_rope_append      rotary positions of new tokens (table: rk_rope_table), and their rows into C_f;
+ *   rk_rope_append_q8   the same into a cache of 8 bits
+ *   rk_full_attn_q8, rk_gather_small_kv_q8
+ *                       the full step over a C_f of 8 bits, and C_p out of it
+ *   rk_prompt_attn      attention of a prompt, a chunk of one, drafted tokens or a single token over C_f, with capped scores,
+ *                       a bias by distance, documents, prefixes and windows
+ *
  * General rules
  * -------------
  * - Every tensor pointer is a DEVICE pointer owned by the caller; `stream` is a hipStream_t
@@ -669,7 +678,10 @@ int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8* full, cons
 
 /* rk_gather_small_kv out of a cache of 8 bits into a bf16 small cache: small.k[b,g,i,:] = the row idx[b,g,i] as the cache stands for it,
  * rounded to bf16 (exact where the scale is a power of two; bit copies from the tail).  Slots whose idx is outside
- * [0, seq_lens[b]) are left untouched.  seq_lens is required; tail_start (optional) <- seq_lens. */
+ * [0, seq_lens[b]) are left untouched.  seq_lens is required; tail_start (optional) <- seq_lens.
+ * The partial steps behind it take the tokens since the refresh as bf16 rows, like the small cache's: with one bf16 buffer whose first k
+ * rows are the small cache and whose next ones rk_rope_append fills (seq_lens = k + tokens since the refresh there, their positions given), they
+ * are rk_partial_attn's full cache, with tail_start = k. */
 int rk_gather_small_kv_q8(const rk_geom* geom, const rk_kv8* full, const int32_t* idx, int32_t k, rk_kv small,
                           const int32_t* seq_lens, int32_t* tail_start,
                           const int32_t* pred, int32_t pred_val, void* stream);
@@ -703,9 +715,9 @@ size_t rk_prompt_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t max
  *     out[b,i,h,:] = sum_j softmax(s)[j] * V[b,g,j,:]          lse[b,i,h] = log sum_j exp(s[j])
  *   q    bf16, row (b, i, h) at q + b * q_stride_b + i * q_stride_t + h * 128; 16-byte aligned, strides multiples of 8
  *   out  bf16 [batch, n_new, n_q_heads, 128] contiguous, 16-byte aligned;  lse fp32 [batch, n_new, n_q_heads] or NULL
- * A token that sees no row gets out = 0 and lse = -inf; entries beyond n are left as they were.  Rows that a token does not see have no part in its
- * result, whatever they hold (infinities and NaN included; one that it sees makes its output infinite or NaN).  With more than 16 / G new tokens the softmax weights enter the product with V as
- * bf16 (sums in fp32), with fewer to 2^-17. */
+ * A token that sees no row gets out = 0 and lse = -inf; entries beyond n are left as they were.  Rows that a token does not see have no
+ * part in its result, whatever they hold (infinities and NaN included; one that it sees makes its output infinite or NaN).  The softmax
+ * weights enter the product with V as bf16 where n_new * G > 16, to 2^-17 where it is less; sums are fp32. */
 int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, rk_kv cache,
                    const int32_t* seq_lens, const int32_t* new_lens, int32_t max_len, const rk_prompt_scores* scores,
                    void* out, float* lse, const int32_t* pred, int32_t pred_val,

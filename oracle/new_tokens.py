@@ -50,7 +50,7 @@ def e4m3_values() -> np.ndarray:
 def nearest_value(x: np.ndarray, fmt: str) -> np.ndarray:
     """The nearest value of the format, ties to the even code (e4m3) or number (int8); |x| within its range."""
     if fmt == "int8":
-        return np.rint(x)
+        return np.rint(x) + 0.0                                                  # (whole numbers have one zero)
     v = e4m3_values()
     a = np.abs(x)
     hi = np.clip(np.searchsorted(v, a), 0, len(v) - 1)
