@@ -2,13 +2,15 @@
 //
 // The query heads of a group and the new tokens are one axis, row = token * G + head, so a tile of rows shares every K and V row that it
 // reads among the group's heads too.  Two kernels:
-//   prompt_tile_kernel  128 rows to a workgroup, 64 cache rows at a time through LDS, everything on the matrix cores:
-//                       bound by those and by the softmax between the two products;
+//   prompt_tile_kernel  128 or 256 rows to a workgroup, the cache rows through LDS, everything on the matrix cores: bound by those, by the
+//                       softmax between the two products and, in long calls, by the power that both draw;
 //   prompt_cols_kernel  up to 16 rows in all (a decode step's token, a few drafted ones): the cache streams past once, bound by memory
 //                       (rk_cols.h).
 // A row r sees cache rows lo <= j < hi.  Tiles that no row of a workgroup sees are never read; only those that a bound runs through are masked.
 // Where there are few rows the cache rows are split over workgroups, and prompt_merge_kernel joins their (maximum, sum, output).
 #include "rk_cols.h"
+
+#include <type_traits>
 
 namespace rk {
 
@@ -53,9 +55,14 @@ __device__ __forceinline__ Query query_of(const PromptParams& p, const Tokens& t
 }
 
 __device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o));
-    return __builtin_amdgcn_readfirstlane(v);
+    auto moved = [](int x, auto how) { return __float_as_int(dpp_move_f<decltype(how)::value>(__int_as_float(x))); };
+    v = min(v, moved(v, std::integral_constant<int, kDppXor1>{}));
+    v = min(v, moved(v, std::integral_constant<int, kDppXor2>{}));
+    v = min(v, moved(v, std::integral_constant<int, kDppRor4>{}));
+    v = min(v, moved(v, std::integral_constant<int, kDppRor8>{}));
+    const LanePair a = rows_xor16(v);
+    const LanePair b = halves_xor32(min(a.a, a.b));
+    return __builtin_amdgcn_readfirstlane(min(b.a, b.b));
 }
 __device__ __forceinline__ int wave_max_i(int v) { return ~wave_min(~v); }
 
@@ -77,10 +84,10 @@ __device__ __forceinline__ float bend(float x, const ScoreForm& f) {
 // Infinities and NaN of V in a tile of which a row sees a part.  A weight of 0 times one of them would be NaN in rows that do not see it, so such
 // tiles are multiplied with zeros in their place, and the rows that see one get it added afterwards, read from memory once more.
 __device__ __forceinline__ bool has_non_finite(u32x4 v) {
-    bool bad = false;
+    uint32_t bad = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad = bad || (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
-    return bad;
+    for (int i = 0; i < 4; ++i) bad |= (uint32_t)((v[i] & 0x7f80u) == 0x7f80u) | (uint32_t)((v[i] & 0x7f800000u) == 0x7f800000u);
+    return bad != 0;
 }
 __device__ __forceinline__ void drop_non_finite(u32x4& v) {
 #pragma unroll
@@ -91,14 +98,25 @@ __device__ __forceinline__ void drop_non_finite(u32x4& v) {
 }
 __device__ __forceinline__ float only_non_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? v : 0.f; }
 
-// ---- 128 rows to a workgroup ----
-constexpr int kPromptRows = 128, kPromptTile = 64;
-constexpr int kMaxSplits = 256;
+// ---- 128 or 256 rows to a workgroup ----
+//   S^T = K Q^T   v_mfma_f32_32x32x16_bf16: lane (n, h) = (lane % 32, lane / 32) gets column (row of the tile) n, cache rows 8 (r / 4) + 4 h + r % 4 of a
+//                 block of 32;
+//   O^T += V^T P^T  the contraction slots are numbered as S^T left the rows in the lanes, so P goes from the softmax to the matrix cores without
+//                 leaving its lane; V is turned around by the transposing reads of LDS.
+// A wavefront takes 32 QB rows and works a block at a time, in stages of 16 QB slots: while the products of the block ahead (S^T) and of the one behind (O^T) are on the matrix
+// cores, it makes weights of the scores between them, a matrix instruction and about five others to a slot.  K and V come through LDS, whose rows are padded so that
+// no two lanes of a read's phase meet in a bank: rings of 4 QB blocks, a barrier to QB stages.
+// 8192 tokens, 32 heads over 8, QB = 2: 519 us, 1059 TFLOP/s (a library matrix product of 8192^3 beside it 1350; with zeros for data, which draw less
+// power, 1236 and 1800).  Three capped chunks, QB = 1: 69 us, 480 TFLOP/s.  Without stages, two tiles of 64 rows in LDS and a barrier a tile: 554 and 76 us.
+constexpr int kPromptRows = 128, kPromptTile = 64, kMaxSplits = 256;      // (cache rows are split over workgroups in tiles of two blocks)
+constexpr int kBlockRows = 32;
+constexpr int kKRow = kD * 2 + 16, kVRow = kD * 2 + 64;     // bytes from row to row in LDS: the reads of a phase fall on different banks
+constexpr int kKBlock = kBlockRows * kKRow, kVBlock = kBlockRows * kVRow;
 
-// SLOPE: scores are worked out one by one, not in the weights' exponents.
-template <bool CAP, bool SLOPE>
-__global__ __launch_bounds__(256, 2)
+template <int QB, bool CAP, bool SLOPE>
+__global__ __launch_bounds__(256, QB == 1 ? 2 : 1)
 void prompt_tile_kernel(const PromptParams p) {
+    constexpr int kRows = kPromptRows * QB, kSlots = 16 * QB, kRing = 4 * QB, kAheadK = 2 + QB, kAheadV = QB;
     // Consecutive workgroups go round the 8 dies, and the (sequence, KV head) pairs run fastest: a die sees few pairs (one, where there are 8; the same
     // head of every sequence), whose rows its L2 keeps, and of each sequence as many row tiles as any other die.  The last tokens', which see most, come first.
     const int pairs = p.Hkv * p.batch, bg = (int)(blockIdx.x % (uint32_t)pairs), rest = (int)(blockIdx.x / (uint32_t)pairs);
@@ -107,262 +125,371 @@ void prompt_tile_kernel(const PromptParams p) {
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
     const Tokens tok = tokens_of(p, b);
     const int n_rows = tok.n * p.G;
-    if (tile * kPromptRows >= n_rows) return;
+    if (tile * kRows >= n_rows) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-    const int row = tile * kPromptRows + w * 32 + n;
-    const bool real = row < n_rows;
-    const Query me = query_of(p, tok, b, g, min(row, n_rows - 1));
-
-    // two tiles of K and V: one is worked on while the next is written
-    constexpr int kHalf = kPromptTile * kD * 2;
-    __shared__ __attribute__((aligned(16))) unsigned char sK[2 * kHalf], sV[2 * kHalf];
-    __shared__ int sLo[4], sHi[4], sInLo[4], sInHi[4], sBad[2];
-
-    // ranges: of the wavefront's rows together, and what all of them see
-    const bool some = real && me.lo < me.hi;
-    const int w_lo = wave_min(some ? me.lo : INT32_MAX), w_hi = wave_max_i(some ? me.hi : INT32_MIN);
-    const int in_lo = wave_max_i(real ? me.lo : INT32_MIN), in_hi = wave_min(real ? me.hi : INT32_MAX);
-    if (lane == 0) { sLo[w] = w_lo; sHi[w] = w_hi; sInLo[w] = in_lo; sInHi[w] = in_hi; }
-    if (tid == 0) sBad[0] = sBad[1] = -1;
-
-    bf16x8 q[8];
-    const uint16_t* qr = p.q + (int64_t)b * p.q_b + (int64_t)me.token * p.q_t + (int64_t)me.head * kD;
+    const int row0 = tile * kRows + w * 32 * QB + n;
+    bool real[QB];
+    Query me[QB];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s + 8 * h);
+    for (int x = 0; x < QB; ++x) { real[x] = row0 + 32 * x < n_rows; me[x] = query_of(p, tok, b, g, min(row0 + 32 * x, n_rows - 1)); }
+
+    __shared__ __attribute__((aligned(16))) unsigned char sK[kRing * kKBlock], sV[kRing * kVBlock];
+    __shared__ int sLo[4], sHi[4], sInLo[4], sInHi[4], sBad;
+
+    int w_lo = INT32_MAX, w_hi = INT32_MIN, in_lo = INT32_MIN, in_hi = INT32_MAX;
+#pragma unroll
+    for (int x = 0; x < QB; ++x) {
+        if (!real[x]) continue;
+        if (me[x].lo < me[x].hi) { w_lo = min(w_lo, me[x].lo); w_hi = max(w_hi, me[x].hi); }
+        in_lo = max(in_lo, me[x].lo); in_hi = min(in_hi, me[x].hi);
+    }
+    w_lo = wave_min(w_lo); w_hi = wave_max_i(w_hi); in_lo = wave_max_i(in_lo); in_hi = wave_min(in_hi);
+    if (lane == 0) { sLo[w] = w_lo; sHi[w] = w_hi; sInLo[w] = in_lo; sInHi[w] = in_hi; }
+    if (tid == 0) sBad = 0;
+
+    bf16x8 q[QB][8];
+#pragma unroll
+    for (int x = 0; x < QB; ++x) {
+        const uint16_t* qr = p.q + (int64_t)b * p.q_b + (int64_t)me[x].token * p.q_t + (int64_t)me[x].head * kD;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) q[x][s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s + 8 * h);
+    }
     ScoreForm form = score_form<CAP>(p, kLog2e);
     if (!SLOPE && form.a < 0.f) {             // raw products are compared below: their order has to be the scores'
         form.a = -form.a;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[s]) ^ 0x80008000u);
+        for (int x = 0; x < QB; ++x)
+#pragma unroll
+            for (int s = 0; s < 8; ++s) q[x][s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[x][s]) ^ 0x80008000u);
     }
-    const float slope2 = SLOPE && p.slopes != nullptr ? p.slopes[me.head] * kLog2e : 0.f;
+    float slope2[QB];
+    if constexpr (SLOPE) {
+#pragma unroll
+        for (int x = 0; x < QB; ++x) slope2[x] = p.slopes != nullptr ? p.slopes[me[x].head] * kLog2e : 0.f;
+    }
     __syncthreads();
     const int lo = __builtin_amdgcn_readfirstlane(min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])));
     const int hi = __builtin_amdgcn_readfirstlane(max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3])));
-    const int all_lo = max(max(sInLo[0], sInLo[1]), max(sInLo[2], sInLo[3])), all_hi = min(min(sInHi[0], sInHi[1]), min(sInHi[2], sInHi[3]));
+    const int all_lo = __builtin_amdgcn_readfirstlane(max(max(sInLo[0], sInLo[1]), max(sInLo[2], sInLo[3])));
+    const int all_hi = __builtin_amdgcn_readfirstlane(min(min(sInHi[0], sInHi[1]), min(sInHi[2], sInHi[3])));
     const int tiles = hi > lo ? (int)(((int64_t)hi - lo + kPromptTile - 1) / kPromptTile) : 0;
     const int parts = max(1, min(p.splits, (int)((uint32_t)(tiles + p.split_tiles - 1) / (uint32_t)p.split_tiles)));
     if (split >= parts) return;
     if (split == 0 && tid == 0 && p.splits > 1) p.parts[bg * p.row_tiles + tile] = parts;
     // (scalars, and known as such: the buffers of the tiles hang on them)
-    const int t0 = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * split / parts));
-    const int t1 = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * (split + 1) / parts));
-
-    float m = -INFINITY, l = 0.f;
-    f32x16 o[4];
+    const int each = tiles / parts, rest_tiles = tiles - each * parts;
+    const int t0 = __builtin_amdgcn_readfirstlane(each * split + rest_tiles * split / parts);
+    const int t1 = __builtin_amdgcn_readfirstlane(each * (split + 1) + rest_tiles * (split + 1) / parts);
+    const int b0 = 2 * t0, b1 = 2 * t1, end = min(hi, lo + b1 * kBlockRows);       // blocks
+    float m[QB], l[QB], from[QB], limit[QB], alpha[QB];
+    f32x16 o[QB][4];
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+    for (int x = 0; x < QB; ++x) {
+        m[x] = limit[x] = -INFINITY; l[x] = from[x] = 0.f; alpha[x] = 1.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[x][d][r] = 0.f;
+    }
 
-    // staging: thread -> chunk of 16 bytes c of rows r16 + 16 i.  K: chunk c of row r lies at c ^ (r & 15); V: at c ^ 2 (r & 7), so that the
-    // transposing reads of four rows of 16 dims fall on different banks.
-    const int c = tid & 15, r16 = tid >> 4;
+    // staging: thread -> chunk of 16 bytes tid % 16 of rows tid / 16 and tid / 16 + 16
     const uint16_t* k_rows = p.k + (int64_t)b * p.s_b + (int64_t)g * p.s_h;
     const uint16_t* v_rows = p.v + (int64_t)b * p.s_b + (int64_t)g * p.s_h;
-    u32x4 kr[4], vr[4];
-    // (a tile is a buffer of its own: rows past `hi` read as zeros, which no row sees)
-    auto request = [&](int t) {
-        const int at = lo + t * kPromptTile, bytes = min(hi - at, kPromptTile) * (kD * 2);
-        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(k_rows) + (int64_t)at * kD, 0, bytes, 0x00020000);
-        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(v_rows) + (int64_t)at * kD, 0, bytes, 0x00020000);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, tid * 16, i * 4096, 0);
-            vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, tid * 16, i * 4096, 0);
+    struct Staged { u32x4 r[2]; };
+    // (a block is a buffer of its own: rows that no stage sees read as zeros, without traffic)
+    struct Block { int64_t at; int32_t bytes; };
+    auto block = [&](int i) {
+        const int at = lo + i * kBlockRows;
+        int have = min(end - at, kBlockRows);
+        asm("" : "+s"(have));
+        return Block{(int64_t)at * kD, max(have, 0) * (kD * 2)};
+    };
+    auto buffer = [&](const uint16_t* rows, const Block& x) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(rows) + x.at, 0, x.bytes, 0x00020000); };
+    auto request = [&](const uint16_t* rows, int i) {
+        const __amdgpu_buffer_rsrc_t rsrc = buffer(rows, block(i));
+        return Staged{__builtin_amdgcn_raw_buffer_load_b128(rsrc, tid * 16, 0, 0), __builtin_amdgcn_raw_buffer_load_b128(rsrc, tid * 16, 4096, 0)};
+    };
+    const int k_slot = (tid >> 4) * kKRow + (tid & 15) * 16, v_slot = (tid >> 4) * kVRow + (tid & 15) * 16;
+    auto write_k = [&](const Staged& s, int at, int c) { *reinterpret_cast<u32x4*>(sK + at + k_slot + c * 16 * kKRow) = s.r[c]; };
+    auto write_v = [&](const Staged& s, int at, int c) { *reinterpret_cast<u32x4*>(sV + at + v_slot + c * 16 * kVRow) = s.r[c]; };
+    auto outside = [&](int i) { const int j0 = lo + i * kBlockRows; return j0 < all_lo || j0 + kBlockRows > all_hi; };
+    auto clean = [&](Staged& v, int i) {      // V's block i, where a row sees a part of it only
+        if (!outside(i)) return;
+        if (has_non_finite(v.r[0]) || has_non_finite(v.r[1])) {
+            sBad = 1;
+            drop_non_finite(v.r[0]);
+            drop_non_finite(v.r[1]);
         }
     };
-    const int k_to = r16 * 256 + ((c ^ r16) << 4), v_to = r16 * 256 + ((c ^ (2 * (r16 & 7))) << 4);
-    const int k_from = n * 256 + ((h ^ (n & 15)) << 4);              // ^ 32 s for operand s; + 8192 for the second block of 32 rows
-    const int i16 = lane & 15, q4 = (lane >> 4) & 1;
-    const int v_from = (4 * h + (i16 >> 2)) * 256 + (((2 * q4 + ((i16 & 3) >> 1)) ^ (2 * (4 * h + (i16 >> 2)))) << 4) + (i16 & 1) * 8;
 
-    auto write = [&](int t) {                 // the requested tile, number t, to its half of the LDS
-        const int j0 = lo + t * kPromptTile, half = (t & 1) * kHalf;
-        if (j0 < all_lo || j0 + kPromptTile > all_hi) {
-            if (has_non_finite(vr[0]) || has_non_finite(vr[1]) || has_non_finite(vr[2]) || has_non_finite(vr[3])) {
-                sBad[t & 1] = t;
+    const int k_from = n * kKRow + h * 16;
+    const int i16 = lane & 15, q4 = (lane >> 4) & 1;
+    const int v_from = (4 * h + (i16 >> 2)) * kVRow + (2 * q4 + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
+    auto key = [&](int at, int s) { return *reinterpret_cast<const bf16x8*>(sK + at + k_from + s * 32); };
+    auto value = [&](int at, int y, int d) {
+        const unsigned char* from = sV + at + v_from + y * 16 * kVRow + d * 64;
+        const v4s v0 = lds_read_tr16(reinterpret_cast<const uint16_t*>(from)), v1 = lds_read_tr16(reinterpret_cast<const uint16_t*>(from + 8 * kVRow));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+
+    // What a stage hands on to the next one, that of block i: its raw products (with CAP or SLOPE what has been made of them), this lane's largest of them, and the first
+    // operands of block i + 1's keys.
+    struct Ahead { f32x16 s[QB]; float top[QB]; bf16x8 k[4]; };
+    struct Weights { u32x4 p[QB][2]; };
+    auto score = [&](Ahead& a, int x, int r, float far0) {
+        if constexpr (CAP) a.s[x][r] = bend<CAP>(a.s[x][r], form);
+        if constexpr (SLOPE) a.s[x][r] = fmaf(-slope2[x], fabsf(far0 - (float)(8 * (r >> 2) + (r & 3))), fmaf(a.s[x][r], form.a, form.b));
+    };
+    auto largest = [&](Ahead& a, int x, int r) {      // of elements up to r + 1, r from 0 in steps of 2
+        a.top[x] = fmaxf(fmaxf(a.s[x][r], a.s[x][r + 1]), r == 0 ? -INFINITY : a.top[x]);
+    };
+    auto mask = [&](Ahead& a, int i) {
+        const int j0 = lo + 32 * i;
+        if (j0 >= in_lo && j0 + 32 <= in_hi) return;
+        asm volatile("" ::: "memory");        // (a branch: most blocks have nothing to mask)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) drop_non_finite(vr[i]);
-            }
-        }
+        for (int x = 0; x < QB; ++x) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<u32x4*>(sK + half + k_to + i * 4096) = kr[i];
-            *reinterpret_cast<u32x4*>(sV + half + v_to + i * 4096) = vr[i];
+            for (int r = 0; r < 16; ++r) { const int j = j0 + 8 * (r >> 2) + 4 * h + (r & 3); a.s[x][r] = j >= me[x].lo && j < me[x].hi ? a.s[x][r] : -INFINITY; }
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) largest(a, x, r);
         }
     };
-    auto work = [&](int t) {
-        const int j0 = lo + t * kPromptTile, half = (t & 1) * kHalf;
-        if (j0 >= w_hi || j0 + kPromptTile <= w_lo) return;
-        const bool masked = j0 < in_lo || j0 + kPromptTile > in_hi;
-        // ---- S^T: rows j0 + 32 x + 8 (r / 4) + 4 h + r % 4 of column n ----
-        f32x16 s[2];
+    // The maximum that weights are taken against follows the true one only when that has grown by more than 8: weights stay below 2^8, the output is rescaled a few
+    // times in all (at the stage's end, when the weights made before have gone into it), and blocks that change nothing cost one comparison.
+    auto follow = [&](Ahead& a) {
+        const bool grew = __any(a.top[0] > limit[0] || (QB > 1 && a.top[QB - 1] > limit[QB - 1]));
+        if (grew) {
+            asm volatile("" ::: "memory");
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
-        // (kAhead operands are read, and waited for, ahead of an unbroken run of products)
-        auto key = [&](int i) { return *reinterpret_cast<const bf16x8*>(sK + half + (k_from ^ (i >> 1 << 5)) + (i & 1) * 8192); };
-        constexpr int kAhead = 6;
-        bf16x8 a[16];
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) a[i] = key(i);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], q[i >> 1], s[i & 1], 0, 0, 0);
-            if (i + kAhead < 16) a[i + kAhead] = key(i + kAhead);
-        }
-#pragma unroll
-        for (int i = 0; i < 16 - kAhead; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
-        __builtin_amdgcn_sched_barrier(0);
-        auto row_of = [&](int x, int r) { return j0 + 32 * x + 8 * (r >> 2) + 4 * h + (r & 3); };
-        if constexpr (CAP || SLOPE) {
-            const float far0 = (float)(me.pos - j0 - 4 * h);       // (distances beyond 2^24 to 2^-24 of themselves)
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[x][r] = bend<CAP>(s[x][r], form);
-                    if constexpr (SLOPE) s[x][r] = fmaf(-slope2, fabsf(far0 - (float)(32 * x + 8 * (r >> 2) + (r & 3))), fmaf(s[x][r], form.a, form.b));
-                }
-        }
-        if (masked) {
-            asm volatile("" ::: "memory");    // (a branch: most tiles have nothing to mask)
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) { const int j = row_of(x, r); s[x][r] = j >= me.lo && j < me.hi ? s[x][r] : -INFINITY; }
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(s[x][r], s[x][r + 1]), mx);
-        if constexpr (!SLOPE) mx = fmaf(mx, form.a, form.b);
-        mx = max_xor32(mx);
-        // The maximum that weights are taken against follows the true one only when that has grown by more than 8: weights stay below 2^8, and the output
-        // is rescaled a few times in all.
-        if (__any(mx > m + 8.f)) {
-            const float to = fmaxf(m, mx), a = to == -INFINITY ? 1.f : fast_exp2(m - to);
-            m = to;
-            l *= a;
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[d][r] *= a;
-        }
-        __builtin_amdgcn_s_setprio(1);        // (two wavefronts to a SIMD: the one here goes first, the other's products fill in; 558 -> 542 us)
-        const float ref = m == -INFINITY ? 0.f : m, from = form.b - ref;
-        // ---- weights, and O^T += V^T P^T, 16 rows at a time: slot e of half h is row 8 (e / 4) + 4 h + e % 4 of them ----
-        auto value = [&](int y, int d) {
-            const unsigned char* at = sV + half + (v_from ^ (d << 6)) + y * 4096;
-            const v4s v0 = lds_read_tr16(reinterpret_cast<const uint16_t*>(at)), v1 = lds_read_tr16(reinterpret_cast<const uint16_t*>(at + 2048));
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        float part[4];
-        auto weights = [&](int y) {
-            u32x4 u;
-            part[y] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float s0 = s[y >> 1][8 * (y & 1) + 2 * e], s1 = s[y >> 1][8 * (y & 1) + 2 * e + 1];
-                const float a = fast_exp2(SLOPE ? s0 - ref : fmaf(s0, form.a, from)), bb = fast_exp2(SLOPE ? s1 - ref : fmaf(s1, form.a, from));
-                part[y] += a + bb;
-                u[e] = pack_bf16(a, bb);              // (8 bits a weight: its rounding is as large as the output's own and not common to the rows)
+            for (int x = 0; x < QB; ++x) {
+                const float mx = max_xor32(SLOPE ? a.top[x] : fmaf(a.top[x], form.a, form.b)), to = mx > m[x] + 8.f ? mx : m[x];
+                alpha[x] = to == -INFINITY ? 1.f : fast_exp2(m[x] - to);
+                m[x] = to;
+                from[x] = (SLOPE ? 0.f : form.b) - (to == -INFINITY ? 0.f : to);
+                limit[x] = SLOPE ? to + 8.f : (to + 8.f - form.b) / form.a;
+                l[x] *= alpha[x];
             }
-            return __builtin_bit_cast(bf16x8, u);
+        }
+        return grew;
+    };
+    auto prime = [&](Ahead& a, int i, int k_at, int k_next) {
+#pragma unroll
+        for (int x = 0; x < QB; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) a.s[x][r] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bf16x8 k = key(k_at, e);
+#pragma unroll
+            for (int x = 0; x < QB; ++x) a.s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[x][e], a.s[x], 0, 0, 0);
+        }
+#pragma unroll
+        for (int x = 0; x < QB; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) { score(a, x, r, (float)(me[x].pos - (lo + 32 * i) - 4 * h)); if (r & 1) largest(a, x, r - 1); }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a.k[e] = key(k_next, e);
+    };
+    auto drain = [&](const Weights& pw, int v_at) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const bf16x8 v = value(v_at, y, d);
+#pragma unroll
+                for (int x = 0; x < QB; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, pw.p[x][y]), o[x][d], 0, 0, 0);
+            }
+    };
+    // Block i's stage, in slots of one matrix instruction and what fits beside it: products of block i + 1 (keys at k_at) in the first half, those of block i - 1's
+    // weights (values at v_at) in the other, block i's weights all along or, where scores take work of their own, in the first half, and that and the
+    // next maximum in the second.  Keys of block i + 2 are at k_next.  Beside it keys of block i + 3 are written to k_to and values of i + 1 to v_to, those of i + 4 and
+    // i + 2 requested.
+    Staged kr, vr;
+    auto wait_lds = [](auto n) { __builtin_amdgcn_s_waitcnt(0xc07f | decltype(n)::value << 8); };
+    auto stage = [&](Ahead& now, Ahead& ahead, const Weights& behind, Weights& made, int i, Block& v_rows_at, int k_at, int k_next, int k_to, int v_at, int v_to, bool fenced, bool fence) {
+        constexpr int kPer = CAP || SLOPE ? 2 : 1, kHalf = kSlots / 2, kTail = kHalf + 2;
+        mask(now, i);
+        const bool grew = follow(now);
+        clean(vr, i + kAheadV);
+        const Block k_rows_at = block(i + kAheadK + 1);
+        const __amdgpu_buffer_rsrc_t k_in = buffer(k_rows, k_rows_at), v_in = buffer(v_rows, v_rows_at);
+        v_rows_at = k_rows_at;                // (of V it is requested two stages later)
+        bf16x8 kk[8], vv[8];
+        float part[QB], wt[16 * QB], far0[QB];
+        if constexpr (SLOPE) {
+#pragma unroll
+            for (int x = 0; x < QB; ++x) far0[x] = (float)(me[x].pos - (lo + 32 * i + 32) - 4 * h);      // (distances beyond 2^24 to 2^-24 of themselves)
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) kk[e] = now.k[e];
+#pragma unroll
+        for (int x = 0; x < QB; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) ahead.s[x][r] = 0.f;
+        auto exponent = [&](int e) { const float v = now.s[e >> 4][e & 15]; wt[e] = SLOPE ? v + from[e >> 4] : fmaf(v, form.a, from[e >> 4]); };
+        auto add = [&](int e) { const float t = wt[e] + wt[e + 1]; part[e >> 4] = e % 16 == 0 ? t : part[e >> 4] + t; };
+        auto pack = [&](int e) {              // (8 bits a weight: its rounding is as large as the output's own and not common to the rows)
+            made.p[e >> 4][(e & 15) >> 3][(e & 7) >> 1] = pack_bf16(wt[e], wt[e + 1]);
         };
-        bf16x8 v[2][4], pw[2];
 #pragma unroll
-        for (int d = 0; d < 4; ++d) v[0][d] = value(0, d);
-        pw[0] = weights(0);
+        for (int e = 0; e < kPer; ++e) exponent(e);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
+        for (int k = 0; k < kSlots; ++k) {
             __builtin_amdgcn_sched_barrier(0);
-            if (y < 3) {
-#pragma unroll
-                for (int d = 0; d < 4; ++d) v[(y + 1) & 1][d] = value(y + 1, d);
-                pw[(y + 1) & 1] = weights(y + 1);
+            const int x = k % QB;
+            if constexpr (QB > 1) {           // (one wavefront to a SIMD: one wait for several operands)
+                if (k == 0 && !fenced) wait_lds(std::integral_constant<int, 0>{});
+                if (k == 4 * QB) wait_lds(std::integral_constant<int, 4>{});
+                if (k == kHalf) wait_lds(std::integral_constant<int, 4>{});
+                if (k == kHalf + 4 * QB) wait_lds(std::integral_constant<int, 0>{});
             }
+            if (k < kHalf) {
+                ahead.s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[k / QB], q[x][k / QB], ahead.s[x], 0, 0, 0);
+            } else {
+                const int j = (k - kHalf) / QB;       // (16 rows, then the other 16)
+                o[x][j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv[j], __builtin_bit_cast(bf16x8, behind.p[x][j >> 2]), o[x][j & 3], 0, 0, 0);
+            }
+            if (k < 4) kk[4 + k] = key(k_at, 4 + k);
+            constexpr int kFirstV = QB == 1 ? 3 : 5;
+            if (k >= kFirstV && k < kFirstV + 8 * QB && (k - kFirstV) % QB == 0) { const int j = (k - kFirstV) / QB; vv[j] = value(v_at, j >> 2, j & 3); }
+            if (k >= kSlots - 4 * QB && (k % QB) == 0) { const int j = (k - (kSlots - 4 * QB)) / QB; ahead.k[j] = key(k_next, j); }
+            if (k >= kHalf && k < kHalf + 4) { if (k - kHalf < 2) write_k(kr, k_to, k - kHalf); else write_v(vr, v_to, k - kHalf - 2); }
+            if (k >= kHalf + 4 && k < kHalf + 6) kr.r[k - kHalf - 4] = __builtin_amdgcn_raw_buffer_load_b128(k_in, tid * 16, (k - kHalf - 4) * 4096, 0);
+            if (k >= kHalf + 6 && k < kHalf + 8) vr.r[k - kHalf - 6] = __builtin_amdgcn_raw_buffer_load_b128(v_in, tid * 16, (k - kHalf - 6) * 4096, 0);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[y & 1][d], pw[y & 1], o[d], 0, 0, 0);
-            if (y < 3) {                      // a matrix instruction, then what fits beside it: transposing reads and the next 16 rows' weights
-                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+            for (int e = kPer * k; e < kPer * (k + 1) && e < 16 * QB; ++e) {
+                wt[e] = fast_exp2(wt[e]);
+                if (e + kPer < 16 * QB) exponent(e + kPer);
+                if (e >= 2 && e % 2 == 0 && kPer == 1) add(e - 2);
+                if (e >= 3 && e % 2 == 1) { if (kPer == 2) add(e - 3); pack(e - 3); }
+            }
+            if (k >= kTail) {
+                if constexpr (CAP || SLOPE) {
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x402, 9, 0);
+                    for (int e = (k - kTail) * 16 * QB / (kSlots - kTail); e < (k - kTail + 1) * 16 * QB / (kSlots - kTail); ++e) {
+                        score(ahead, e >> 4, e & 15, far0[e >> 4]);
+                        if (e & 1) largest(ahead, e >> 4, (e & 15) - 1);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = (k - kTail) * 8 * QB / (kSlots - kTail); e < (k - kTail + 1) * 8 * QB / (kSlots - kTail); ++e) largest(ahead, e % QB, 2 * (e / QB));
                 }
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_setprio(0);
-        l += (part[0] + part[1]) + (part[2] + part[3]);
-        if (sBad[t & 1] == t) {
-            const uint16_t* from = p.v + (int64_t)b * p.s_b + (int64_t)g * p.s_h + 4 * h;
-            for (int j = max(j0, me.lo); j < j0 + kPromptTile && j < me.hi; ++j) {
+        add(16 * QB - 2); pack(16 * QB - 2);
+#pragma unroll
+        for (int x = 0; x < QB; ++x) {
+            l[x] += part[x];
+            asm volatile("" : "+v"(made.p[x][0]), "+v"(made.p[x][1]), "+v"(l[x]), "+v"(ahead.top[x]));      // (made here, and not where they are needed)
+        }
+        if (grew) {
+#pragma unroll
+            for (int x = 0; x < QB; ++x)
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const uint2 x = *reinterpret_cast<const uint2*>(from + (int64_t)j * kD + 32 * d + 8 * r);
-                        o[d][4 * r] += only_non_finite(bf16_lo(x.x)); o[d][4 * r + 1] += only_non_finite(bf16_hi(x.x));
-                        o[d][4 * r + 2] += only_non_finite(bf16_lo(x.y)); o[d][4 * r + 3] += only_non_finite(bf16_hi(x.y));
+                    for (int r = 0; r < 16; ++r) o[x][d][r] *= alpha[x];
+        }
+        if (fence) lds_barrier();
+    };
+
+    // (the queries are here before the loop begins: see queries_here)
+#pragma unroll
+    for (int x = 0; x < QB; ++x)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            u32x4 u = __builtin_bit_cast(u32x4, q[x][e]);
+            if constexpr (QB == 1) asm volatile("" : "+v"(u));
+            else asm volatile("" : "+a"(u));
+            q[x][e] = __builtin_bit_cast(bf16x8, u);
+        }
+    if (b0 < b1) {
+        // tiles of two blocks in LDS
+        constexpr int kKTile = 2 * kKBlock, kVTile = 2 * kVBlock, kTiles = kRing / 2;
+        int kt[kTiles], vt[kTiles];           // of the block's own tile, the next one, ..
+#pragma unroll
+        for (int c = 0; c < kTiles; ++c) { kt[c] = c * kKTile; vt[c] = c * kVTile; }
+        Staged ks[kAheadK], vs[kAheadV];
+#pragma unroll
+        for (int c = 0; c < kAheadK; ++c) ks[c] = request(k_rows, b0 + c);
+#pragma unroll
+        for (int c = 0; c < kAheadV; ++c) vs[c] = request(v_rows, b0 + c);
+        for (int x = tid; x < kVBlock / 16; x += 256) *reinterpret_cast<u32x4*>(sV + (kRing - 1) * kVBlock + 16 * x) = u32x4{0u, 0u, 0u, 0u};      // (nothing lies behind the first block)
+#pragma unroll
+        for (int c = 0; c < kAheadK; ++c) { write_k(ks[c], c * kKBlock, 0); write_k(ks[c], c * kKBlock, 1); }
+#pragma unroll
+        for (int c = 0; c < kAheadV; ++c) { clean(vs[c], b0 + c); write_v(vs[c], c * kVBlock, 0); write_v(vs[c], c * kVBlock, 1); }
+        kr = request(k_rows, b0 + kAheadK);
+        vr = request(v_rows, b0 + kAheadV);
+        Block v_even = block(b0 + kAheadV + 1), v_odd = block(b0 + kAheadV + 2);
+        __syncthreads();
+        Ahead even, odd;
+        Weights pe, po{};
+        prime(even, b0, 0, kKBlock);
+        for (int i = b0; i < b1; i += 2) {
+            constexpr int last = kTiles - 1;
+            if constexpr (QB == 1) {
+                stage(even, odd, po, pe, i, v_even, kt[0] + kKBlock, kt[1], kt[1] + kKBlock, vt[last] + kVBlock, vt[0] + kVBlock, true, true);
+                stage(odd, even, pe, po, i + 1, v_odd, kt[1], kt[1] + kKBlock, kt[0], vt[0], vt[1], true, true);
+            } else {
+                stage(even, odd, po, pe, i, v_even, kt[0] + kKBlock, kt[1], kt[2 % kTiles], vt[last] + kVBlock, vt[1], true, false);
+                stage(odd, even, pe, po, i + 1, v_odd, kt[1], kt[1] + kKBlock, kt[2 % kTiles] + kKBlock, vt[0], vt[1] + kVBlock, false, true);
+            }
+            const int k0 = kt[0], v0 = vt[0];
+#pragma unroll
+            for (int c = 0; c < last; ++c) { kt[c] = kt[c + 1]; vt[c] = vt[c + 1]; }
+            kt[last] = k0; vt[last] = v0;
+        }
+        drain(po, vt[kTiles - 1] + kVBlock);
+        if (sBad != 0) {
+#pragma unroll 1
+            for (int i = b0; i < b1; ++i) {
+                if (!outside(i)) continue;
+                const int j0 = lo + i * kBlockRows;
+#pragma unroll
+                for (int x = 0; x < QB; ++x)
+                    for (int j = max(j0, me[x].lo); j < j0 + kBlockRows && j < me[x].hi; ++j) {
+#pragma unroll
+                        for (int d = 0; d < 4; ++d)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const uint2 u = *reinterpret_cast<const uint2*>(v_rows + 4 * h + (int64_t)j * kD + 32 * d + 8 * e);
+                                o[x][d][4 * e] += only_non_finite(bf16_lo(u.x)); o[x][d][4 * e + 1] += only_non_finite(bf16_hi(u.x));
+                                o[x][d][4 * e + 2] += only_non_finite(bf16_lo(u.y)); o[x][d][4 * e + 3] += only_non_finite(bf16_hi(u.y));
+                            }
                     }
             }
         }
-    };
-    // (the queries are here before the loop begins: see queries_here)
+    }
+    // ---- lane (n, h) has dims 32 d + 8 (r / 4) + 4 h + r % 4 of rows n + 32 x ----
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-        u32x4 x = __builtin_bit_cast(u32x4, q[s]);
-        asm volatile("" : "+v"(x));
-        q[s] = __builtin_bit_cast(bf16x8, x);
-    }
-    if (t0 < t1) {
-        request(t0);
-        write(t0);
-        if (t0 + 1 < t1) request(t0 + 1);
-        __syncthreads();
-    }
-    for (int t = t0; t < t1; ++t) {
-        work(t);
-        if (t + 1 < t1) write(t + 1);
-        if (t + 2 < t1) request(t + 2);
-        lds_barrier();
-    }
-    // ---- lane (n, h) has dims 32 d + 8 (r / 4) + 4 h + r % 4 of row n ----
-    l = sum_xor32(l);
-    if (!real) return;
-    if (parts > 1) {
-        const int64_t at = ((int64_t)bg * p.n_new * p.G + row) * p.splits + split;
-        if (h == 0) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(m, l);
-        float* to = p.part_o + at * kD + 4 * h;
+    for (int x = 0; x < QB; ++x) {
+        const float sum = sum_xor32(l[x]);
+        if (!real[x]) continue;
+        if (parts > 1) {
+            const int64_t at = ((int64_t)bg * p.n_new * p.G + row0 + 32 * x) * p.splits + split;
+            if (h == 0) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(m[x], sum);
+            float* to = p.part_o + at * kD + 4 * h;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    *reinterpret_cast<float4*>(to + 32 * d + 8 * r) = make_float4(o[x][d][4 * r], o[x][d][4 * r + 1], o[x][d][4 * r + 2], o[x][d][4 * r + 3]);
+            continue;
+        }
+        const int64_t at = ((int64_t)b * p.n_new + me[x].token) * p.Hq + me[x].head;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (h == 0 && p.lse != nullptr) p.lse[at] = sum == 0.f ? -INFINITY : (m[x] + __builtin_amdgcn_logf(sum)) * (1.f / kLog2e);
+        uint16_t* to = p.out + at * kD + 4 * h;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                *reinterpret_cast<float4*>(to + 32 * d + 8 * r) = make_float4(o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]);
-        return;
+                *reinterpret_cast<uint2*>(to + 32 * d + 8 * r) =
+                    make_uint2(pack_bf16(o[x][d][4 * r] * inv, o[x][d][4 * r + 1] * inv), pack_bf16(o[x][d][4 * r + 2] * inv, o[x][d][4 * r + 3] * inv));
     }
-    const int64_t at = ((int64_t)b * p.n_new + me.token) * p.Hq + me.head;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (h == 0 && p.lse != nullptr) p.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.f / kLog2e);
-    uint16_t* to = p.out + at * kD + 4 * h;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            *reinterpret_cast<uint2*>(to + 32 * d + 8 * r) =
-                make_uint2(pack_bf16(o[d][4 * r] * inv, o[d][4 * r + 1] * inv), pack_bf16(o[d][4 * r + 2] * inv, o[d][4 * r + 3] * inv));
 }
 
 // ---- up to 16 rows in all ----
@@ -545,24 +672,29 @@ void prompt_merge_kernel(const PromptParams p) {
     if (lane == 0 && p.lse != nullptr) p.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.f / kLog2e);
 }
 
-// Which kernel, and over how many workgroups at most the cache rows of one row tile are split: so that the launch has up to kPromptTarget workgroups (two to
-// a compute unit).  Columns: none with fewer than a round of 128 rows.  Row tiles: a part no shorter than split_tiles tiles of 64 rows, which
-// the kernel sees to, as only it knows the ranges: 32, or 16 where there are few row tiles.  us, 32 heads over 8 (parts: most to a row tile):
-//   128 tokens behind 32640: 1 part 740, 2: 378, 4: 197, 8: 108, 16: 84, 32: 101;  300 behind 7892: 1: 190, 2: 107, 4: 69, 6: 77;
-//   512 behind 32256: 1: 742, 4: 285;  8 behind 32760, parts of 32 tiles: 47, 16: 32, 8: 33, 4: 43;  whole prompts of 600: 1: 20.0, 2: 26.4,
-//   of 2048: 1: 59, 2: 77 (there the partial results cost more than the even spread gains).
+// Which kernel, and over how many workgroups at most the cache rows of one row tile are split.
+// 64 rows to a wavefront where two rounds of such workgroups or more come together, nothing capped and no bias: those are long enough for the card to lower its clock
+// with the power it draws, and half the reads from LDS then count for more than a second wavefront on the SIMD (us, 64 rows / 32: 8192 tokens of 32 heads over 8
+// 519 / 540, and 445 / 402 with zeros for data, where the clock stays; 4096 tokens 144 / 155; 4 prompts of 1024, one round: 54.9 / 53.9; three capped chunks 132 / 70).
+// Columns: no part with fewer than a round of 128 rows, two workgroups to a compute unit.  Row tiles: one workgroup to a compute unit, two where that leaves parts of more than
+// 32 tiles of cache rows; no part shorter than split_tiles tiles, which the kernel sees to, as only it knows the ranges.  us, 32 heads over 8, by workgroups in all (256 / 512):
+// 8 tokens behind 32752 33.7 / 35.0, 64 behind 16320 34.8 / 38.3, 128 behind 8064 34.4 / 37.4, 128 behind 32640 99 / 91, 300 behind 7892 64 / 61, 512 behind 32256
+// 348 / 287; by the shortest part (4 / 8 / 16 tiles): 8 tokens behind 992 12.9 / 17.0 / 22.0, 8 behind 4088 14.8 / 18.2 / 26.4, whole prompts of 400 19.1 / 13.9 / 14.0.
 constexpr int kPromptTarget = 2 * kComputeUnits;
-struct PromptPlan { bool cols; int row_tiles, splits, split_tiles; };
-static PromptPlan prompt_plan(const rk_geom* g, int64_t n_new, int64_t max_len) {
+struct PromptPlan { bool cols, wide; int row_tiles, splits, split_tiles; };
+static PromptPlan prompt_plan(const rk_geom* g, int64_t n_new, int64_t max_len, bool plain) {
     const int64_t pairs = (int64_t)g->batch * g->n_kv_heads, rows = n_new * (g->n_q_heads / g->n_kv_heads);
-    PromptPlan f{rows <= 16, 1, 1, 1};
-    int64_t most = (max_len + kMinChunk - 1) / kMinChunk;
+    PromptPlan f{rows <= 16, plain && pairs * ((rows + 2 * kPromptRows - 1) / (2 * kPromptRows)) >= 2 * kComputeUnits, 1, 1, 1};
+    int64_t s = kPromptTarget / pairs, most = (max_len + kMinChunk - 1) / kMinChunk;
     if (!f.cols) {
-        f.row_tiles = (int)((rows + kPromptRows - 1) / kPromptRows);
-        f.split_tiles = pairs * f.row_tiles < 64 ? 16 : 32;
-        most = (max_len + f.split_tiles * kPromptTile - 1) / (f.split_tiles * kPromptTile);
+        const int tile = f.wide ? 2 * kPromptRows : kPromptRows;
+        f.row_tiles = (int)((rows + tile - 1) / tile);
+        const int64_t wgs = pairs * f.row_tiles, tiles = (max_len + kPromptTile - 1) / kPromptTile;
+        s = kComputeUnits / wgs;
+        f.split_tiles = wgs <= 32 ? 4 : 8;
+        if (tiles > 32 * (s < 1 ? 1 : s)) { s = f.wide ? 1 : kPromptTarget / wgs; f.split_tiles = 16; }
+        most = (tiles + f.split_tiles - 1) / f.split_tiles;
     }
-    int64_t s = kPromptTarget / (pairs * f.row_tiles);
     if (s > most) s = most;
     if (s > kMaxSplits) s = kMaxSplits;
     f.splits = (int)(s < 1 ? 1 : s);
@@ -597,8 +729,10 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
     if ((rc = check_kv(cache)) != RK_OK) return rc;
     const int G = geom->n_q_heads / geom->n_kv_heads;
     const int64_t pairs = (int64_t)geom->batch * geom->n_kv_heads;
-    if ((int64_t)n_new * G > INT32_MAX - kPromptRows) return RK_ERR_UNSUPPORTED;
-    const PromptPlan plan = prompt_plan(geom, n_new, max_len);
+    if ((int64_t)n_new * G > INT32_MAX - 128) return RK_ERR_UNSUPPORTED;
+    // (a scale of 0 goes with the slopes: masked products would be 0 times infinity in a weight's exponent)
+    const bool cap = scores && scores->cap > 0.f, slope = (scores && scores->slopes) || (geom->scale == 0.f && !cap);
+    const PromptPlan plan = prompt_plan(geom, n_new, max_len, !cap && !slope);
     if (pairs * plan.row_tiles * plan.splits > INT32_MAX / 2) return RK_ERR_UNSUPPORTED;
     PromptParams p{};
     p.q = (const uint16_t*)q; p.q_b = q_stride_b; p.q_t = q_stride_t;
@@ -620,16 +754,15 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
         p.cols = plan.cols ? 1 : 0;
         p.ragged = plan.cols ? ragged_batch_of(geom) : 0;
     }
-    // (a scale of 0 goes with the slopes: masked products would be 0 times infinity in a weight's exponent)
-    const bool cap = p.cap > 0.f, slope = p.slopes != nullptr || (p.scale == 0.f && !cap);
     hipStream_t st = (hipStream_t)stream;
     if (plan.cols) {
         auto kernel = cap ? (slope ? prompt_cols_kernel<true, true> : prompt_cols_kernel<true, false>)
                           : (slope ? prompt_cols_kernel<false, true> : prompt_cols_kernel<false, false>);
         hipLaunchKernelGGL(kernel, dim3(plan.splits, geom->n_kv_heads, geom->batch), dim3(kColWaves * 64), 0, st, p);
     } else {
-        auto kernel = cap ? (slope ? prompt_tile_kernel<true, true> : prompt_tile_kernel<true, false>)
-                          : (slope ? prompt_tile_kernel<false, true> : prompt_tile_kernel<false, false>);
+        auto kernel = plan.wide ? prompt_tile_kernel<2, false, false>
+                      : cap     ? (slope ? prompt_tile_kernel<1, true, true> : prompt_tile_kernel<1, true, false>)
+                                : (slope ? prompt_tile_kernel<1, false, true> : prompt_tile_kernel<1, false, false>);
         const int64_t total = pairs * plan.row_tiles * plan.splits;
         hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(256), 0, st, p);
     }
