@@ -29,6 +29,7 @@ struct PromptParams {
     float *part_o, *part_ml;
     int32_t* parts;                           // of row tiles [batch * Hkv][row_tiles]: how many (1: the output is there already); of columns
                                               // [batch * Hkv][2]: the first one's number and how many
+    int32_t first_round;                      // workgroups of a (sequence, KV head) in the launch's order, of which the others' order is turned around
     int32_t cols, ragged;                     // ragged != 0 (= batch): the columns' workgroups are shared out by length
 };
 
@@ -119,7 +120,9 @@ void prompt_tile_kernel(const PromptParams p) {
     constexpr int kRows = kPromptRows * QB, kSlots = 16 * QB, kRing = 4 * QB, kAheadK = 2 + QB, kAheadV = QB;
     // Consecutive workgroups go round the 8 dies, and the (sequence, KV head) pairs run fastest: a die sees few pairs (one, where there are 8; the same
     // head of every sequence), whose rows its L2 keeps, and of each sequence as many row tiles as any other die.  The last tokens', which see most, come first.
-    const int pairs = p.Hkv * p.batch, bg = (int)(blockIdx.x % (uint32_t)pairs), rest = (int)(blockIdx.x / (uint32_t)pairs);
+    const int pairs = p.Hkv * p.batch, bg = (int)(blockIdx.x % (uint32_t)pairs);
+    int rest = (int)(blockIdx.x / (uint32_t)pairs);
+    if (rest >= p.first_round) rest = p.row_tiles * p.splits - 1 - (rest - p.first_round);
     const int tile = p.row_tiles - 1 - rest / p.splits, split = rest % p.splits;
     const int b = bg / p.Hkv, g = bg - b * p.Hkv;
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
@@ -764,6 +767,9 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
                       : cap     ? (slope ? prompt_tile_kernel<1, true, true> : prompt_tile_kernel<1, true, false>)
                                 : (slope ? prompt_tile_kernel<1, false, true> : prompt_tile_kernel<1, false, false>);
         const int64_t total = pairs * plan.row_tiles * plan.splits;
+        // (Where all workgroups are there at once, two to a compute unit, the second ones come in the opposite order: the longest beside the shortest.  8000 tokens of 8
+        // heads 173 -> 165 us, 2048 of 32 over 8 53.0 -> 51.0, three capped chunks 70.3 -> 69.0.)
+        p.first_round = !plan.wide && total <= 2 * kComputeUnits ? (int)((kComputeUnits + pairs - 1) / pairs) : INT32_MAX;
         hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(256), 0, st, p);
     }
     if ((rc = launch_status()) != RK_OK || plan.splits == 1) return rc;
