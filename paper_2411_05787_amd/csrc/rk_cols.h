@@ -116,7 +116,7 @@ __device__ __forceinline__ void value_operands(const TileRows<FORMAT>& t, int h,
 }
 
 // The queries' operands are here once this returns.  Called behind the first tile's requests: left to itself the compiler finds them still on their way
-// where the loop begins, and every round of the loop then waits for all that is in flight (18.4 -> 15.2 us for 32777 rows of 8 bits).
+// where the loop begins, and every round of the loop then waits for all that is in flight (with tiles as buffers 18.4 -> 16.8 us for 32777 rows of 8 bits).
 __device__ __forceinline__ void queries_here(bf16x8 (&q)[4]) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -202,11 +202,11 @@ __device__ __forceinline__ void tile_output(const TileRows<FORMAT>& t, ColState&
     }
 }
 
-// The workgroup's columns < ncols merged over its wavefronts: calls put(column, dim, o0, o1) for the pairs of dims (the unnormalised output against the
-// common maximum) and stat(column, m, l).
-struct ColMergeLds { float m[kColWaves][16], l[kColWaves][16]; float o[kColWaves][16][kD]; };
-template <class Put, class Stat>
-__device__ __forceinline__ void merge_columns(ColMergeLds& lds, ColState& st, int ncols, Put&& put, Stat&& stat) {
+// The workgroup's columns < ncols <= C merged over its W wavefronts: calls put(column, dim, o0, o1, L) for the pairs of dims (the unnormalised output against the
+// common maximum, and its sum) and stat(column, m, l).
+template <int W, int C> struct ColMergeLds { float m[W][16], l[W][16]; float o[W][C][kD]; };
+template <int W, int C, class Put, class Stat>
+__device__ __forceinline__ void merge_columns(ColMergeLds<W, C>& lds, ColState& st, int ncols, Put&& put, Stat&& stat) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
     const float l = sum_xor32(sum_xor16(st.l));
     if (g == 0) { lds.m[w][n] = st.m; lds.l[w][n] = l; }
@@ -219,20 +219,20 @@ __device__ __forceinline__ void merge_columns(ColMergeLds& lds, ColState& st, in
         }
     }
     __syncthreads();
-    for (int x = tid; x < ncols * (kD / 2); x += kColWaves * 64) {
+    for (int x = tid; x < ncols * (kD / 2); x += W * 64) {
         const int c = x / (kD / 2), d = 2 * (x % (kD / 2));
         float M = lds.m[0][c];
 #pragma unroll
-        for (int i = 1; i < kColWaves; ++i) M = fmaxf(M, lds.m[i][c]);
+        for (int i = 1; i < W; ++i) M = fmaxf(M, lds.m[i][c]);
         float L = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll
-        for (int i = 0; i < kColWaves; ++i) {
+        for (int i = 0; i < W; ++i) {
             const float a = lds.m[i][c] == -INFINITY ? 0.f : fast_exp2((lds.m[i][c] - M) * kLog2e);
             const float2 v = *reinterpret_cast<const float2*>(&lds.o[i][c][d]);
             // (a wavefront without rows has nothing; NaN statistics stay NaN)
             L = fmaf(a, lds.l[i][c], L); o0 = fmaf(a, v.x, o0); o1 = fmaf(a, v.y, o1);
         }
-        put(c, d, o0, o1);
+        put(c, d, o0, o1, L);
         if (d == 0) stat(c, M, L);
     }
 }

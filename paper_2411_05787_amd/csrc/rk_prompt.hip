@@ -595,12 +595,12 @@ void prompt_cols_kernel(const PromptParams p) {
         request_values<kBf16>(rows, v, first_of(t + step), hi - first_of(t + step));
     }
 
-    __shared__ __attribute__((aligned(16))) ColMergeLds lds;
+    __shared__ __attribute__((aligned(16))) ColMergeLds<kColWaves, 16> lds;
     __shared__ float sInv[16];
     if (p.splits > 1) {
         const int64_t at = ((int64_t)g * p.splits * p.batch + slot) * p.n_new * p.G;
         merge_columns(lds, st, n_rows,
-                      [&](int x, int d, float o0, float o1) {
+                      [&](int x, int d, float o0, float o1, float) {
                           *reinterpret_cast<float2*>(p.part_o + (at + x) * kD + d) = make_float2(o0, o1);
                       },
                       [&](int x, float m, float l) {
@@ -612,7 +612,7 @@ void prompt_cols_kernel(const PromptParams p) {
     auto out_row = [&](int x) { const int i = x / p.G; return ((int64_t)b * p.n_new + i) * p.Hq + g * p.G + (x - i * p.G); };
     float* o = &lds.o[0][0][0];
     merge_columns(lds, st, n_rows,
-                  [&](int x, int d, float o0, float o1) { o[x * kD + d] = o0; o[x * kD + d + 1] = o1; },
+                  [&](int x, int d, float o0, float o1, float) { o[x * kD + d] = o0; o[x * kD + d + 1] = o1; },
                   [&](int x, float m, float l) {
                       sInv[x] = l == 0.f ? 0.f : 1.f / l;
                       if (p.lse != nullptr) p.lse[out_row(x)] = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l) * (1.f / kLog2e);

@@ -17,26 +17,44 @@ static int q8_split_workgroups(const rk_geom* g, int32_t max_len, bool weights) 
     return split_workgroups(max_len, (int64_t)g->batch * g->n_kv_heads, kMaxChunks, weights ? emit_split_target(g, max_len) : kComputeUnits);
 }
 
+// One workgroup of kAlone wavefronts to a (sequence, KV head), and no launch behind it: where the pairs fill the chip by themselves and no sharing by length is there to lose,
+// or the sequences are so short that a second launch costs more than the rows.  us, without weights, 32 heads over 8, e4m3 (split / alone): 4 sequences of 500 rows 9.1 / 8.4,
+// of 1000 9.3 / 11.6, 16 of 500 12.5 / 9.6, of 1000 14.6 / 13.6, of 1500 17.3 / 17.5, 32 of 500 16.5 / 10.0, of 2000 30.5 / 24.7, of 4000 49.7 / 43.0, one of 500 8.1 / 8.3.
+constexpr int kAlone = 16;
+static bool q8_alone(const rk_geom* g, int32_t max_len) {
+    const int64_t pairs = (int64_t)g->batch * g->n_kv_heads;
+    return (pairs >= 32 && max_len <= (pairs > 64 ? 8 * pairs : 512)) || (pairs >= kComputeUnits && ragged_batch_of(g) == 0);
+}
+
+// log-sum-exp as hi + lo, of a maximum and a sum (no rows: -inf; a NaN among the sums: NaN).
+__device__ __forceinline__ float2 lse_of(float m, double l) {
+    if (l == 0.0) return make_float2(-INFINITY, 0.f);
+    const double x = (double)m + log(l);
+    const float hi = (float)x;
+    return make_float2(hi, (float)(x - (double)hi));
+}
+
 // Tiles of a sequence of len rows (of which the call looks at the first n): those of whole blocks, then those of the tail.
-template <int FORMAT, bool EMIT>
-__global__ __launch_bounds__(kColWaves * 64, 2)
+// ALONE: one workgroup of W wavefronts has all rows, and does what the launch behind would.
+template <int FORMAT, bool EMIT, int W, bool ALONE>
+__global__ __launch_bounds__(W * 64, ALONE ? 1 : 2)
 void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
     const int g = blockIdx.y;
-    int b = blockIdx.z, c = blockIdx.x, nchunks = 0;
-    if (p.ragged_batch != 0) {
+    int b = blockIdx.z, c = blockIdx.x, nchunks = 1;
+    if (!ALONE && p.ragged_batch != 0) {
         const RaggedSlot slot = ragged_slot<false>(p, p.seq_lens, (int)(blockIdx.z * gridDim.x + blockIdx.x));
         if (slot.b < 0) return;
         b = slot.b; c = slot.c; nchunks = slot.nchunks;
     }
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
     const int len = __builtin_amdgcn_readfirstlane(min(max(p.seq_lens[b], 0), p.cap2)), n = min(len, p.max_rows2);
-    if (p.ragged_batch == 0) {
+    if (!ALONE && p.ragged_batch == 0) {
         nchunks = active_workgroups(n, p.nch);
         if (c >= nchunks) return;
     }
     const int G = p.Hq / p.Hkv;
     const int64_t bg = (int64_t)b * p.Hkv + g;
-    if (p.ragged_batch != 0 && c == 0 && threadIdx.x == 0) store_chunks(p.counters, bg, nchunks);
+    if (!ALONE && p.ragged_batch != 0 && c == 0 && threadIdx.x == 0) store_chunks(p.counters, bg, nchunks);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, gr = lane >> 4;
     const int full = len >> c8.shift << c8.shift, main_rows = min(n, full);
     const int main_tiles = (main_rows + kTileRows - 1) / kTileRows, tiles = main_tiles + (n - main_rows + kTileRows - 1) / kTileRows;
@@ -88,7 +106,7 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
         }
         tile_softmax(st, s);
     };
-    const int t0 = c * kColWaves + w, step = nchunks * kColWaves;
+    const int t0 = c * W + w, step = nchunks * W;
     TileRows<FORMAT> rows;
     // the scales of a tile's two blocks of 16 rows, requested with its rows
     struct Scales { float k0, k1, v0, v1; };
@@ -138,11 +156,35 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
         tile_output<kBf16>(x, st, hi, lo);
     }
 
-    __shared__ __attribute__((aligned(16))) ColMergeLds lds;
+    __shared__ __attribute__((aligned(16))) ColMergeLds<W, RK_MAX_GROUP> lds;
+    if constexpr (ALONE) {
+        __shared__ float2 sLse[RK_MAX_GROUP];
+        const int64_t head0 = (int64_t)b * p.Hq + g * G;
+        merge_columns(lds, st, G,
+                      [&](int x, int d, float o0, float o1, float l) {
+                          const float inv = l == 0.f ? 0.f : 1.f / l;
+                          uint16_t* out = p.out + (head0 + x) * kD + d;
+                          out[0] = f32_to_bf16(o0 * inv);      // (out is 2-byte aligned)
+                          out[1] = f32_to_bf16(o1 * inv);
+                      },
+                      [&](int x, float m, float l) {
+                          sLse[x] = lse_of(m, (double)l);
+                          if (p.lse != nullptr) p.lse[head0 + x] = sLse[x].x;
+                      });
+        if constexpr (EMIT) {
+            __syncthreads();                  // (this workgroup's scores are written)
+            for (int x = 0; x < G; ++x) {
+                float* row = p.weights + (head0 + x) * p.w_stride;
+                const float nl = -sLse[x].x, ll = sLse[x].y;
+                for (int j = threadIdx.x; j < n; j += W * 64) row[j] = weight_of(row[j], nl, ll);
+            }
+        }
+        return;
+    }
     float* po = p.part_o + (bg * p.max_chunks + c) * G * kD;
     float* ml = p.part_ml + (bg * kMaxChunks + c) * G * 2;
     merge_columns(lds, st, G,
-                  [&](int x, int d, float o0, float o1) { *reinterpret_cast<float2*>(po + x * kD + d) = make_float2(o0, o1); },
+                  [&](int x, int d, float o0, float o1, float) { *reinterpret_cast<float2*>(po + x * kD + d) = make_float2(o0, o1); },
                   [&](int x, float m, float l) { *reinterpret_cast<float2*>(ml + 2 * x) = make_float2(m, l); });
 }
 
@@ -168,13 +210,6 @@ __device__ __forceinline__ HeadStats head_stats(const AttnParams& p, int G, int6
         l += (double)a[i] * (double)t[i].y;
     }
     return {m, wave_sum(l)};
-}
-// log-sum-exp as hi + lo (no rows: -inf; a NaN among the sums: NaN).
-__device__ __forceinline__ float2 head_lse(const HeadStats& s) {
-    if (s.L == 0.0) return make_float2(-INFINITY, 0.f);
-    const double x = (double)s.M + log(s.L);
-    const float hi = (float)x;
-    return make_float2(hi, (float)(x - (double)hi));
 }
 static_assert(kMaxChunks == 256, "statistics in four registers to a lane");
 
@@ -208,7 +243,8 @@ void q8_finish_kernel(const AttnParams p) {
         }
         for (int gi = w; gi < G; gi += 4) {
             float a[kMaxChunks / 64];
-            const float2 lse = head_lse(head_stats(p, G, bg, gi, nchunks, a));
+            const HeadStats hs = head_stats(p, G, bg, gi, nchunks, a);
+            const float2 lse = lse_of(hs.M, hs.L);
             if (lane == 0) sLse[gi] = lse;
         }
         __syncthreads();
@@ -258,7 +294,7 @@ void q8_finish_kernel(const AttnParams p) {
     uint16_t* out = p.out + (head0 + x) * kD + 2 * lane;
     out[0] = f32_to_bf16((sOut[0][lane].x + sOut[1][lane].x + sOut[2][lane].x + sOut[3][lane].x) * inv);      // (out is 2-byte aligned)
     out[1] = f32_to_bf16((sOut[0][lane].y + sOut[1][lane].y + sOut[2][lane].y + sOut[3][lane].y) * inv);
-    if (lane == 0 && p.lse != nullptr) p.lse[head0 + x] = head_lse(st).x;
+    if (lane == 0 && p.lse != nullptr) p.lse[head0 + x] = lse_of(st.M, st.L).x;
 }
 
 // rk_gather_small_kv out of a cache of 8 bits: 16 lanes to a row.
@@ -332,8 +368,14 @@ extern "C" int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8*
                       full->block == 16 ? 4 : full->block == 32 ? 5 : full->block == 64 ? 6 : 7};
     const dim3 grid(p.nch, geom->n_kv_heads, geom->batch);
     const bool e4m3 = full->format == RK_Q8_E4M3;
-    auto kernel = e4m3 ? (weights ? q8_attn_kernel<RK_Q8_E4M3, true> : q8_attn_kernel<RK_Q8_E4M3, false>)
-                       : (weights ? q8_attn_kernel<RK_Q8_INT8, true> : q8_attn_kernel<RK_Q8_INT8, false>);
+    if (q8_alone(geom, max_len)) {
+        auto kernel = e4m3 ? (weights ? q8_attn_kernel<RK_Q8_E4M3, true, kAlone, true> : q8_attn_kernel<RK_Q8_E4M3, false, kAlone, true>)
+                           : (weights ? q8_attn_kernel<RK_Q8_INT8, true, kAlone, true> : q8_attn_kernel<RK_Q8_INT8, false, kAlone, true>);
+        hipLaunchKernelGGL(kernel, dim3(1, geom->n_kv_heads, geom->batch), dim3(kAlone * 64), 0, (hipStream_t)stream, p, rows);
+        return launch_status();
+    }
+    auto kernel = e4m3 ? (weights ? q8_attn_kernel<RK_Q8_E4M3, true, kColWaves, false> : q8_attn_kernel<RK_Q8_E4M3, false, kColWaves, false>)
+                       : (weights ? q8_attn_kernel<RK_Q8_INT8, true, kColWaves, false> : q8_attn_kernel<RK_Q8_INT8, false, kColWaves, false>);
     hipLaunchKernelGGL(kernel, grid, dim3(kColWaves * 64), 0, (hipStream_t)stream, p, rows);
     if ((rc = launch_status()) != RK_OK) return rc;
     const int tiles = weights ? (max_len + kWeightTile - 1) / kWeightTile : 0;
