@@ -496,8 +496,10 @@ void prompt_tile_kernel(const PromptParams p) {
 }
 
 // ---- up to 16 rows in all ----
-template <bool CAP, bool SLOPE>
-__global__ __launch_bounds__(kColWaves * 64, 2)
+// (W = kColAlone wavefronts where a workgroup has all rows of a (sequence, KV head))
+constexpr int kColAlone = 8;
+template <int W, bool CAP, bool SLOPE>
+__global__ __launch_bounds__(W * 64, W == kColWaves ? 2 : 1)
 void prompt_cols_kernel(const PromptParams p) {
     const int g = blockIdx.y, slot = (int)(blockIdx.z * gridDim.x + blockIdx.x);
     int b = blockIdx.z, split = blockIdx.x, parts = p.splits;
@@ -535,8 +537,8 @@ void prompt_cols_kernel(const PromptParams p) {
     ColState st;
     st.clear();
     TileRows<kBf16> rows;
-    const int step = parts * kColWaves;
-    int t = split * kColWaves + w;
+    const int step = parts * W;
+    int t = split * W + w;
     auto first_of = [&](int x) { return lo + x * kTileRows; };        // (past the rows there are by a round at most: see check_kv)
     if (t < tiles) {
         request_keys<kBf16, false>(rows, k, first_of(t), hi - first_of(t));
@@ -595,7 +597,7 @@ void prompt_cols_kernel(const PromptParams p) {
         request_values<kBf16>(rows, v, first_of(t + step), hi - first_of(t + step));
     }
 
-    __shared__ __attribute__((aligned(16))) ColMergeLds<kColWaves, 16> lds;
+    __shared__ __attribute__((aligned(16))) ColMergeLds<W, 16> lds;
     __shared__ float sInv[16];
     if (p.splits > 1) {
         const int64_t at = ((int64_t)g * p.splits * p.batch + slot) * p.n_new * p.G;
@@ -618,7 +620,7 @@ void prompt_cols_kernel(const PromptParams p) {
                       if (p.lse != nullptr) p.lse[out_row(x)] = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l) * (1.f / kLog2e);
                   });
     __syncthreads();
-    for (int x = threadIdx.x; x < n_rows * (kD / 2); x += kColWaves * 64) {
+    for (int x = threadIdx.x; x < n_rows * (kD / 2); x += W * 64) {
         const int r = x / (kD / 2), d = 2 * (x % (kD / 2));
         *reinterpret_cast<uint32_t*>(p.out + out_row(r) * kD + d) = pack_bf16(o[r * kD + d] * sInv[r], o[r * kD + d + 1] * sInv[r]);
     }
@@ -679,15 +681,17 @@ void prompt_merge_kernel(const PromptParams p) {
 // 64 rows to a wavefront where two rounds of such workgroups or more come together, nothing capped and no bias: those are long enough for the card to lower its clock
 // with the power it draws, and half the reads from LDS then count for more than a second wavefront on the SIMD (us, 64 rows / 32: 8192 tokens of 32 heads over 8
 // 519 / 540, and 445 / 402 with zeros for data, where the clock stays; 4096 tokens 144 / 155; 4 prompts of 1024, one round: 54.9 / 53.9; three capped chunks 132 / 70).
-// Columns: no part with fewer than a round of 128 rows, two workgroups to a compute unit.  Row tiles: one workgroup to a compute unit, two where that leaves parts of more than
+// Columns: no part with fewer than a round of 128 rows, two workgroups to a compute unit; or a larger workgroup alone with all rows and no second launch, where the pairs nearly fill
+// the chip or the sequences are short (us, one token, split / alone: 16 sequences of 500 rows 13.5 / 11.4, of 1000 19.1 / 18.8, 32 of 500 19.0 / 13.2, of 1000 27.6 / 23.0,
+// 64 of 1000, 28 heads over 4, 29.7 / 23.1, 4 of 1000 9.9 / 13.8; 64 of 2000, 32 heads over 8, which four wavefronts take alone: 76.3 / 79.3).  Row tiles: one workgroup to a compute unit, two where that leaves parts of more than
 // 32 tiles of cache rows; no part shorter than split_tiles tiles, which the kernel sees to, as only it knows the ranges.  us, 32 heads over 8, by workgroups in all (256 / 512):
 // 8 tokens behind 32752 33.7 / 35.0, 64 behind 16320 34.8 / 38.3, 128 behind 8064 34.4 / 37.4, 128 behind 32640 99 / 91, 300 behind 7892 64 / 61, 512 behind 32256
 // 348 / 287; by the shortest part (4 / 8 / 16 tiles): 8 tokens behind 992 12.9 / 17.0 / 22.0, 8 behind 4088 14.8 / 18.2 / 26.4, whole prompts of 400 19.1 / 13.9 / 14.0.
 constexpr int kPromptTarget = 2 * kComputeUnits;
-struct PromptPlan { bool cols, wide; int row_tiles, splits, split_tiles; };
+struct PromptPlan { bool cols, wide, alone; int row_tiles, splits, split_tiles; };
 static PromptPlan prompt_plan(const rk_geom* g, int64_t n_new, int64_t max_len, bool plain) {
     const int64_t pairs = (int64_t)g->batch * g->n_kv_heads, rows = n_new * (g->n_q_heads / g->n_kv_heads);
-    PromptPlan f{rows <= 16, plain && pairs * ((rows + 2 * kPromptRows - 1) / (2 * kPromptRows)) >= 2 * kComputeUnits, 1, 1, 1};
+    PromptPlan f{rows <= 16, plain && pairs * ((rows + 2 * kPromptRows - 1) / (2 * kPromptRows)) >= 2 * kComputeUnits, false, 1, 1, 1};
     int64_t s = kPromptTarget / pairs, most = (max_len + kMinChunk - 1) / kMinChunk;
     if (!f.cols) {
         const int tile = f.wide ? 2 * kPromptRows : kPromptRows;
@@ -701,6 +705,8 @@ static PromptPlan prompt_plan(const rk_geom* g, int64_t n_new, int64_t max_len, 
     if (s > most) s = most;
     if (s > kMaxSplits) s = kMaxSplits;
     f.splits = (int)(s < 1 ? 1 : s);
+    f.alone = f.cols && pairs < kPromptTarget && ((pairs >= 64 && max_len <= (pairs > 64 ? 8 * pairs : 512)) || (pairs >= kComputeUnits && ragged_batch_of(g) == 0));
+    if (f.alone) f.splits = 1;
     return f;
 }
 // Rows of partial results that any call of up to n_new tokens and max_len rows can need: a launch that splits has at most
@@ -759,9 +765,12 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
     }
     hipStream_t st = (hipStream_t)stream;
     if (plan.cols) {
-        auto kernel = cap ? (slope ? prompt_cols_kernel<true, true> : prompt_cols_kernel<true, false>)
-                          : (slope ? prompt_cols_kernel<false, true> : prompt_cols_kernel<false, false>);
-        hipLaunchKernelGGL(kernel, dim3(plan.splits, geom->n_kv_heads, geom->batch), dim3(kColWaves * 64), 0, st, p);
+        constexpr int A = kColAlone;
+        auto kernel = plan.alone ? (cap ? (slope ? prompt_cols_kernel<A, true, true> : prompt_cols_kernel<A, true, false>)
+                                        : (slope ? prompt_cols_kernel<A, false, true> : prompt_cols_kernel<A, false, false>))
+                                 : (cap ? (slope ? prompt_cols_kernel<kColWaves, true, true> : prompt_cols_kernel<kColWaves, true, false>)
+                                        : (slope ? prompt_cols_kernel<kColWaves, false, true> : prompt_cols_kernel<kColWaves, false, false>));
+        hipLaunchKernelGGL(kernel, dim3(plan.splits, geom->n_kv_heads, geom->batch), dim3((plan.alone ? A : kColWaves) * 64), 0, st, p);
     } else {
         auto kernel = plan.wide ? prompt_tile_kernel<2, false, false>
                       : cap     ? (slope ? prompt_tile_kernel<1, true, true> : prompt_tile_kernel<1, true, false>)

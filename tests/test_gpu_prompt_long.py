@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from oracle import new_tokens as o
-from test_gpu_prompt_attn import ranges
+from test_gpu_prompt_attn import close, ranges
 
 pytestmark = pytest.mark.gpu
 SCALE = float(np.float32(1 / np.sqrt(128)))
@@ -134,3 +134,24 @@ def test_predicate_and_captured(rk):
         call(eager)
         torch.cuda.synchronize()
         assert torch.equal(held, eager) and (held[1::2] == 9).all()
+
+
+@pytest.mark.parametrize("kind,cap,slopes", [("causal", 0.0, False), ("causal", 5.0, True), ("docs", 0.0, True), ("holes", 4.0, False)])
+@pytest.mark.parametrize("n_b,hq,h,t,rows", [(16, 16, 8, 3, 500), (20, 28, 4, 1, 512), (17, 8, 8, 16, 640), (70, 8, 4, 2, 700)])
+def test_few_tokens_of_many_heads(rk, kind, cap, slopes, n_b, hq, h, t, rows):
+    """A workgroup alone with all rows of a (sequence, KV head), of ragged sequences; what none of them has is NaN."""
+    geom = rk.Geom(n_b, hq, h, 128, SCALE)
+    g = torch.Generator().manual_seed(n_b)
+    lens = [1 + (173 * i) % rows for i in range(n_b)]
+    new = [min(m, t) if i % 4 else min(m, 1) for i, m in enumerate(lens)]
+    q = (torch.randn(n_b, t, hq, 128, generator=g) * 2).to(torch.bfloat16)
+    K, V = (torch.randn(n_b, h, rows, 128, generator=g).to(torch.bfloat16) for _ in range(2))
+    for b, m in enumerate(lens):
+        K[b, :, m:], V[b, :, m:] = math.nan, math.nan
+    first, end = ranges(kind, n_b, t, lens, new, 9)
+    sl = torch.exp2(-torch.arange(1, hq + 1).float() * 6 / hq) if slopes else None
+    out, lse = torch.full((n_b, t, hq, 128), 9.0, dtype=torch.bfloat16, device="cuda"), torch.full((n_b, t, hq), 9.0, device="cuda")
+    rk.rk_prompt_attn(geom, q.cuda(), K.cuda(), V.cuda(), i32(lens), rows, out, new_lens=i32(new), first=None if first is None else i32(first),
+                      end=None if end is None else i32(end), cap=cap, slopes=None if sl is None else sl.cuda(), lse=lse, workspace=rk.PromptWorkspace(geom, t, rows))
+    torch.cuda.synchronize()
+    close(("alone", n_b, hq, h, t, lens, new, kind, cap, slopes), geom, q, K, V, new, first, end, sl, out, lse)
