@@ -184,6 +184,8 @@ void prompt_tile_kernel(const PromptParams p) {
     const int t0 = __builtin_amdgcn_readfirstlane(each * split + rest_tiles * split / parts);
     const int t1 = __builtin_amdgcn_readfirstlane(each * (split + 1) + rest_tiles * (split + 1) / parts);
     const int b0 = 2 * t0, b1 = 2 * t1, end = min(hi, lo + b1 * kBlockRows);       // blocks
+    // the blocks whose stage has nothing to mask and nothing to clean: safe .. safe + n_safe - 1
+    const int safe = (int)(((int64_t)all_lo - lo + kBlockRows - 1) >> 5), n_safe = max((int)(((int64_t)all_hi - lo) >> 5) - kAheadV - safe, 0);
     float m[QB], l[QB], from[QB], limit[QB], alpha[QB];
     f32x16 o[QB][4];
 #pragma unroll
@@ -200,16 +202,14 @@ void prompt_tile_kernel(const PromptParams p) {
     const uint16_t* v_rows = p.v + (int64_t)b * p.s_b + (int64_t)g * p.s_h;
     struct Staged { u32x4 r[2]; };
     // (a block is a buffer of its own: rows that no stage sees read as zeros, without traffic)
-    struct Block { int64_t at; int32_t bytes; };
-    auto block = [&](int i) {
-        const int at = lo + i * kBlockRows;
-        int have = min(end - at, kBlockRows);
+    auto bytes_of = [&](int i) {
+        int have = min(end - (lo + i * kBlockRows), kBlockRows);
         asm("" : "+s"(have));
-        return Block{(int64_t)at * kD, max(have, 0) * (kD * 2)};
+        return max(have, 0) * (kD * 2);
     };
-    auto buffer = [&](const uint16_t* rows, const Block& x) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(rows) + x.at, 0, x.bytes, 0x00020000); };
+    auto buffer = [&](const uint16_t* rows, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(rows), 0, bytes, 0x00020000); };
     auto request = [&](const uint16_t* rows, int i) {
-        const __amdgpu_buffer_rsrc_t rsrc = buffer(rows, block(i));
+        const __amdgpu_buffer_rsrc_t rsrc = buffer(rows + (int64_t)(lo + i * kBlockRows) * kD, bytes_of(i));
         return Staged{__builtin_amdgcn_raw_buffer_load_b128(rsrc, tid * 16, 0, 0), __builtin_amdgcn_raw_buffer_load_b128(rsrc, tid * 16, 4096, 0)};
     };
     const int k_slot = (tid >> 4) * kKRow + (tid & 15) * 16, v_slot = (tid >> 4) * kVRow + (tid & 15) * 16;
@@ -249,7 +249,6 @@ void prompt_tile_kernel(const PromptParams p) {
     auto mask = [&](Ahead& a, int i) {
         const int j0 = lo + 32 * i;
         if (j0 >= in_lo && j0 + 32 <= in_hi) return;
-        asm volatile("" ::: "memory");        // (a branch: most blocks have nothing to mask)
 #pragma unroll
         for (int x = 0; x < QB; ++x) {
 #pragma unroll
@@ -309,15 +308,20 @@ void prompt_tile_kernel(const PromptParams p) {
     // next maximum in the second.  Keys of block i + 2 are at k_next.  Beside it keys of block i + 3 are written to k_to and values of i + 1 to v_to, those of i + 4 and
     // i + 2 requested.
     Staged kr, vr;
+    const uint16_t *k_next_rows = k_rows, *v_next_rows = v_rows;      // of the blocks that are requested next
     auto wait_lds = [](auto n) { __builtin_amdgcn_s_waitcnt(0xc07f | decltype(n)::value << 8); };
-    auto stage = [&](Ahead& now, Ahead& ahead, const Weights& behind, Weights& made, int i, Block& v_rows_at, int k_at, int k_next, int k_to, int v_at, int v_to, bool fenced, bool fence) {
+    auto stage = [&](Ahead& now, Ahead& ahead, const Weights& behind, Weights& made, int i, int& v_bytes, int k_at, int k_next, int k_to, int v_at, int v_to, bool fenced, bool fence) {
         constexpr int kPer = CAP || SLOPE ? 2 : 1, kHalf = kSlots / 2, kTail = kHalf + 2;
-        mask(now, i);
+        if ((uint32_t)(i - safe) >= (uint32_t)n_safe) {
+            asm volatile("" ::: "memory");    // (a branch: most blocks have nothing of it)
+            mask(now, i);
+            clean(vr, i + kAheadV);
+        }
         const bool grew = follow(now);
-        clean(vr, i + kAheadV);
-        const Block k_rows_at = block(i + kAheadK + 1);
-        const __amdgpu_buffer_rsrc_t k_in = buffer(k_rows, k_rows_at), v_in = buffer(v_rows, v_rows_at);
-        v_rows_at = k_rows_at;                // (of V it is requested two stages later)
+        const int k_bytes = bytes_of(i + kAheadK + 1);
+        const __amdgpu_buffer_rsrc_t k_in = buffer(k_next_rows, k_bytes), v_in = buffer(v_next_rows, v_bytes);
+        v_bytes = k_bytes;                    // (of V that block is requested two stages later)
+        k_next_rows += kBlockRows * kD; v_next_rows += kBlockRows * kD;
         bf16x8 kk[8], vv[8];
         float part[QB], wt[16 * QB], far0[QB];
         if constexpr (SLOPE) {
@@ -346,6 +350,7 @@ void prompt_tile_kernel(const PromptParams p) {
                 if (k == 4 * QB) wait_lds(std::integral_constant<int, 4>{});
                 if (k == kHalf) wait_lds(std::integral_constant<int, 4>{});
                 if (k == kHalf + 4 * QB) wait_lds(std::integral_constant<int, 0>{});
+                if (k == kHalf) __builtin_amdgcn_s_waitcnt(0xf70);      // (vmcnt 0: all that the last stage requested, before the first of it is written)
             }
             if (k < kHalf) {
                 ahead.s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[k / QB], q[x][k / QB], ahead.s[x], 0, 0, 0);
@@ -426,7 +431,8 @@ void prompt_tile_kernel(const PromptParams p) {
         for (int c = 0; c < kAheadV; ++c) { clean(vs[c], b0 + c); write_v(vs[c], c * kVBlock, 0); write_v(vs[c], c * kVBlock, 1); }
         kr = request(k_rows, b0 + kAheadK);
         vr = request(v_rows, b0 + kAheadV);
-        Block v_even = block(b0 + kAheadV + 1), v_odd = block(b0 + kAheadV + 2);
+        int v_even = bytes_of(b0 + kAheadV + 1), v_odd = bytes_of(b0 + kAheadV + 2);
+        k_next_rows += (int64_t)(lo + (b0 + kAheadK + 1) * kBlockRows) * kD; v_next_rows += (int64_t)(lo + (b0 + kAheadV + 1) * kBlockRows) * kD;
         __syncthreads();
         Ahead even, odd;
         Weights pe, po{};
@@ -482,7 +488,8 @@ void prompt_tile_kernel(const PromptParams p) {
                     *reinterpret_cast<float4*>(to + 32 * d + 8 * r) = make_float4(o[x][d][4 * r], o[x][d][4 * r + 1], o[x][d][4 * r + 2], o[x][d][4 * r + 3]);
             continue;
         }
-        const int64_t at = ((int64_t)b * p.n_new + me[x].token) * p.Hq + me[x].head;
+        const int token = (uint32_t)(row0 + 32 * x) / (uint32_t)p.G;
+        const int64_t at = ((int64_t)b * p.n_new + token) * p.Hq + g * p.G + (row0 + 32 * x - token * p.G);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         if (h == 0 && p.lse != nullptr) p.lse[at] = sum == 0.f ? -INFINITY : (m[x] + __builtin_amdgcn_logf(sum)) * (1.f / kLog2e);
         uint16_t* to = p.out + at * kD + 4 * h;
