@@ -19,7 +19,7 @@ HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",
                "-mllvm", "-amdgpu-kernarg-preload-count=16",
                "-Wall", "-Wno-unused-function"]
 # Matrix instructions may leave their results in either half of the register file: a wavefront of rk_prompt's larger form holds 370 registers, and without this
-# all of them leave theirs in the half that other instructions do not reach (540 us instead of 519 for 8192 tokens, from the copies).
+# all of them leave theirs in the half that other instructions do not reach (64 copies to a stage of 250 instructions).
 SOURCE_FLAGS = {"rk_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

@@ -107,8 +107,9 @@ __device__ __forceinline__ float only_non_finite(float v) { return (__float_as_u
 // A wavefront takes 32 QB rows and works a block at a time, in stages of 16 QB slots: while the products of the block ahead (S^T) and of the one behind (O^T) are on the matrix
 // cores, it makes weights of the scores between them, a matrix instruction and about five others to a slot.  K and V come through LDS, whose rows are padded so that
 // no two lanes of a read's phase meet in a bank: rings of 4 QB blocks, a barrier to QB stages.
-// 8192 tokens, 32 heads over 8, QB = 2: 519 us, 1059 TFLOP/s (a library matrix product of 8192^3 beside it 1350; with zeros for data, which draw less
-// power, 1236 and 1800).  Three capped chunks, QB = 1: 69 us, 480 TFLOP/s.  Without stages, two tiles of 64 rows in LDS and a barrier a tile: 554 and 76 us.
+// 8192 tokens, 32 heads over 8, QB = 2: 480-490 us, 1120-1145 TFLOP/s (a library matrix product of 8192^3 beside it 1390; with zeros for data, which draw less
+// power, 1320 and 1800).  Three capped chunks, QB = 1: 69 us, 480 TFLOP/s.  Without stages, two tiles of 64 rows in LDS and a barrier a tile: 554 and 76 us.
+// Instructions count: one wavefront on a SIMD issues one every five cycles or so (QB = 2: 218 to a stage, 32 of them products).
 constexpr int kPromptRows = 128, kPromptTile = 64, kMaxSplits = 256;      // (cache rows are split over workgroups in tiles of two blocks)
 constexpr int kBlockRows = 32;
 constexpr int kKRow = kD * 2 + 16, kVRow = kD * 2 + 64;     // bytes from row to row in LDS: the reads of a phase fall on different banks
@@ -688,7 +689,8 @@ void prompt_merge_kernel(const PromptParams p) {
 // Which kernel, and over how many workgroups at most the cache rows of one row tile are split.
 // 64 rows to a wavefront where two rounds of such workgroups or more come together, nothing capped and no bias: those are long enough for the card to lower its clock
 // with the power it draws, and half the reads from LDS then count for more than a second wavefront on the SIMD (us, 64 rows / 32: 8192 tokens of 32 heads over 8
-// 519 / 540, and 445 / 402 with zeros for data, where the clock stays; 4096 tokens 144 / 155; 4 prompts of 1024, one round: 54.9 / 53.9; three capped chunks 132 / 70).
+// 480 / 514, and 416 / 387 with zeros for data, where the clock stays; 4096 tokens 133 / 147, 3000 84.4 / 83.5, 2048 59.0 / 46.9; 4 prompts of 1024 52.3 / 51.9; three
+// capped chunks 132 / 70).
 // Columns: no part with fewer than a round of 128 rows, two workgroups to a compute unit; or a larger workgroup alone with all rows and no second launch, where the pairs nearly fill
 // the chip or the sequences are short (us, one token, split / alone: 16 sequences of 500 rows 13.5 / 11.4, of 1000 19.1 / 18.8, 32 of 500 19.0 / 13.2, of 1000 27.6 / 23.0,
 // 64 of 1000, 28 heads over 4, 29.7 / 23.1, 4 of 1000 9.9 / 13.8; 64 of 2000, 32 heads over 8, which four wavefronts take alone: 76.3 / 79.3).  Row tiles: one workgroup to a compute unit, two where that leaves parts of more than
