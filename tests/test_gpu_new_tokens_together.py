@@ -303,6 +303,93 @@ def test_a_cache_of_8_bits_past_32_bits(rk):
             assert (np.abs(out[0, h].double().cpu().numpy() - want) <= (2.0 ** -8 + 2.0 ** -16) * np.abs(want) + 2.0 ** -16 * np.abs(rows[1][h]).max()).all()
 
 
+@gpu
+def test_two_servers_at_once(rk):
+    """The whole chain on two streams at the same time, each with its own cache and scratch, has the results of one after the other."""
+    B, Hq, H, cap, T, k = 2, 8, 2, 2048, 40, 64
+    geom = rk.Geom(B, Hq, H, 128, SCALE)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    sides = []
+    for _ in range(2):
+        w = torch.randn(B, T, Hq + 2 * H, 128, generator=g, device="cuda").to(torch.bfloat16)
+        K, V = (torch.randn(B, H, cap, 128, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+        sides.append((w, K, V))
+    rope = rk.Rope(rk.rope_table(cap, 128))
+
+    def chain(side):
+        w, K, V = side[0], side[1].clone(), side[2].clone()
+        cache, ws, pws = rk.Kv8.empty(geom, cap, 32, torch.int8), rk.Workspace(geom, cap, k), rk.PromptWorkspace(geom, T, cap)
+        old = i32([2000, 1500])
+        rk.rk_rope_append_q8(geom, None, K[:, :, :2000].transpose(1, 2).contiguous(), V[:, :, :2000].transpose(1, 2).contiguous(), None, cache, old, None, new_lens=old)
+        got = []
+        for r in range(6):
+            sl = old + r + T
+            qo, out = torch.zeros(B, T, Hq, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, T, Hq, 128, dtype=torch.bfloat16, device="cuda")
+            rk.rk_rope_append(geom, w[:, :, :Hq], w[:, :, Hq:Hq + H], w[:, :, Hq + H:], rope, K, V, sl, qo)
+            rk.rk_prompt_attn(geom, qo, K, V, sl, cap, out, workspace=pws)
+            q1 = qo[:, r].contiguous()
+            rk.rk_rope_append_q8(geom, None, w[:, r:r + 1, Hq:Hq + H], w[:, r:r + 1, Hq + H:], rope, cache, old + r + 1, None)
+            o1, wt, idx = torch.zeros(B, Hq, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, Hq, cap, device="cuda"), torch.zeros(B, H, k, dtype=torch.int32, device="cuda")
+            rk.rk_full_attn_q8(geom, q1, cache, old + r + 1, cap, o1, weights=wt, workspace=ws)
+            rk.rk_topk_select(geom, wt, old + r + 1, cap, k, 7, idx, workspace=ws)
+            sK, sV = torch.zeros(2, B, H, k, 128, dtype=torch.bfloat16, device="cuda")
+            rk.rk_gather_small_kv_q8(geom, cache, idx, k, sK, sV, old + r + 1)
+            got += [qo, out, o1, wt, idx, sK, sV]
+        return got + [K, V, cache.k.view(torch.uint8), cache.k_scale, cache.v_tail]
+    one = [chain(x) for x in sides]
+    torch.cuda.synchronize()
+    streams, both = [torch.cuda.Stream() for _ in range(2)], []
+    for s_, x in zip(streams, sides):
+        with torch.cuda.stream(s_):
+            both.append(chain(x))
+    torch.cuda.synchronize()
+    for a, b in zip(one, both):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
+
+
+@gpu
+@pytest.mark.parametrize("eight", [False, True])
+def test_appended_rows_at_the_edges(rk, eight):
+    """One token's rows for all sequences (a batch stride of 0), counts outside 0 .. n_new, sequences that the predicate leaves alone, lengths below the count."""
+    B, Hq, H, T, cap = 4, 4, 2, 5, 64
+    geom = rk.Geom(B, Hq, H, 128, SCALE)
+    g = torch.Generator().manual_seed(19)
+    w = torch.randn(1, T, Hq + 2 * H, 128, generator=g).to(torch.bfloat16).cuda()
+    wide = w.expand(B, T, Hq + 2 * H, 128)
+    rope = rk.Rope(rk.rope_table(cap, 64))
+    lens, new, pred = [5, 40, 3, 50], [99, -3, 5, 2], [1, 1, 1, 0]
+
+    def run(rows, into):
+        qo = torch.full((B, T, Hq, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+        args = (geom, rows[:, :, :Hq], rows[:, :, Hq:Hq + H], rows[:, :, Hq + H:], rope)
+        kw = dict(new_lens=i32(new), pred=i32(pred), pred_val=1)
+        if eight:
+            rk.rk_rope_append_q8(*args, into, i32(lens), qo, **kw)
+        else:
+            rk.rk_rope_append(*args, *into, i32(lens), qo, **kw)
+        torch.cuda.synchronize()
+        return qo
+
+    def room():
+        if eight:
+            return rk.Kv8.empty(geom, cap, 16)
+        return [torch.full((B, H, cap, 128), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    a, b = room(), room()
+    qa, qb = run(wide, a), run(wide.contiguous(), b)
+    held = lambda x: [getattr(x, n).view(torch.uint8) for n in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail")] if eight else x  # noqa: E731
+    assert torch.equal(qa.view(torch.int16), qb.view(torch.int16)) and all(torch.equal(x, y) for x, y in zip(held(a), held(b)))
+    assert (qa[1] == 7).all() and (qa[3] == 7).all()                             # none; left alone
+    # three rows of a sequence of 3 with five new ones: entries 2 .. 4; the first two lie before the cache, and their position is in no table
+    assert qa[2, :2, :, :64].isnan().all() and torch.equal(qa[2, :2, :, 64:], w[0, :2, :Hq, 64:].expand(2, Hq, 64)) and qa[2, 2:].isfinite().all()
+    if eight:
+        assert not a.k_tail[1].any() and not a.k_tail[3].any() and a.k_tail[2, :, :3].isfinite().all() and not a.k_tail[2, :, 3:].any()
+        assert torch.equal(a.v_tail[2, :, :3], w[0, 2:5, Hq + H:].transpose(0, 1)) and torch.equal(a.v_tail[0, :, :5], w[0, :, Hq + H:].transpose(0, 1))
+    else:
+        assert (a[1][1] == 3).all() and (a[1][3] == 3).all() and torch.equal(a[1][2, :, :3], w[0, 2:5, Hq + H:].transpose(0, 1)) and (a[1][2, :, 3:] == 3).all()
+        assert torch.equal(a[1][0, :, :5], w[0, :, Hq + H:].transpose(0, 1))
+
+
 FORMS = {"plain": "", "strided": "", "stream": "", "parameter": "", "subclass": "append append8 full8 gather8 prompt", "numpy_int": "full8 gather8 prompt",
          "wrong_shape": "append append8 full8 prompt", "wrong_type": "append append8 full8 prompt", "other_geometry": "append8 full8 gather8", "int_cap": "prompt"}
 
