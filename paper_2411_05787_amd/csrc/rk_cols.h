@@ -33,9 +33,9 @@ template <> struct TileRows<RK_Q8_INT8> { u32x4 k[2][2]; uint2 v[8]; };
 // Row of the tile that slot e of lane group g of the second product is.
 __device__ __forceinline__ int slot_row(int e, int g) { return (e >> 2) * 16 + 4 * g + (e & 3); }
 
-// Requests the rows at..at + 31 of k, v (base pointers of the (sequence, KV head), the same in the whole wavefront), of which `left` exist (any number, also none): the
-// tile is a buffer of its own, so that a lane's place in it is worked out once for all tiles and rows past the end read as zeros without traffic.
-// All are streamed: see load_rows16.
+// Requests the rows at..at + 31 of k, v (base pointers of the (sequence, KV head), the same in the whole wavefront), of which `left` exist (any
+// number, also none): the tile is a buffer of its own, so that a lane's place in it is worked out once for all tiles and rows past the end read as
+// zeros without traffic. All are streamed: see load_rows16.
 constexpr int kStreamAux = 2;                 // cache-policy operand of buffer loads: nt
 template <int FORMAT>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_buffer(const void* base, int at, int left) {
@@ -115,8 +115,9 @@ __device__ __forceinline__ void value_operands(const TileRows<FORMAT>& t, int h,
     }
 }
 
-// The queries' operands are here once this returns.  Called behind the first tile's requests: left to itself the compiler finds them still on their way
-// where the loop begins, and every round of the loop then waits for all that is in flight (with tiles as buffers 18.4 -> 16.8 us for 32777 rows of 8 bits).
+// The queries' operands are here once this returns.  Called behind the first tile's requests: left to itself the compiler finds them still on their
+// way where the loop begins, and every round of the loop then waits for all that is in flight (with tiles as buffers 18.4 -> 16.8 us for 32777 rows
+// of 8 bits).
 __device__ __forceinline__ void queries_here(bf16x8 (&q)[4]) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -202,8 +203,8 @@ __device__ __forceinline__ void tile_output(const TileRows<FORMAT>& t, ColState&
     }
 }
 
-// The workgroup's columns < ncols <= C merged over its W wavefronts: calls put(column, dim, o0, o1, L) for the pairs of dims (the unnormalised output against the
-// common maximum, and its sum) and stat(column, m, l).
+// The workgroup's columns < ncols <= C merged over its W wavefronts: calls put(column, dim, o0, o1, L) for the pairs of dims (the unnormalised
+// output against the common maximum, and its sum) and stat(column, m, l).
 template <int W, int C> struct ColMergeLds { float m[W][16], l[W][16]; float o[W][C][kD]; };
 template <int W, int C, class Put, class Stat>
 __device__ __forceinline__ void merge_columns(ColMergeLds<W, C>& lds, ColState& st, int ncols, Put&& put, Stat&& stat) {

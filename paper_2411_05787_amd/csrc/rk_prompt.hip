@@ -104,12 +104,13 @@ __device__ __forceinline__ float only_non_finite(float v) { return (__float_as_u
 //                 block of 32;
 //   O^T += V^T P^T  the contraction slots are numbered as S^T left the rows in the lanes, so P goes from the softmax to the matrix cores without
 //                 leaving its lane; V is turned around by the transposing reads of LDS.
-// A wavefront takes 32 QB rows and works a block at a time, in stages of 16 QB slots: while the products of the block ahead (S^T) and of the one behind (O^T) are on the matrix
-// cores, it makes weights of the scores between them, a matrix instruction and about five others to a slot.  K and V come through LDS, whose rows are padded so that
-// no two lanes of a read's phase meet in a bank: rings of 4 QB blocks, a barrier to QB stages.
-// 8192 tokens, 32 heads over 8, QB = 2: 480-490 us, 1120-1145 TFLOP/s (a library matrix product of 8192^3 beside it 1390; with zeros for data, which draw less
-// power, 1320 and 1800).  Three capped chunks, QB = 1: 69 us, 480 TFLOP/s.  Without stages, two tiles of 64 rows in LDS and a barrier a tile: 554 and 76 us.
-// Instructions count: one wavefront on a SIMD issues one every five cycles or so (QB = 2: 218 to a stage, 32 of them products).
+// A wavefront takes 32 QB rows and works a block at a time, in stages of 16 QB slots: while the products of the block ahead (S^T) and of the one
+// behind (O^T) are on the matrix cores, it makes weights of the scores between them, a matrix instruction and about five others to a slot.  K and V
+// come through LDS, whose rows are padded so that no two lanes of a read's phase meet in a bank: rings of 4 QB blocks, a barrier to QB stages. 8192
+// tokens, 32 heads over 8, QB = 2: 480-490 us, 1120-1145 TFLOP/s (a library matrix product of 8192^3 beside it 1390; with zeros for data, which
+// draw less power, 1320 and 1800).  Three capped chunks, QB = 1: 69 us, 480 TFLOP/s.  Without stages, two tiles of 64 rows in LDS and a barrier a
+// tile: 554 and 76 us. Instructions count: one wavefront on a SIMD issues one every five cycles or so (QB = 2: 218 to a stage, 32 of them
+// products).
 constexpr int kPromptRows = 128, kPromptTile = 64, kMaxSplits = 256;      // (cache rows are split over workgroups in tiles of two blocks)
 constexpr int kBlockRows = 32;
 constexpr int kKRow = kD * 2 + 16, kVRow = kD * 2 + 64;     // bytes from row to row in LDS: the reads of a phase fall on different banks
@@ -119,8 +120,9 @@ template <int QB, bool CAP, bool SLOPE>
 __global__ __launch_bounds__(256, QB == 1 ? 2 : 1)
 void prompt_tile_kernel(const PromptParams p) {
     constexpr int kRows = kPromptRows * QB, kSlots = 16 * QB, kRing = 4 * QB, kAheadK = 2 + QB, kAheadV = QB;
-    // Consecutive workgroups go round the 8 dies, and the (sequence, KV head) pairs run fastest: a die sees few pairs (one, where there are 8; the same
-    // head of every sequence), whose rows its L2 keeps, and of each sequence as many row tiles as any other die.  The last tokens', which see most, come first.
+    // Consecutive workgroups go round the 8 dies, and the (sequence, KV head) pairs run fastest: a die sees few pairs (one, where there are 8; the
+    // same head of every sequence), whose rows its L2 keeps, and of each sequence as many row tiles as any other die.  The last tokens', which see
+    // most, come first.
     const int pairs = p.Hkv * p.batch, bg = (int)(blockIdx.x % (uint32_t)pairs);
     int rest = (int)(blockIdx.x / (uint32_t)pairs);
     if (rest >= p.first_round) rest = p.row_tiles * p.splits - 1 - (rest - p.first_round);
@@ -236,8 +238,8 @@ void prompt_tile_kernel(const PromptParams p) {
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
-    // What a stage hands on to the next one, that of block i: its raw products (with CAP or SLOPE what has been made of them), this lane's largest of them, and the first
-    // operands of block i + 1's keys.
+    // What a stage hands on to the next one, that of block i: its raw products (with CAP or SLOPE what has been made of them), this lane's largest
+    // of them, and the first operands of block i + 1's keys.
     struct Ahead { f32x16 s[QB]; float top[QB]; bf16x8 k[4]; };
     struct Weights { u32x4 p[QB][2]; };
     auto score = [&](Ahead& a, int x, int r, float far0) {
@@ -258,8 +260,9 @@ void prompt_tile_kernel(const PromptParams p) {
             for (int r = 0; r < 16; r += 2) largest(a, x, r);
         }
     };
-    // The maximum that weights are taken against follows the true one only when that has grown by more than 8: weights stay below 2^8, the output is rescaled a few
-    // times in all (at the stage's end, when the weights made before have gone into it), and blocks that change nothing cost one comparison.
+    // The maximum that weights are taken against follows the true one only when that has grown by more than 8: weights stay below 2^8, the output
+    // is rescaled a few times in all (at the stage's end, when the weights made before have gone into it), and blocks that change nothing cost one
+    // comparison.
     auto follow = [&](Ahead& a) {
         const bool grew = __any(a.top[0] > limit[0] || (QB > 1 && a.top[QB - 1] > limit[QB - 1]));
         if (grew) {
@@ -304,10 +307,10 @@ void prompt_tile_kernel(const PromptParams p) {
                 for (int x = 0; x < QB; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, pw.p[x][y]), o[x][d], 0, 0, 0);
             }
     };
-    // Block i's stage, in slots of one matrix instruction and what fits beside it: products of block i + 1 (keys at k_at) in the first half, those of block i - 1's
-    // weights (values at v_at) in the other, block i's weights all along or, where scores take work of their own, in the first half, and that and the
-    // next maximum in the second.  Keys of block i + 2 are at k_next.  Beside it keys of block i + 3 are written to k_to and values of i + 1 to v_to, those of i + 4 and
-    // i + 2 requested.
+    // Block i's stage, in slots of one matrix instruction and what fits beside it: products of block i + 1 (keys at k_at) in the first half, those
+    // of block i - 1's weights (values at v_at) in the other, block i's weights all along or, where scores take work of their own, in the first
+    // half, and that and the next maximum in the second.  Keys of block i + 2 are at k_next.  Beside it keys of block i + kAheadK are written to
+    // k_to and values of block i + kAheadV to v_to, those of the blocks behind them requested.
     Staged kr, vr;
     const uint16_t *k_next_rows = k_rows, *v_next_rows = v_rows;      // of the blocks that are requested next
     auto wait_lds = [](auto n) { __builtin_amdgcn_s_waitcnt(0xc07f | decltype(n)::value << 8); };
@@ -504,8 +507,8 @@ void prompt_tile_kernel(const PromptParams p) {
 }
 
 // ---- up to 16 rows in all ----
-// The tile of rk_cols.h; bound by memory: 8 sequences of up to 16384 rows, 356 MB, 63.6 us with the launch that joins the parts (5.6 TB/s), 32 of 4000 rows alone 77 (6.8 TB/s).
-// (W = kColAlone wavefronts where a workgroup has all rows of a (sequence, KV head))
+// The tile of rk_cols.h; bound by memory: 8 sequences of up to 16384 rows, 356 MB, 63.6 us with the launch that joins the parts (5.6 TB/s), 32 of
+// 4000 rows alone 77 (6.8 TB/s). (W = kColAlone wavefronts where a workgroup has all rows of a (sequence, KV head))
 constexpr int kColAlone = 8;
 template <int W, bool CAP, bool SLOPE>
 __global__ __launch_bounds__(W * 64, W == kColWaves ? 2 : 1)
@@ -635,7 +638,8 @@ void prompt_cols_kernel(const PromptParams p) {
     }
 }
 
-// Joins the parts of a row, sum_s 2^(m_s - m) (l_s, o_s): a wavefront each.  8 sequences of one token, 32 heads: 4.2 us, a launch and three dependent reads.
+// Joins the parts of a row, sum_s 2^(m_s - m) (l_s, o_s): a wavefront each.  8 sequences of one token, 32 heads: 4.2 us, a launch and three
+// dependent reads.
 __global__ __launch_bounds__(256)
 void prompt_merge_kernel(const PromptParams p) {
     const int g = blockIdx.y, b = blockIdx.z, w = threadIdx.x >> 6, lane = threadIdx.x & 63, row = blockIdx.x * 4 + w;
@@ -686,17 +690,18 @@ void prompt_merge_kernel(const PromptParams p) {
     if (lane == 0 && p.lse != nullptr) p.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.f / kLog2e);
 }
 
-// Which kernel, and over how many workgroups at most the cache rows of one row tile are split.
-// 64 rows to a wavefront where two rounds of such workgroups or more come together, nothing capped and no bias: those are long enough for the card to lower its clock
-// with the power it draws, and half the reads from LDS then count for more than a second wavefront on the SIMD (us, 64 rows / 32: 8192 tokens of 32 heads over 8
-// 480 / 514, and 416 / 387 with zeros for data, where the clock stays; 4096 tokens 133 / 147, 3000 84.4 / 83.5, 2048 59.0 / 46.9; 4 prompts of 1024 52.3 / 51.9; three
-// capped chunks 132 / 70).
-// Columns: no part with fewer than a round of 128 rows, two workgroups to a compute unit; or a larger workgroup alone with all rows and no second launch, where the pairs nearly fill
-// the chip or the sequences are short (us, one token, split / alone: 16 sequences of 500 rows 13.5 / 11.4, of 1000 19.1 / 18.8, 32 of 500 19.0 / 13.2, of 1000 27.6 / 23.0,
-// 64 of 1000, 28 heads over 4, 29.7 / 23.1, 4 of 1000 9.9 / 13.8; 64 of 2000, 32 heads over 8, which four wavefronts take alone: 76.3 / 79.3).  Row tiles: one workgroup to a compute unit, two where that leaves parts of more than
-// 32 tiles of cache rows; no part shorter than split_tiles tiles, which the kernel sees to, as only it knows the ranges.  us, 32 heads over 8, by workgroups in all (256 / 512):
-// 8 tokens behind 32752 33.7 / 35.0, 64 behind 16320 34.8 / 38.3, 128 behind 8064 34.4 / 37.4, 128 behind 32640 99 / 91, 300 behind 7892 64 / 61, 512 behind 32256
-// 348 / 287; by the shortest part (4 / 8 / 16 tiles): 8 tokens behind 992 12.9 / 17.0 / 22.0, 8 behind 4088 14.8 / 18.2 / 26.4, whole prompts of 400 19.1 / 13.9 / 14.0.
+// Which kernel, and over how many workgroups at most the cache rows of one row tile are split. 64 rows to a wavefront where two rounds of such
+// workgroups or more come together, nothing capped and no bias: those are long enough for the card to lower its clock with the power it draws, and
+// half the reads from LDS then count for more than a second wavefront on the SIMD (us, 64 rows / 32: 8192 tokens of 32 heads over 8 480 / 514, and
+// 416 / 387 with zeros for data, where the clock stays; 4096 tokens 133 / 147, 3000 84.4 / 83.5, 2048 59.0 / 46.9; 4 prompts of 1024 52.3 / 51.9;
+// three capped chunks 132 / 70). Columns: no part with fewer than a round of 128 rows, two workgroups to a compute unit; or a larger workgroup
+// alone with all rows and no second launch, where the pairs nearly fill the chip or the sequences are short (us, one token, split / alone: 16
+// sequences of 500 rows 13.5 / 11.4, of 1000 19.1 / 18.8, 32 of 500 19.0 / 13.2, of 1000 27.6 / 23.0, 64 of 1000, 28 heads over 4, 29.7 / 23.1, 4
+// of 1000 9.9 / 13.8; 64 of 2000, 32 heads over 8, which four wavefronts take alone: 76.3 / 79.3).  Row tiles: one workgroup to a compute unit, two
+// where that leaves parts of more than 32 tiles of cache rows; no part shorter than split_tiles tiles, which the kernel sees to, as only it knows
+// the ranges.  us, 32 heads over 8, by workgroups in all (256 / 512): 8 tokens behind 32752 33.7 / 35.0, 64 behind 16320 34.8 / 38.3, 128 behind
+// 8064 34.4 / 37.4, 128 behind 32640 99 / 91, 300 behind 7892 64 / 61, 512 behind 32256 348 / 287; by the shortest part (4 / 8 / 16 tiles): 8
+// tokens behind 992 12.9 / 17.0 / 22.0, 8 behind 4088 14.8 / 18.2 / 26.4, whole prompts of 400 19.1 / 13.9 / 14.0.
 constexpr int kPromptTarget = 2 * kComputeUnits;
 struct PromptPlan { bool cols, wide, alone; int row_tiles, splits, split_tiles; };
 static PromptPlan prompt_plan(const rk_geom* g, int64_t n_new, int64_t max_len, bool plain) {
@@ -786,8 +791,8 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
                       : cap     ? (slope ? prompt_tile_kernel<1, true, true> : prompt_tile_kernel<1, true, false>)
                                 : (slope ? prompt_tile_kernel<1, false, true> : prompt_tile_kernel<1, false, false>);
         const int64_t total = pairs * plan.row_tiles * plan.splits;
-        // (Where all workgroups are there at once, two to a compute unit, the second ones come in the opposite order: the longest beside the shortest.  8000 tokens of 8
-        // heads 173 -> 165 us, 2048 of 32 over 8 53.0 -> 51.0, three capped chunks 70.3 -> 69.0.)
+        // (Where all workgroups are there at once, two to a compute unit, the second ones come in the opposite order: the longest beside the
+        // shortest.  8000 tokens of 8 heads 173 -> 165 us, 2048 of 32 over 8 53.0 -> 51.0, three capped chunks 70.3 -> 69.0.)
         p.first_round = !plan.wide && total <= 2 * kComputeUnits ? (int)((kComputeUnits + pairs - 1) / pairs) : INT32_MAX;
         hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(256), 0, st, p);
     }

@@ -17,9 +17,10 @@ static int q8_split_workgroups(const rk_geom* g, int32_t max_len, bool weights) 
     return split_workgroups(max_len, (int64_t)g->batch * g->n_kv_heads, kMaxChunks, weights ? emit_split_target(g, max_len) : kComputeUnits);
 }
 
-// One workgroup of kAlone wavefronts to a (sequence, KV head), and no launch behind it: where the pairs fill the chip by themselves and no sharing by length is there to lose,
-// or the sequences are so short that a second launch costs more than the rows.  us, without weights, 32 heads over 8, e4m3 (split / alone): 4 sequences of 500 rows 9.1 / 8.4,
-// of 1000 9.3 / 11.6, 16 of 500 12.5 / 9.6, of 1000 14.6 / 13.6, of 1500 17.3 / 17.5, 32 of 500 16.5 / 10.0, of 2000 30.5 / 24.7, of 4000 49.7 / 43.0, one of 500 8.1 / 8.3.
+// One workgroup of kAlone wavefronts to a (sequence, KV head), and no launch behind it: where the pairs fill the chip by themselves and no sharing
+// by length is there to lose, or the sequences are so short that a second launch costs more than the rows.  us, without weights, 32 heads over 8,
+// e4m3 (split / alone): 4 sequences of 500 rows 9.1 / 8.4, of 1000 9.3 / 11.6, 16 of 500 12.5 / 9.6, of 1000 14.6 / 13.6, of 1500 17.3 / 17.5, 32
+// of 500 16.5 / 10.0, of 2000 30.5 / 24.7, of 4000 49.7 / 43.0, one of 500 8.1 / 8.3.
 constexpr int kAlone = 16;
 static bool q8_alone(const rk_geom* g, int32_t max_len) {
     const int64_t pairs = (int64_t)g->batch * g->n_kv_heads;
@@ -34,10 +35,9 @@ __device__ __forceinline__ float2 lse_of(float m, double l) {
     return make_float2(hi, (float)(x - (double)hi));
 }
 
-// Tiles of a sequence of len rows (of which the call looks at the first n): those of whole blocks, then those of the tail.
-// ALONE: one workgroup of W wavefronts has all rows, and does what the launch behind would.
-// 32777 rows, with weights: 15.5 us (4.6 TB/s with what it writes); 131072: 52.4 us (5.4 TB/s); a tile's requests are ahead by one tile, more does not help (131072 rows 65.0 -> 64.5
-// in all, 32777 21.0 -> 22.8).
+// Tiles of a sequence of len rows (of which the call looks at the first n): those of whole blocks, then those of the tail. ALONE: one workgroup of
+// W wavefronts has all rows, and does what the launch behind would. 32777 rows, with weights: 15.5 us (4.6 TB/s with what it writes); 131072: 52.4
+// us (5.4 TB/s); a tile's requests are ahead by one tile, more does not help (131072 rows 65.0 -> 64.5 in all, 32777 21.0 -> 22.8).
 template <int FORMAT, bool EMIT, int W, bool ALONE>
 __global__ __launch_bounds__(W * 64, ALONE ? 1 : 2)
 void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
@@ -190,9 +190,10 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
                   [&](int x, float m, float l) { *reinterpret_cast<float2*>(ml + 2 * x) = make_float2(m, l); });
 }
 
-// The launch behind it (5.1 us at 32777 rows, 11 at 131072, where it moves 33.5 MB).  Workgroups x < G: the output of query head x of the group, four wavefronts with every fourth partial result each.  The
-// others: kWeightTile positions of all G heads, raw scores -> weights in place, requested before the log-sum-exps that they wait for are worked
-// out, by a wavefront each.  Every wavefront that needs a head's statistics reduces them by itself, without a barrier.
+// The launch behind it (5.1 us at 32777 rows, 11 at 131072, where it moves 33.5 MB).  Workgroups x < G: the output of query head x of the group,
+// four wavefronts with every fourth partial result each.  The others: kWeightTile positions of all G heads, raw scores -> weights in place,
+// requested before the log-sum-exps that they wait for are worked out, by a wavefront each.  Every wavefront that needs a head's statistics reduces
+// them by itself, without a barrier.
 constexpr int kWeightTile = 1024, kOutRound = 16;
 struct HeadStats { float M; double L; };
 // a[i]: what partial result lane + 64 i weighs.
@@ -299,8 +300,8 @@ void q8_finish_kernel(const AttnParams p) {
     if (lane == 0 && p.lse != nullptr) p.lse[head0 + x] = lse_of(st.M, st.L).x;
 }
 
-// rk_gather_small_kv out of a cache of 8 bits: 16 lanes to a row.  Bound by its reads of 128 bytes out of all of the cache: 16 sequences, 101 MB, 21.7 us (4.7 TB/s); 2048 rows 4.2 us,
-// a launch and two dependent reads.
+// rk_gather_small_kv out of a cache of 8 bits: 16 lanes to a row.  Bound by its reads of 128 bytes out of all of the cache: 16 sequences, 101 MB,
+// 21.7 us (4.7 TB/s); 2048 rows 4.2 us, a launch and two dependent reads.
 constexpr int kGatherRows8 = 16;
 template <int FORMAT>
 __global__ __launch_bounds__(256)
