@@ -17,14 +17,16 @@ static int q8_split_workgroups(const rk_geom* g, int32_t max_len, bool weights) 
     return split_workgroups(max_len, (int64_t)g->batch * g->n_kv_heads, kMaxChunks, weights ? emit_split_target(g, max_len) : kComputeUnits);
 }
 
-// One workgroup of kAlone wavefronts to a (sequence, KV head), and no launch behind it: where the pairs fill the chip by themselves and no sharing
-// by length is there to lose, or the sequences are so short that a second launch costs more than the rows.  us, without weights, 32 heads over 8,
-// e4m3 (split / alone): 4 sequences of 500 rows 9.1 / 8.4, of 1000 9.3 / 11.6, 16 of 500 12.5 / 9.6, of 1000 14.6 / 13.6, of 1500 17.3 / 17.5, 32
-// of 500 16.5 / 10.0, of 2000 30.5 / 24.7, of 4000 49.7 / 43.0, one of 500 8.1 / 8.3.
+// One workgroup of kAlone wavefronts to a (sequence, KV head), and no launch behind it: where the pairs fill the chip once or twice and no sharing by
+// length is there to lose, or the sequences are so short that a second launch costs more than the rows.  us, e4m3, 32 heads over 8 unless said
+// (split / alone): without weights 4 sequences of 500 rows 9.1 / 8.4, of 1000 9.3 / 11.6, 16 of 500 12.5 / 9.6, of 1000 14.6 / 13.6, of 1500 17.3 / 17.5, 32
+// of 500 16.5 / 10.0, of 2000 30.5 / 24.7, 64 of 1000 34.9 / 28.9, of 4000 92 / 85, one of 500 8.1 / 8.3, but 100 of 1000 49.8 / 52.5; with weights, which
+// the workgroup goes over once more, 32 of 500 19.6 / 13.2, 64 of 4000 136 / 128, 66 of 1000, 28 heads over 4, 45.8 / 36.4, of 4000 87 / 108.
 constexpr int kAlone = 16;
-static bool q8_alone(const rk_geom* g, int32_t max_len) {
+static bool q8_alone(const rk_geom* g, int32_t max_len, bool weights) {
     const int64_t pairs = (int64_t)g->batch * g->n_kv_heads;
-    return (pairs >= 32 && max_len <= (pairs > 64 ? 8 * pairs : 512)) || (pairs >= kComputeUnits && ragged_batch_of(g) == 0);
+    if (pairs < 32 || pairs > 2 * kComputeUnits) return false;
+    return max_len <= (pairs > 64 ? 8 * pairs : 512) || (!weights && pairs >= kComputeUnits && ragged_batch_of(g) == 0);
 }
 
 // log-sum-exp as hi + lo, of a maximum and a sum (no rows: -inf; a NaN among the sums: NaN).
@@ -175,11 +177,24 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
                       });
         if constexpr (EMIT) {
             __syncthreads();                  // (this workgroup's scores are written)
-            for (int x = 0; x < G; ++x) {
-                float* row = p.weights + (head0 + x) * p.w_stride;
-                const float nl = -sLse[x].x, ll = sLse[x].y;
-                for (int j = threadIdx.x; j < n; j += W * 64) row[j] = weight_of(row[j], nl, ll);
-            }
+            float* first = p.weights + head0 * p.w_stride;
+            auto normalise = [&](int j) {      // four positions of all heads, requested together
+                float v[RK_MAX_GROUP][4];
+#pragma unroll
+                for (int x = 0; x < RK_MAX_GROUP; ++x) {
+                    if (x >= G) break;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) if (j + u * (W * 64) < n) v[x][u] = first[x * p.w_stride + j + u * (W * 64)];
+                }
+#pragma unroll
+                for (int x = 0; x < RK_MAX_GROUP; ++x) {
+                    if (x >= G) break;
+                    const float nl = -sLse[x].x, ll = sLse[x].y;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) if (j + u * (W * 64) < n) first[x * p.w_stride + j + u * (W * 64)] = weight_of(v[x][u], nl, ll);
+                }
+            };
+            for (int j = threadIdx.x; j < n; j += 4 * W * 64) normalise(j);
         }
         return;
     }
@@ -372,7 +387,7 @@ extern "C" int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8*
                       full->block == 16 ? 4 : full->block == 32 ? 5 : full->block == 64 ? 6 : 7};
     const dim3 grid(p.nch, geom->n_kv_heads, geom->batch);
     const bool e4m3 = full->format == RK_Q8_E4M3;
-    if (q8_alone(geom, max_len)) {
+    if (q8_alone(geom, max_len, weights != nullptr)) {
         auto kernel = e4m3 ? (weights ? q8_attn_kernel<RK_Q8_E4M3, true, kAlone, true> : q8_attn_kernel<RK_Q8_E4M3, false, kAlone, true>)
                            : (weights ? q8_attn_kernel<RK_Q8_INT8, true, kAlone, true> : q8_attn_kernel<RK_Q8_INT8, false, kAlone, true>);
         hipLaunchKernelGGL(kernel, dim3(1, geom->n_kv_heads, geom->batch), dim3(kAlone * 64), 0, (hipStream_t)stream, p, rows);

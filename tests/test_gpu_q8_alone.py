@@ -18,7 +18,7 @@ CASES = [
     ("g8_block128", 16, 16, 2, 128, "e4m3", [(37 * i) % 513 for i in range(16)], 512),
     ("g1", 32, 1, 1, 64, "int8", [(61 * i) % 500 for i in range(32)], 512),
     ("longer_rounds", 32, 16, 8, 32, "e4m3", [(409 * i) % 2049 for i in range(32)], 2048),
-    ("more_than_are_shared_out", 66, 12, 4, 32, "int8", [(1031 * i) % 3000 for i in range(66)], 3008),
+    ("more_than_are_shared_out", 66, 12, 4, 32, "int8", [(1031 * i) % 2049 for i in range(66)], 2048),
     ("beyond_the_capacity", 33, 2, 1, 32, "e4m3", [600] * 33, 512),
 ]
 
@@ -56,6 +56,25 @@ def test_attn(rk, case, width):
         for h in range(Hq) if B <= 16 or b % 5 == 0 else (0, Hq - 1):
             check(q, rows, SCALE, b, Hq // H, h, m, a, l, wn, (name, b, h))
         assert (wn[b, :, m:] == -7).all()
+
+
+@pytest.mark.parametrize("n_b,hq,h", [(65, 8, 4), (129, 4, 4)])
+def test_longer_ones_of_more_than_are_shared_out(rk, n_b, hq, h):
+    """Beyond what a workgroup takes alone with its weights, and beyond two workgroups to a compute unit."""
+    lens = [(1213 * i) % 2900 for i in range(n_b)]
+    geom = rk.Geom(n_b, hq, h, 128, SCALE)
+    cache, rows = make(rk, 15, n_b, h, 2912, 32, "e4m3", lens)
+    cache = cache(geom)
+    q = torch.randn(n_b, hq, 128, generator=torch.Generator().manual_seed(16)).to(torch.bfloat16)
+    sl, ws = torch.tensor(lens, dtype=torch.int32, device="cuda"), rk.Workspace(geom, 2912, 1)
+    for weights in (None, torch.zeros(n_b, hq, 2912, device="cuda")):
+        out, lse = torch.full((n_b, hq, 128), 9.0, dtype=torch.bfloat16, device="cuda"), torch.full((n_b, hq), 9.0, device="cuda")
+        rk.rk_full_attn_q8(geom, q.cuda(), cache, sl, 2912, out, weights=weights, lse=lse, workspace=ws)
+        torch.cuda.synchronize()
+        a, l, wn = out.double().cpu().numpy(), lse.double().cpu().numpy(), None if weights is None else weights.double().cpu().numpy()
+        for b in range(0, n_b, 8):
+            for x in (0, hq - 1):
+                check(q, rows, SCALE, b, hq // h, x, lens[b], a, l, wn, (weights is None, b, x))
 
 
 def test_max_len_captured_and_a_nan_block(rk):
