@@ -696,7 +696,7 @@ void prompt_merge_kernel(const PromptParams p) {
 // 416 / 387 with zeros for data, where the clock stays; 4096 tokens 133 / 147, 3000 84.4 / 83.5, 2048 59.0 / 46.9; 4 prompts of 1024 52.3 / 51.9;
 // three capped chunks 132 / 70). Columns: no part with fewer than a round of 128 rows, two workgroups to a compute unit; or a larger workgroup
 // alone with all rows and no second launch, where the pairs nearly fill the chip or the sequences are short (us, one token, split / alone: 16
-// sequences of 500 rows 13.5 / 11.4, of 1000 19.1 / 18.8, 32 of 500 19.0 / 13.2, of 1000 27.6 / 23.0, 64 of 1000, 28 heads over 4, 29.7 / 23.1, 4
+// sequences of 500 rows 13.5 / 11.4, of 1000 19.1 / 18.8, of up to 1000 15.9 / 17.5, 32 of 500 19.0 / 13.2, of 1000 27.6 / 23.0, 64 of 1000, 28 heads over 4, 29.7 / 23.1, 4
 // of 1000 9.9 / 13.8; 64 of 2000, 32 heads over 8, which four wavefronts take alone: 76.3 / 79.3).  Row tiles: one workgroup to a compute unit, two
 // where that leaves parts of more than 32 tiles of cache rows; no part shorter than split_tiles tiles, which the kernel sees to, as only it knows
 // the ranges.  us, 32 heads over 8, by workgroups in all (256 / 512): 8 tokens behind 32752 33.7 / 35.0, 64 behind 16320 34.8 / 38.3, 128 behind
@@ -720,7 +720,7 @@ static PromptPlan prompt_plan(const rk_geom* g, int64_t n_new, int64_t max_len, 
     if (s > most) s = most;
     if (s > kMaxSplits) s = kMaxSplits;
     f.splits = (int)(s < 1 ? 1 : s);
-    f.alone = f.cols && pairs < kPromptTarget && ((pairs >= 64 && max_len <= (pairs > 64 ? 8 * pairs : 512)) || (pairs >= kComputeUnits && ragged_batch_of(g) == 0));
+    f.alone = f.cols && pairs >= 64 && pairs < kPromptTarget && (max_len <= (pairs >= kComputeUnits ? 8 * pairs : 512) || (pairs >= kComputeUnits && ragged_batch_of(g) == 0));
     if (f.alone) f.splits = 1;
     return f;
 }
