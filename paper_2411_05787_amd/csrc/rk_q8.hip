@@ -7,6 +7,8 @@
 
 namespace rk {
 
+// Four weights of a row, which starts at any multiple of four bytes: memory takes them as one access all the same.
+typedef float Floats4 __attribute__((ext_vector_type(4), aligned(4)));
 struct Q8Rows { const uint8_t *k, *v; const float *ks, *vs; const uint16_t *kt, *vt; int64_t s_b; int32_t s_h, blocks, shift; };
 
 // Workgroups per (sequence, KV head): with the scores returned as the step over the bf16 cache has it, without them one to a compute unit, as
@@ -85,16 +87,16 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[x][i] *= x ? k1 : k0;
         }
-        if (EMIT && p.w_vec != 0 && rows >= kTileRows) {      // (the same for the whole wavefront)
+        if (EMIT && rows >= kTileRows) {      // (the same for the whole wavefront)
             // the second block's scores to the lanes behind the group's: whole lines of 128 bytes leave in one store
             const int from = (lane & 48) + (col >= G ? col - G : col);
-            float4 v;
+            Floats4 v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float up = __int_as_float(__builtin_amdgcn_ds_bpermute(from * 4, __float_as_int(s[1][i])));
-                (&v.x)[i] = col < G ? s[0][i] : up;
+                v[i] = col < G ? s[0][i] : up;
             }
-            if (col < 2 * G) *reinterpret_cast<float4*>(wline + first + 4 * gr) = v;
+            if (col < 2 * G) *reinterpret_cast<Floats4*>(wline + first + 4 * gr) = v;
         } else if (EMIT && col < G) {
             float* to = wrow + first + 4 * gr;
 #pragma unroll
@@ -246,14 +248,15 @@ void q8_finish_kernel(const AttnParams p) {
         float* rows = p.weights + head0 * p.w_stride + j0;
         const int n = len - j0;
         float v[RK_MAX_GROUP][4];
-        const bool vec = p.w_vec != 0 && n >= kWeightTile;
+        const bool vec = n >= kWeightTile;
 #pragma unroll
         for (int gi = 0; gi < RK_MAX_GROUP; ++gi) {
             if (gi >= G) break;
             const float* row = rows + gi * p.w_stride;
             if (vec) {
-                const float4 f = *reinterpret_cast<const float4*>(row + 4 * tid);
-                v[gi][0] = f.x; v[gi][1] = f.y; v[gi][2] = f.z; v[gi][3] = f.w;
+                const Floats4 f = *reinterpret_cast<const Floats4*>(row + 4 * tid);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[gi][i] = f[i];
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[gi][i] = tid + 256 * i < n ? row[tid + 256 * i] : 0.f;
@@ -274,7 +277,7 @@ void q8_finish_kernel(const AttnParams p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[gi][i] = weight_of(v[gi][i], nl, ll);
             if (vec) {
-                *reinterpret_cast<float4*>(row + 4 * tid) = make_float4(v[gi][0], v[gi][1], v[gi][2], v[gi][3]);
+                *reinterpret_cast<Floats4*>(row + 4 * tid) = Floats4{v[gi][0], v[gi][1], v[gi][2], v[gi][3]};
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) if (tid + 256 * i < n) row[tid + 256 * i] = v[gi][i];
@@ -377,7 +380,7 @@ extern "C" int rk_full_attn_q8(const rk_geom* geom, const void* q, const rk_kv8*
     p.Hq = geom->n_q_heads; p.Hkv = geom->n_kv_heads;
     p.scale = geom->scale;
     p.out = (uint16_t*)out;
-    p.weights = weights; p.w_stride = w_stride; p.w_vec = weights && w_stride % 4 == 0 && aligned16(weights) ? 1 : 0;
+    p.weights = weights; p.w_stride = w_stride;
     p.lse = lse;
     p.pred = pred; p.pred_val = pred_val;
     p.counters = ws.counters; p.part_ml = ws.part_ml; p.part_o = ws.part_o; p.max_chunks = ws.max_chunks;
