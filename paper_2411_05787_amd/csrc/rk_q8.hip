@@ -7,7 +7,8 @@
 
 namespace rk {
 
-// Four weights of a row, which starts at any multiple of four bytes: memory takes them as one access all the same.
+// Four weights of a row, which starts at any multiple of four bytes: memory takes them as one access all the same.  They are streamed: stores that
+// the caches keep cost 131072 rows 64.9 us instead of 60.9 (45 without weights at all).
 typedef float Floats4 __attribute__((ext_vector_type(4), aligned(4)));
 struct Q8Rows { const uint8_t *k, *v; const float *ks, *vs; const uint16_t *kt, *vt; int64_t s_b; int32_t s_h, blocks, shift; };
 
@@ -96,7 +97,7 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
                 const float up = __int_as_float(__builtin_amdgcn_ds_bpermute(from * 4, __float_as_int(s[1][i])));
                 v[i] = col < G ? s[0][i] : up;
             }
-            if (col < 2 * G) *reinterpret_cast<Floats4*>(wline + first + 4 * gr) = v;
+            if (col < 2 * G) __builtin_nontemporal_store(v, reinterpret_cast<Floats4*>(wline + first + 4 * gr));
         } else if (EMIT && col < G) {
             float* to = wrow + first + 4 * gr;
 #pragma unroll
@@ -254,7 +255,7 @@ void q8_finish_kernel(const AttnParams p) {
             if (gi >= G) break;
             const float* row = rows + gi * p.w_stride;
             if (vec) {
-                const Floats4 f = *reinterpret_cast<const Floats4*>(row + 4 * tid);
+                const Floats4 f = __builtin_nontemporal_load(reinterpret_cast<const Floats4*>(row + 4 * tid));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[gi][i] = f[i];
             } else {
@@ -277,7 +278,7 @@ void q8_finish_kernel(const AttnParams p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[gi][i] = weight_of(v[gi][i], nl, ll);
             if (vec) {
-                *reinterpret_cast<Floats4*>(row + 4 * tid) = Floats4{v[gi][0], v[gi][1], v[gi][2], v[gi][3]};
+                __builtin_nontemporal_store(Floats4{v[gi][0], v[gi][1], v[gi][2], v[gi][3]}, reinterpret_cast<Floats4*>(row + 4 * tid));
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) if (tid + 256 * i < n) row[tid + 256 * i] = v[gi][i];
