@@ -7,14 +7,15 @@
 
 namespace rk {
 
-// Four weights of a row, which starts at any multiple of four bytes: memory takes them as one access all the same.  They are streamed: stores that
-// the caches keep cost 131072 rows 64.9 us instead of 60.9 (45 without weights at all).
+// Four weights of a row, which starts at any multiple of four bytes: memory takes them as one access all the same.  Those that a second
+// launch reads are streamed: stores that the caches keep cost 131072 rows 64.9 us instead of 60.9 (45 without weights at all).  Where the workgroup that wrote
+// them reads them, the caches keep them: 64 sequences of 4000 rows 131.1 -> 128.0, of 1000 41.1 -> 39.9.
 typedef float Floats4 __attribute__((ext_vector_type(4), aligned(4)));
 struct Q8Rows { const uint8_t *k, *v; const float *ks, *vs; const uint16_t *kt, *vt; int64_t s_b; int32_t s_h, blocks, shift; };
 
 // Workgroups per (sequence, KV head): with the scores returned as the step over the bf16 cache has it, without them one to a compute unit, as
-// no stores come between the requests.  us by workgroups in all (256 / 512 / 768 / 1024), 32 heads over 8, e4m3: with weights 32777 rows 21.0 /
-// 21.3 / 22.4 / 24.3, 65536 37.4 / 34.4 / 34.9 / 34.6, 131072 71.7 / 70.4 / 68.0 / 65.4, without 65536 26.5 / 26.6 / 28.2 / 28.7, 4 sequences of
+// no stores come between the requests.  us by workgroups in all (256 / 512 / 768 / 1024), 32 heads over 8, e4m3: with weights 32777 rows 20.8 /
+// 21.3 / 22.2 / 23.9, 65536 35.5 / 35.4 / 35.8 / 34.2, 131072 70.3 / 68.0 / 66.9 / 60.7, without 65536 26.4 / 26.9 / 28.6 / 28.8, 4 sequences of
 // 32768 45.0 / 46.7 / 47.2 / 47.6, 16 ragged ones of up to 16384, 28 over 4, int8 36.2 / 35.6 / 35.7 / 38.9.
 static int q8_split_workgroups(const rk_geom* g, int32_t max_len, bool weights) {
     return split_workgroups(max_len, (int64_t)g->batch * g->n_kv_heads, kMaxChunks, weights ? emit_split_target(g, max_len) : kComputeUnits);
@@ -24,7 +25,7 @@ static int q8_split_workgroups(const rk_geom* g, int32_t max_len, bool weights) 
 // length is there to lose, or the sequences are so short that a second launch costs more than the rows.  us, e4m3, 32 heads over 8 unless said
 // (split / alone): without weights 4 sequences of 500 rows 9.1 / 8.4, of 1000 9.3 / 11.6, 16 of 500 12.5 / 9.6, of 1000 14.6 / 13.6, of 1500 17.3 / 17.5, 32
 // of 500 16.5 / 10.0, of 2000 30.5 / 24.7, 64 of 1000 34.9 / 28.9, of 4000 92 / 85, one of 500 8.1 / 8.3, but 100 of 1000 49.8 / 52.5; with weights, which
-// the workgroup goes over once more, 32 of 500 19.6 / 13.2, 64 of 4000 136 / 128, 66 of 1000, 28 heads over 4, 45.8 / 36.4, of 4000 87 / 108.
+// the workgroup goes over once more, 32 of 500 19.6 / 13.2, 64 of 4000 139 / 128, 66 of 1000, 28 heads over 4, 47.4 / 36.4, of 4000 87 / 108.
 constexpr int kAlone = 16;
 static bool q8_alone(const rk_geom* g, int32_t max_len, bool weights) {
     const int64_t pairs = (int64_t)g->batch * g->n_kv_heads;
@@ -41,8 +42,9 @@ __device__ __forceinline__ float2 lse_of(float m, double l) {
 }
 
 // Tiles of a sequence of len rows (of which the call looks at the first n): those of whole blocks, then those of the tail. ALONE: one workgroup of
-// W wavefronts has all rows, and does what the launch behind would. 32777 rows, with weights: 15.5 us (4.6 TB/s with what it writes); 131072: 52.4
-// us (5.4 TB/s); a tile's requests are ahead by one tile, more does not help (131072 rows 65.0 -> 64.5 in all, 32777 21.0 -> 22.8).
+// W wavefronts has all rows, and does what the launch behind would. 32777 rows, with weights: 15.5 us (4.6 TB/s with what it writes); 131072: 50.4
+// us (5.7 TB/s); a tile's requests are ahead by one tile, more does not help (measured before the scores were streamed: 131072 rows
+// 65.0 -> 64.5 in all, 32777 21.0 -> 22.8).
 template <int FORMAT, bool EMIT, int W, bool ALONE>
 __global__ __launch_bounds__(W * 64, ALONE ? 1 : 2)
 void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
@@ -97,7 +99,11 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
                 const float up = __int_as_float(__builtin_amdgcn_ds_bpermute(from * 4, __float_as_int(s[1][i])));
                 v[i] = col < G ? s[0][i] : up;
             }
-            if (col < 2 * G) __builtin_nontemporal_store(v, reinterpret_cast<Floats4*>(wline + first + 4 * gr));
+            if (col < 2 * G) {
+                Floats4* to = reinterpret_cast<Floats4*>(wline + first + 4 * gr);
+                if constexpr (ALONE) *to = v;
+                else __builtin_nontemporal_store(v, to);
+            }
         } else if (EMIT && col < G) {
             float* to = wrow + first + 4 * gr;
 #pragma unroll
@@ -208,7 +214,7 @@ void q8_attn_kernel(const AttnParams p, const Q8Rows c8) {
                   [&](int x, float m, float l) { *reinterpret_cast<float2*>(ml + 2 * x) = make_float2(m, l); });
 }
 
-// The launch behind it (5.1 us at 32777 rows, 11 at 131072, where it moves 33.5 MB).  Workgroups x < G: the output of query head x of the group,
+// The launch behind it (5.1 us at 32777 rows, 10.2 at 131072, where it moves 33.5 MB).  Workgroups x < G: the output of query head x of the group,
 // four wavefronts with every fourth partial result each.  The others: kWeightTile positions of all G heads, raw scores -> weights in place,
 // requested before the log-sum-exps that they wait for are worked out, by a wavefront each.  Every wavefront that needs a head's statistics reduces
 // them by itself, without a barrier.
