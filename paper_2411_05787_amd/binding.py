@@ -308,6 +308,7 @@ class Workspace:
         self.max_len = int(max_len)
         self.nbytes = workspace_bytes(geom, max_len, max_k)
         self.buf = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
+        self.device_index = self.buf.device.index
         self.ptr = (self.buf.data_ptr() + 255) // 256 * 256
         rk_workspace_init(geom, self, stream=stream)
 
@@ -916,7 +917,9 @@ def rk_full_attn_q8(geom: Geom, q, cache: Kv8, seq_lens, max_len: int, out, weig
     if rc is not None:
         return _check("rk_full_attn_q8", rc)
     B, Hq, D = geom.batch, geom.n_q_heads, geom.head_dim
-    dev = _same_device(_cache8(geom, cache), q, seq_lens, out, weights, lse, pred)
+    if workspace is None:
+        raise ValueError("a workspace is required")
+    dev = _same_device(_cache8(geom, cache), q, seq_lens, out, weights, lse, pred, workspace.buf)
     if max_len > cache.capacity:
         raise ValueError("max_len %d exceeds the cache capacity %d" % (max_len, cache.capacity))
     w_stride = 0
@@ -957,6 +960,7 @@ class PromptWorkspace:
         self.geom, self.n_new, self.max_len = geom, int(n_new), int(max_len)
         self.nbytes = rk_prompt_workspace_bytes(geom, n_new, max_len)
         self.buf = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
+        self.device_index = self.buf.device.index
         self.ptr = (self.buf.data_ptr() + 255) // 256 * 256
 
 

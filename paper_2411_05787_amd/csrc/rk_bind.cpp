@@ -119,6 +119,12 @@ struct Args {
         Scratch s{(void*)attribute(a[i], ptr), (size_t)attribute(a[i], bytes)};
         return s;
     }
+    Scratch workspace_here(int i) {           // ... that has to be in the memory of the other arguments' device
+        static PyObject* const dev = PyUnicode_InternFromString("device_index");
+        const Scratch s = workspace(i);
+        on((int64_t)attribute(a[i], dev));
+        return s;
+    }
     void* stream(int i) {                     // (asked for last, once every tensor is known to be in GPU memory)
         if (!ok || !g_stream) { ok = false; return nullptr; }
         PyObject *d = nullptr, *h = nullptr;
@@ -311,7 +317,7 @@ PyObject* full_attn_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         auto* lse = (float*)x.dev_or_null(7, f32, {g.batch, g.n_q_heads});
         auto* pred = (const int32_t*)x.dev_or_null(8, i32t, {g.batch});
-        const Args::Scratch ws = x.workspace(10);
+        const Args::Scratch ws = x.workspace_here(10);
         void* st = x.stream_here(11);
         if (!x.ok || max_len > c8.capacity) return nullptr;
         return status_of([&] { return rk_full_attn_q8(&g, q, &c8, lens, max_len, out, weights, width, lse, pred, pred_val, ws.ptr, ws.bytes, st); });
@@ -354,7 +360,7 @@ PyObject* prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
         s.slopes = (const float*)x.dev_or_null(11, f32, {g.n_q_heads});
         auto* lse = (float*)x.dev_or_null(12, f32, {g.batch, T, g.n_q_heads});
         auto* pred = (const int32_t*)x.dev_or_null(13, i32t, {g.batch});
-        const Args::Scratch ws = x.a[15] == Py_None ? Args::Scratch{nullptr, 0} : x.workspace(15);
+        const Args::Scratch ws = x.a[15] == Py_None ? Args::Scratch{nullptr, 0} : x.workspace_here(15);
         void* st = x.stream_here(16);
         if (!x.ok) return nullptr;
         return status_of([&] { return rk_prompt_attn(&g, q.ptr, q.b, q.t, (int32_t)T, kv, lens, new_lens, max_len, &s, out, lse, pred, pred_val, ws.ptr, ws.bytes, st); });
