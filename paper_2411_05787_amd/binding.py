@@ -771,8 +771,7 @@ def rope_table(max_pos: int, rot_dim: int, base: float = 10000.0, factor: float 
     if max_pos < 1 or rot_dim < 1:
         raise ValueError("max_pos and rot_dim must be positive")
     table = torch.empty(int(max_pos), int(rot_dim), dtype=torch.float32, device=device)
-    with torch.cuda.device(table.device):
-        rk_rope_table(table, base, factor, low_turns, high_turns, original_len, amplitude, stream=stream)
+    rk_rope_table(table, base, factor, low_turns, high_turns, original_len, amplitude, stream=stream)
     return table
 
 
@@ -781,7 +780,7 @@ def rk_rope_table(table: torch.Tensor, base: float = 10000.0, factor: float = 1.
     if table.dim() != 2:
         raise ValueError("table must be [max_pos, rot_dim]")
     s = _RopeScaling(float(base), float(factor), float(low_turns), float(high_turns), float(original_len), float(amplitude))
-    _check("rk_rope_table", lib.rk_rope_table(_dev(table, torch.float32, "table"), table.shape[0], table.shape[1], C.byref(s), _stream(stream)))
+    _launch("rk_rope_table", table.device, stream, _dev(table, torch.float32, "table"), table.shape[0], table.shape[1], C.byref(s))
 
 
 Q8_FORMATS = {torch.float8_e4m3fn: 0, torch.int8: 1}
