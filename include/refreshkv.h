@@ -689,7 +689,8 @@ int rk_gather_small_kv_q8(const rk_geom* geom, const rk_kv8* full, const int32_t
 /* ---- attention of new tokens ---------------------------------------------------------------- */
 
 /* What rk_prompt_attn does with the scores (a NULL pointer to it: the plain causal step).
- *   cap     > 0: the score x = scale * <q, k> becomes cap * tanh(x / cap);  0: as it is
+ *   cap     > 0: the score x = scale * <q, k> becomes cap * tanh(x / cap), to 2^-22 of the cap where that is at most 128, to 2^-19 of itself with a
+ *           larger one (any finite number: one far above all scores leaves them as they are);  0: as it is
  *   slopes  device fp32 [n_q_heads] or NULL: minus slopes[h] * |position of the token - row|, after the cap
  *   first, end  device int32 [batch, n_new] or NULL: token i of sequence b sees the rows first[b,i] <= j < end[b,i] of the cache.  NULL: from
  *           row 0, and up to its own row.  Packed documents: first = the row where the token's document starts.  A prefix that sees itself

@@ -10,6 +10,7 @@
 // Where there are few rows the cache rows are split over workgroups, and prompt_merge_kernel joins their (maximum, sum, output).
 #include "rk_cols.h"
 
+#include <cfloat>
 #include <type_traits>
 
 namespace rk {
@@ -67,18 +68,32 @@ __device__ __forceinline__ int wave_min(int v) {
 }
 __device__ __forceinline__ int wave_max_i(int v) { return ~wave_min(~v); }
 
-// Raw product x -> score = a * bend(x) + b, in units of ln 2 or 1 / `unit` of that.  Without a cap bend(x) = x; with one, cap tanh(y / cap) =
-// 2 cap / (1 + e^(-2 y / cap)) - cap, right at both ends and off by 2^-22 of the cap between: one exponential and one reciprocal, and the
-// product and sum around them become part of the multiply-add ahead of the weight's exponential.
-struct ScoreForm { float a, b, inner; };
-template <bool CAP>
+// Raw product x -> score = a * bend(x) + b, in units of ln 2 or 1 / `unit` of that.  CAP says how bend caps:
+//   kNoCap    bend(x) = x.
+//   kNearCap  y = scale * x, cap tanh(y / cap) = 2 cap / (1 + e^(-2 y / cap)) - cap: one exponential and one reciprocal, and the product and sum around
+//             them become part of the multiply-add ahead of the weight's exponential.  A difference of numbers of the cap's size: right at both ends and
+//             off by 2^-22 of the cap between, 2^-15 for the largest cap that takes it (kNearCapMost).
+//   kFarCap   any cap, to 2^-19 of the score: y (1 - z^2 / 3 + 2 z^4 / 15 - 17 z^6 / 315 + 62 z^8 / 2835), z = y / cap, where |z| < 1/4 (what the series
+//             leaves out is below 2^-26 there), and as above beyond, where tanh is no smaller than 0.24.  Three capped chunks 93.4 us, kNearCap 69.1.
+constexpr int kNoCap = 0, kNearCap = 1, kFarCap = 2;
+constexpr float kNearCapMost = 128.f;
+struct ScoreForm { float a, b, inner, per, cap; };
+template <int CAP>
 __device__ __forceinline__ ScoreForm score_form(const PromptParams& p, float unit) {
-    if constexpr (CAP) return {2.f * p.cap * unit, -p.cap * unit, p.scale / p.cap * (-2.f * kLog2e)};
-    return {p.scale * unit, 0.f, 0.f};
+    // (kept finite below caps of 1e-38 or so: a product of 0 stays 0)
+    if constexpr (CAP == kNearCap) return {2.f * p.cap * unit, -p.cap * unit, fminf(fmaxf(p.scale / p.cap * (-2.f * kLog2e), -FLT_MAX), FLT_MAX), 0.f, 0.f};
+    if constexpr (CAP == kFarCap) return {unit, 0.f, p.scale, 1.f / p.cap, p.cap};
+    return {p.scale * unit, 0.f, 0.f, 0.f, 0.f};
 }
-template <bool CAP>
+template <int CAP>
 __device__ __forceinline__ float bend(float x, const ScoreForm& f) {
-    if constexpr (CAP) return __builtin_amdgcn_rcpf(fast_exp2(x * f.inner) + 1.f);
+    if constexpr (CAP == kNearCap) return __builtin_amdgcn_rcpf(fast_exp2(x * f.inner) + 1.f);
+    if constexpr (CAP == kFarCap) {
+        const float y = x * f.inner, z = y * f.per, zz = z * z;
+        const float near = y * fmaf(zz, fmaf(zz, fmaf(zz, fmaf(zz, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+        const float far = f.cap * fmaf(2.f, __builtin_amdgcn_rcpf(fast_exp2(z * (-2.f * kLog2e)) + 1.f), -1.f);
+        return fabsf(z) < 0.25f ? near : far;
+    }
     return x;
 }
 
@@ -116,7 +131,7 @@ constexpr int kBlockRows = 32;
 constexpr int kKRow = kD * 2 + 16, kVRow = kD * 2 + 64;     // bytes from row to row in LDS: the reads of a phase fall on different banks
 constexpr int kKBlock = kBlockRows * kKRow, kVBlock = kBlockRows * kVRow;
 
-template <int QB, bool CAP, bool SLOPE>
+template <int QB, int CAP, bool SLOPE>
 __global__ __launch_bounds__(256, QB == 1 ? 2 : 1)
 void prompt_tile_kernel(const PromptParams p) {
     constexpr int kRows = kPromptRows * QB, kSlots = 16 * QB, kRing = 4 * QB, kAheadK = 2 + QB, kAheadV = QB;
@@ -243,7 +258,7 @@ void prompt_tile_kernel(const PromptParams p) {
     struct Ahead { f32x16 s[QB]; float top[QB]; bf16x8 k[4]; };
     struct Weights { u32x4 p[QB][2]; };
     auto score = [&](Ahead& a, int x, int r, float far0) {
-        if constexpr (CAP) a.s[x][r] = bend<CAP>(a.s[x][r], form);
+        if constexpr (CAP != kNoCap) a.s[x][r] = bend<CAP>(a.s[x][r], form);
         if constexpr (SLOPE) a.s[x][r] = fmaf(-slope2[x], fabsf(far0 - (float)(8 * (r >> 2) + (r & 3))), fmaf(a.s[x][r], form.a, form.b));
     };
     auto largest = [&](Ahead& a, int x, int r) {      // of elements up to r + 1, r from 0 in steps of 2
@@ -315,7 +330,7 @@ void prompt_tile_kernel(const PromptParams p) {
     const uint16_t *k_next_rows = k_rows, *v_next_rows = v_rows;      // of the blocks that are requested next
     auto wait_lds = [](auto n) { __builtin_amdgcn_s_waitcnt(0xc07f | decltype(n)::value << 8); };
     auto stage = [&](Ahead& now, Ahead& ahead, const Weights& behind, Weights& made, int i, int& v_bytes, int k_at, int k_next, int k_to, int v_at, int v_to, bool fenced, bool fence) {
-        constexpr int kPer = CAP || SLOPE ? 2 : 1, kHalf = kSlots / 2, kTail = kHalf + 2;
+        constexpr int kPer = CAP != kNoCap || SLOPE ? 2 : 1, kHalf = kSlots / 2, kTail = kHalf + 2;
         if ((uint32_t)(i - safe) >= (uint32_t)n_safe) {
             asm volatile("" ::: "memory");    // (a branch: most blocks have nothing of it)
             mask(now, i);
@@ -377,7 +392,7 @@ void prompt_tile_kernel(const PromptParams p) {
                 if (e >= 3 && e % 2 == 1) { if (kPer == 2) add(e - 3); pack(e - 3); }
             }
             if (k >= kTail) {
-                if constexpr (CAP || SLOPE) {
+                if constexpr (CAP != kNoCap || SLOPE) {
 #pragma unroll
                     for (int e = (k - kTail) * 16 * QB / (kSlots - kTail); e < (k - kTail + 1) * 16 * QB / (kSlots - kTail); ++e) {
                         score(ahead, e >> 4, e & 15, far0[e >> 4]);
@@ -510,7 +525,7 @@ void prompt_tile_kernel(const PromptParams p) {
 // The tile of rk_cols.h; bound by memory: 8 sequences of up to 16384 rows, 356 MB, 63.6 us with the launch that joins the parts (5.6 TB/s), 32 of
 // 4000 rows alone 77 (6.8 TB/s). (W = kColAlone wavefronts where a workgroup has all rows of a (sequence, KV head))
 constexpr int kColAlone = 8;
-template <int W, bool CAP, bool SLOPE>
+template <int W, int CAP, bool SLOPE>
 __global__ __launch_bounds__(W * 64, W == kColWaves ? 2 : 1)
 void prompt_cols_kernel(const PromptParams p) {
     const int g = blockIdx.y, slot = (int)(blockIdx.z * gridDim.x + blockIdx.x);
@@ -732,6 +747,23 @@ static int64_t prompt_partials(const rk_geom* g, int64_t n_new, int64_t max_len)
     return pairs > kPromptTarget / 2 ? 0 : all < most ? all : most;
 }
 
+static int cap_form(const rk_prompt_scores* s) { return !s || s->cap == 0.f ? kNoCap : s->cap <= kNearCapMost ? kNearCap : kFarCap; }
+using PromptKernel = void (*)(const PromptParams);
+template <int W> static PromptKernel prompt_cols_form(const rk_prompt_scores* s, bool slope) {
+    switch (cap_form(s)) {
+        case kNearCap: return slope ? prompt_cols_kernel<W, kNearCap, true> : prompt_cols_kernel<W, kNearCap, false>;
+        case kFarCap: return slope ? prompt_cols_kernel<W, kFarCap, true> : prompt_cols_kernel<W, kFarCap, false>;
+        default: return slope ? prompt_cols_kernel<W, kNoCap, true> : prompt_cols_kernel<W, kNoCap, false>;
+    }
+}
+static PromptKernel prompt_tile_form(const rk_prompt_scores* s, bool slope) {
+    switch (cap_form(s)) {
+        case kNearCap: return slope ? prompt_tile_kernel<1, kNearCap, true> : prompt_tile_kernel<1, kNearCap, false>;
+        case kFarCap: return slope ? prompt_tile_kernel<1, kFarCap, true> : prompt_tile_kernel<1, kFarCap, false>;
+        default: return slope ? prompt_tile_kernel<1, kNoCap, true> : prompt_tile_kernel<1, kNoCap, false>;
+    }
+}
+
 }  // namespace rk
 
 using namespace rk;
@@ -780,16 +812,10 @@ extern "C" int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stri
     }
     hipStream_t st = (hipStream_t)stream;
     if (plan.cols) {
-        constexpr int A = kColAlone;
-        auto kernel = plan.alone ? (cap ? (slope ? prompt_cols_kernel<A, true, true> : prompt_cols_kernel<A, true, false>)
-                                        : (slope ? prompt_cols_kernel<A, false, true> : prompt_cols_kernel<A, false, false>))
-                                 : (cap ? (slope ? prompt_cols_kernel<kColWaves, true, true> : prompt_cols_kernel<kColWaves, true, false>)
-                                        : (slope ? prompt_cols_kernel<kColWaves, false, true> : prompt_cols_kernel<kColWaves, false, false>));
-        hipLaunchKernelGGL(kernel, dim3(plan.splits, geom->n_kv_heads, geom->batch), dim3((plan.alone ? A : kColWaves) * 64), 0, st, p);
+        auto kernel = plan.alone ? prompt_cols_form<kColAlone>(scores, slope) : prompt_cols_form<kColWaves>(scores, slope);
+        hipLaunchKernelGGL(kernel, dim3(plan.splits, geom->n_kv_heads, geom->batch), dim3((plan.alone ? kColAlone : kColWaves) * 64), 0, st, p);
     } else {
-        auto kernel = plan.wide ? prompt_tile_kernel<2, false, false>
-                      : cap     ? (slope ? prompt_tile_kernel<1, true, true> : prompt_tile_kernel<1, true, false>)
-                                : (slope ? prompt_tile_kernel<1, false, true> : prompt_tile_kernel<1, false, false>);
+        auto kernel = plan.wide ? prompt_tile_kernel<2, kNoCap, false> : prompt_tile_form(scores, slope);
         const int64_t total = pairs * plan.row_tiles * plan.splits;
         // (Where all workgroups are there at once, two to a compute unit, the second ones come in the opposite order: the longest beside the
         // shortest.  8000 tokens of 8 heads 173 -> 165 us, 2048 of 32 over 8 53.0 -> 51.0, three capped chunks 70.3 -> 69.0.)
