@@ -49,10 +49,11 @@ __device__ __forceinline__ Query query_of(const PromptParams& p, const Tokens& t
     x.token = (uint32_t)row / (uint32_t)p.G;
     x.head = g * p.G + row - x.token * p.G;
     const int64_t pos = t.start + x.token;
-    x.pos = (int)pos;
+    x.pos = (int)max(pos, (int64_t)INT32_MIN);
     const int64_t at = (int64_t)b * p.n_new + x.token;
     x.lo = max(p.first != nullptr ? p.first[at] : 0, 0);
-    x.hi = (int)min((int64_t)t.len, p.end != nullptr ? (int64_t)p.end[at] : pos + 1);
+    // (a negative length less its tokens is below 32 bits: bounded before it is narrowed)
+    x.hi = (int)max(min((int64_t)t.len, p.end != nullptr ? (int64_t)p.end[at] : pos + 1), (int64_t)0);
     return x;
 }
 
