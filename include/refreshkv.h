@@ -659,7 +659,7 @@ typedef struct rk_kv8 {
 /* rk_rope_append into a cache of 8 bits.  New rows of a block that is not full go to the tail; a block that fills is quantised, the
  * rows that were there already being taken from the tail: with a its largest magnitude (of the bf16 rows, keys turned),
  *   scale = the smallest power of two, at least 2^-126, with a <= M * scale (M = 448 or 127);  1 for a block of zeros,
- *   k8 = k / scale (exact), rounded to the nearest value of the format, ties to even.
+ *   k8 = k / scale (exact, or too small to round to anything but 0), rounded to the nearest value of the format, ties to even.
  * A block with an infinity or a NaN gets a NaN as its scale (and zeros), so that whatever is computed from it is NaN.
  * The rows before the new ones must have been put there the same way: a sequence can be shortened and continued only within the
  * rows of the block that is not full. */

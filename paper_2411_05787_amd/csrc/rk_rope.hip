@@ -138,7 +138,7 @@ __device__ __forceinline__ int scale_exponent(uint32_t a, int format) {
     return max(e - (format == RK_Q8_E4M3 ? 8 : 6) + over, -126);
 }
 
-// Eight bf16 -> eight values of the format, x * inv exact.
+// Eight bf16 -> eight values of the format.  x * inv is exact, or beside a largest value near the end of the range below 2^-126, and rounds to 0 either way.
 template <int FORMAT>
 __device__ __forceinline__ uint2 quantise8(const u32x4 x, float inv) {
     uint32_t o[2];
@@ -220,7 +220,7 @@ __device__ __forceinline__ void append_block(const RopeParams& p, int b, int x, 
     top = max(max(sTop[0], sTop[1]), max(sTop[2], sTop[3]));
     const bool finite = top < 0x7f80u;
     const int e = top != 0 && finite ? scale_exponent(top, FORMAT) : 0;
-    const float inv = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : 0.f;      // 2^-e: e is -126 .. 121
+    const float inv = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : 0.f;      // 2^-e: e is -126 .. 122
     if (threadIdx.x == 0) {
         float* scales = (values ? p.c8.v_scale : p.c8.k_scale) + ((int64_t)b * p.Hkv + g) * (p.c8.capacity / blk);
         scales[number] = finite ? __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7fc00000u);
