@@ -818,6 +818,8 @@ class Kv8:
     def empty(cls, geom: Geom, capacity: int, block: int = 32, dtype=torch.float8_e4m3fn, device="cuda") -> "Kv8":
         """A cache with room for `capacity` rows (rounded up to whole blocks) and nothing in it."""
         B, H, D = geom.batch, geom.n_kv_heads, geom.head_dim
+        if capacity < 1 or block < 1 or dtype not in Q8_FORMATS:
+            raise ValueError("a capacity and a block of at least 1 and float8_e4m3fn or int8, got %s, %s, %s" % (capacity, block, dtype))
         cap = (int(capacity) + block - 1) // block * block
         new = lambda shape, t: torch.zeros(shape, dtype=t, device=device)  # noqa: E731
         return cls(geom, *(torch.zeros(B, H, cap, D, dtype=torch.uint8, device=device).view(dtype) for _ in range(2)),
