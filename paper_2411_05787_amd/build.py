@@ -18,8 +18,8 @@ HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",
                # the first scalar kernel arguments arrive in registers (see attn_split_kernel)
                "-mllvm", "-amdgpu-kernarg-preload-count=16",
                "-Wall", "-Wno-unused-function"]
-# Matrix instructions may leave their results in either half of the register file: a wavefront of rk_prompt's larger form holds 370 registers, and without this
-# all of them leave theirs in the half that other instructions do not reach (64 copies to a stage of 250 instructions).
+# Matrix instructions may leave their results in either half of the register file: a wavefront of rk_prompt's larger form holds 362 registers, and without this
+# all of them leave theirs in the half that other instructions do not reach (64 copies to a stage that has 218 instructions without them).
 SOURCE_FLAGS = {"rk_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

@@ -124,7 +124,8 @@ __device__ __forceinline__ float only_non_finite(float v) { return (__float_as_u
 // behind (O^T) are on the matrix cores, it makes weights of the scores between them, a matrix instruction and about five others to a slot.  K and V
 // come through LDS, whose rows are padded so that no two lanes of a read's phase meet in a bank: rings of 4 QB blocks, a barrier to QB stages. 8192
 // tokens, 32 heads over 8, QB = 2: 480-490 us, 1120-1145 TFLOP/s (a library matrix product of 8192^3 beside it 1390; with zeros for data, which
-// draw less power, 1320 and 1800).  Three capped chunks, QB = 1: 69 us, 480 TFLOP/s.  Without stages, two tiles of 64 rows in LDS and a barrier a
+// draw less power, 1320 and 1800).  Three capped chunks, QB = 1: 69 us, 480 TFLOP/s.  8192 tokens with a
+// bias or a cap of 50, QB = 1 too: 662 us, 507 plain beside them.  Without stages, two tiles of 64 rows in LDS and a barrier a
 // tile: 554 and 76 us. Instructions count: one wavefront on a SIMD issues one every five cycles or so (QB = 2: 218 to a stage, 32 of them
 // products).
 constexpr int kPromptRows = 128, kPromptTile = 64, kMaxSplits = 256;      // (cache rows are split over workgroups in tiles of two blocks)

@@ -14,9 +14,9 @@ typedef float Floats4 __attribute__((ext_vector_type(4), aligned(4)));
 struct Q8Rows { const uint8_t *k, *v; const float *ks, *vs; const uint16_t *kt, *vt; int64_t s_b; int32_t s_h, blocks, shift; };
 
 // Workgroups per (sequence, KV head): with the scores returned as the step over the bf16 cache has it, without them one to a compute unit, as
-// no stores come between the requests.  us by workgroups in all (256 / 512 / 768 / 1024), 32 heads over 8, e4m3: with weights 32777 rows 20.8 /
-// 21.3 / 22.2 / 23.9, 65536 35.5 / 35.4 / 35.8 / 34.2, 131072 70.3 / 68.0 / 66.9 / 60.7, without 65536 26.4 / 26.9 / 28.6 / 28.8, 4 sequences of
-// 32768 45.0 / 46.7 / 47.2 / 47.6, 16 ragged ones of up to 16384, 28 over 4, int8 36.2 / 35.6 / 35.7 / 38.9.
+// no stores come between the requests.  us by workgroups in all (256 / 512 / 768 / 1024), 32 heads over 8, e4m3: with weights 32777 rows 21.6 /
+// 21.6 / 22.3 / 24.0, 65536 36.4 / 35.7 / 36.2 / 34.2, 131072 70.4 / 68.5 / 67.3 / 60.8, without 65536 26.9 / 27.0 / 28.7 / 28.8, 4 sequences of
+// 32768 45.6 / 47.1 / 47.6 / 48.2, 16 ragged ones of up to 16384, 28 over 4, int8 37.8 / 35.6 / 36.1 / 38.6.
 static int q8_split_workgroups(const rk_geom* g, int32_t max_len, bool weights) {
     return split_workgroups(max_len, (int64_t)g->batch * g->n_kv_heads, kMaxChunks, weights ? emit_split_target(g, max_len) : kComputeUnits);
 }
