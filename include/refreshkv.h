@@ -620,7 +620,8 @@ typedef struct rk_new_rows {
  * Sequence b has n = new_lens[b] new tokens (new_lens: device int32[batch], clamped to [0, n_new]; NULL: n_new of each), entries 0 .. n-1
  * of its rows; entry i is row r = seq_lens[b] - n + i of the cache (seq_lens counts the new tokens), and its position is r, or
  * positions[b * n_new + i] where positions (device int32 [batch, n_new]) is given.
- *   q_out[b, i, h, :] = q turned           bf16 [batch, n_new, n_q_heads, 128] contiguous, 16-byte aligned; may be q itself
+ *   q_out[b, i, h, :] = q turned           bf16 [batch, n_new, n_q_heads, 128] contiguous, 16-byte aligned; may be q itself where
+ *                          that is contiguous too (RK_ERR_INVALID_ARG otherwise), and shares no memory with the rows in any other way
  *   cache.k[b, g, r, :] = k turned,  cache.v[b, g, r, :] = v
  * rope NULL: nothing is turned (q must be NULL then: it would be a copy).  Entries beyond n, and all other rows of the cache, are
  * left as they were; rows outside [0, cache.capacity) are not written (their q is). */

@@ -289,6 +289,12 @@ static int check_rope(const rk_geom* geom, const rk_new_rows* rows, const rk_rop
     return RK_OK;
 }
 
+// In place a row has to be written where it was read: elsewhere it would be another token's.
+static bool turned_over_others(const rk_geom* g, const rk_new_rows* rows, const void* q_out) {
+    const int64_t token = (int64_t)g->n_q_heads * kD;
+    return rows->q && rows->q == q_out && ((rows->n_new > 1 && rows->q_stride_t != token) || (g->batch > 1 && rows->q_stride_b != rows->n_new * token));
+}
+
 static RopeParams rope_params(const rk_geom* geom, const rk_new_rows* rows, const rk_rope* rope, const int32_t* positions,
                               const int32_t* seq_lens, const int32_t* new_lens, void* q_out, const int32_t* pred, int32_t pred_val) {
     RopeParams p{};
@@ -327,6 +333,7 @@ extern "C" int rk_rope_append(const rk_geom* geom, const rk_new_rows* rows, cons
     p.rows_per_token = (rows->q ? p.Hq : 0) + 2 * p.Hkv;
     const int64_t wgs = ((int64_t)p.n_new * p.rows_per_token + 31) / 32;
     if (wgs * 32 > INT32_MAX) return RK_ERR_UNSUPPORTED;
+    if (turned_over_others(geom, rows, q_out)) return RK_ERR_INVALID_ARG;
     hipLaunchKernelGGL(rope_append_kernel, dim3((unsigned)wgs, geom->batch), dim3(256), 0, (hipStream_t)stream, p);
     return launch_status();
 }
@@ -343,6 +350,7 @@ extern "C" int rk_rope_append_q8(const rk_geom* geom, const rk_new_rows* rows, c
     const int64_t blocks = ((int64_t)p.n_new + p.c8.block - 2) / p.c8.block + 1;       // that n_new rows can touch
     const int64_t block_wgs = blocks * 2 * p.Hkv, q_wgs = ((int64_t)p.n_new * p.rows_per_token + 31) / 32;
     if (block_wgs + q_wgs * 32 > INT32_MAX) return RK_ERR_UNSUPPORTED;
+    if (turned_over_others(geom, rows, q_out)) return RK_ERR_INVALID_ARG;
     p.block_wgs = (int32_t)block_wgs;
     const bool e4m3 = cache->format == RK_Q8_E4M3;
     auto kernel = cache->block == 128 ? (e4m3 ? rope_append_q8_kernel<RK_Q8_E4M3, 4> : rope_append_q8_kernel<RK_Q8_INT8, 4>)
