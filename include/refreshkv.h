@@ -33,6 +33,14 @@
  *   rk_prompt_attn      attention of a prompt, a chunk of one, drafted tokens or a single token over C_f, with capped scores,
  *                       a bias by distance, documents, prefixes and windows
  *
+ * and over a cache in pages:
+ *
+ *   rk_rope_append_paged, rk_paged_attn
+ *                       the append and the attention of new tokens
+ *   rk_prefix_attn      the same for a batch whose sequences share their first rows, which are read once
+ *   rk_page_scores, rk_page_select, rk_sparse_attn
+ *                       the pages that can score most for each token, and the attention over them
+ *
  * General rules
  * -------------
  * - Every tensor pointer is a DEVICE pointer owned by the caller; `stream` is a hipStream_t
@@ -724,6 +732,87 @@ int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64
                    const int32_t* seq_lens, const int32_t* new_lens, int32_t max_len, const rk_prompt_scores* scores,
                    void* out, float* lse, const int32_t* pred, int32_t pred_val,
                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- a cache in pages ----------------------------------------------------------------------- */
+
+/* A pool of pages, each with `page` rows of every KV head, for the sequences of any number of batches.  Row r of sequence b is row r % page of page
+ * table[b * table_width + r / page]; the calls below take the table (device int32 [batch, table_width]) beside the pool.  Sequences may name
+ * the same pages (a prefix that they share) as long as none is appended to.  A number outside [0, n_pages) names no page: rows there are not
+ * written, and nobody sees them.  Rows from table_width * page on do not exist.
+ *   k, v         bf16 [n_pages, n_kv_heads, page, 128], strides in elements (non-negative multiples of 8, below 2^40), 16-byte aligned
+ *   k_min, k_max bf16 [n_pages, n_kv_heads, 128] contiguous, 16-byte aligned, or both NULL: the least and the largest of a page's keys in each dim, in
+ *                the order -NaN < -infinity < .. < -0 < +0 < .. < +infinity < NaN (rk_rope_append_paged keeps them, rk_page_scores reads them)
+ *   page         16, 32, 64 or 128 (RK_ERR_UNSUPPORTED otherwise) */
+typedef struct rk_pages {
+    void* k;
+    void* v;
+    void* k_min;
+    void* k_max;
+    int64_t stride_p;
+    int64_t stride_h;
+    int32_t n_pages;
+    int32_t page;
+} rk_pages;
+
+/* rk_rope_append into pages.  Where the pool has bounds, those of every page that gets a row become the bounds of the rows that it then holds
+ * (of the sequence's rows in it, up to seq_lens[b]), so they are the same however many rows came at a time, and right when a sequence has been
+ * shortened and is continued. */
+int rk_rope_append_paged(const rk_geom* geom, const rk_new_rows* rows, const rk_rope* rope, const int32_t* positions,
+                         const rk_pages* pages, const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens,
+                         void* q_out, const int32_t* pred, int32_t pred_val, void* stream);
+
+/* rk_prompt_attn over a cache in pages: whole prompts, chunks, drafted tokens or a decode step's single token.  Arguments, results and workspace
+ * (rk_prompt_workspace_bytes) as there. */
+int rk_paged_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
+                  const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens, int32_t max_len,
+                  const rk_prompt_scores* scores, void* out, float* lse, const int32_t* pred, int32_t pred_val,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of scratch that rk_prefix_attn needs for up to n_new new tokens per sequence, a prefix of up to max_prefix rows and up to max_own rows of a
+ * sequence behind it (256-byte aligned device memory, as for rk_prompt_attn).  Host-only; 0: invalid. */
+size_t rk_prefix_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t max_prefix, int32_t max_own);
+
+/* rk_paged_attn for sequences that begin with the same rows (a system prompt, a document that all ask about), which are read once for the whole
+ * batch: rows j < P of every sequence are those of the pages prefix_table[0 .. prefix_width), rows from P on those of its own table, whose
+ * entries for whole pages before P are not looked at.  P = *prefix_len (device int32[1], clamped to [0, min(max_prefix, prefix_width * page)]; any number, also
+ * within a page).  seq_lens, positions, first and end count from the prefix's first row, as in rk_paged_attn; a sequence that is shorter than the
+ * prefix has its first rows.  max_prefix, max_own: host bounds of P and of seq_lens[b] - P (rows from P + max_own on are not seen). */
+int rk_prefix_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
+                   const int32_t* prefix_table, int32_t prefix_width, const int32_t* prefix_len, int32_t max_prefix,
+                   const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens, int32_t max_own,
+                   const rk_prompt_scores* scores, void* out, float* lse, const int32_t* pred, int32_t pred_val,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* What a token's scores can reach in each page, out of the page's bounds (512 bytes of a page and KV head instead of its keys): for token i of
+ * sequence b at position p = seq_lens[b] - n + i >= 0 (tokens as in rk_prompt_attn), KV head g and the pages j <= p / page, j < min(table_width, s_stride),
+ *     scores[b,i,g,j] = agg over the heads h of g of  scale * sum_d (max(q_d, 0) * k_max_d + min(q_d, 0) * k_min_d)
+ * with q = q[b,i,h,:] and the bounds of page table[b][j]: where scale >= 0 no row of the page scores more with head h.  Sums in fp32; a bound that is infinite or no
+ * number makes a score that is +infinity or no number.  A page that the pool does not have: -infinity.  Other entries are left as they were.
+ *   agg     RK_AGG_MAX, RK_AGG_MEAN or RK_AGG_FIRST, as in rk_topk_select
+ *   scores  fp32 [batch, n_new, n_kv_heads, s_stride] */
+int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
+                   const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens, int32_t agg,
+                   float* scores, int64_t s_stride, const int32_t* pred, int32_t pred_val, void* stream);
+
+/* The pages that a token reads: of the N = min(p / page + 1, s_stride) pages of token i (none: N = 0) those with the k largest scores, for every KV
+ * head; equal ones, and the last places, to the lower page.  The first keep_first pages and the last keep_last (of p / page + 1: the token's own page is the last)
+ * count as +infinity, and so does a score that is no number.  idx int32 [batch, n_new, n_kv_heads, k]: min(k, N) page numbers within the sequence in
+ * ascending order, then -1.  Entries of tokens that there are not are left as they were. */
+int rk_page_select(const rk_geom* geom, const float* scores, int64_t s_stride, int32_t n_new, int32_t page, const int32_t* seq_lens,
+                   const int32_t* new_lens, int32_t k, int32_t keep_first, int32_t keep_last, int32_t* idx,
+                   const int32_t* pred, int32_t pred_val, void* stream);
+
+/* Bytes of scratch that rk_sparse_attn needs for up to n_new new tokens per sequence and k pages of `page` rows (as for rk_prompt_attn).
+ * Host-only; 0: invalid. */
+size_t rk_sparse_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t k, int32_t page);
+
+/* Attention of each new token over some pages of its sequence, its own for every KV head: rk_paged_attn in which the query heads of KV head g see, of
+ * the rows that token i sees, those in the pages idx[b,i,g,0 .. k) (numbers within the sequence, as rk_page_select leaves them, in any order; a
+ * number outside [0, table_width): no page; one that is there twice counts twice). */
+int rk_sparse_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
+                   const int32_t* table, int32_t table_width, const int32_t* idx, int32_t k,
+                   const int32_t* seq_lens, const int32_t* new_lens, const rk_prompt_scores* scores, void* out, float* lse,
+                   const int32_t* pred, int32_t pred_val, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,9 @@ EXPORTS = ["rk_version", "rk_status_string", "rk_workspace_bytes", "rk_workspace
            "rk_full_attn", "rk_full_attn_scores", "rk_topk_select", "rk_full_attn_select", "rk_full_attn_pool", "rk_full_attn_deferred", "rk_select_pooled", "rk_score_select", "rk_window_select", "rk_gather_small_kv", "rk_partial_attn", "rk_partial_attn_static", "rk_partial_attn_static_bytes", "rk_partial_attn_fixed", "rk_partial_attn_lazy", "rk_gather_attn", "rk_partial_attn_triggered", "rk_decode_step", "rk_decode_step_overlapped", "rk_refresh_batched", "rk_decode_step_batched",
            "rk_query_sim", "rk_mark_refresh", "rk_calibration_copy", "rk_calibration_read", "rk_debug_set_slice_spin", "rk_h2o_append", "rk_h2o_update", "rk_h2o_step",
            "rk_rope_table", "rk_rope_append", "rk_rope_append_q8", "rk_full_attn_q8", "rk_gather_small_kv_q8",
-           "rk_prompt_workspace_bytes", "rk_prompt_attn"]
+           "rk_prompt_workspace_bytes", "rk_prompt_attn",
+           "rk_rope_append_paged", "rk_paged_attn", "rk_prefix_workspace_bytes", "rk_prefix_attn", "rk_page_scores", "rk_page_select",
+           "rk_sparse_workspace_bytes", "rk_sparse_attn"]
 
 RK_AGG_MAX, RK_AGG_MEAN, RK_AGG_FIRST = 0, 1, 2
 
@@ -85,6 +87,11 @@ class _Kv8(C.Structure):
 
 class _PromptScores(C.Structure):
     _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("first", C.c_void_p), ("end", C.c_void_p)]
+
+
+class _Pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_min", C.c_void_p), ("k_max", C.c_void_p), ("stride_p", C.c_int64),
+                ("stride_h", C.c_int64), ("n_pages", C.c_int32), ("page", C.c_int32)]
 
 
 STEP_KINDS = {1: "full", 2: "partial", 3: "both"}
@@ -180,6 +187,23 @@ def _load(path: str = LIB_PATH) -> C.CDLL:
     l.rk_prompt_workspace_bytes.argtypes = [G, I32, I32]
     l.rk_prompt_attn.argtypes = [G, P, I64, I64, I32, _Kv, P, P, I32, C.POINTER(_PromptScores), P, P, P, I32, P, SZ, P]
     l.rk_prompt_attn.restype = C.c_int
+    PG, SC = C.POINTER(_Pages), C.POINTER(_PromptScores)
+    l.rk_rope_append_paged.argtypes = [G, C.POINTER(_NewRows), C.POINTER(_Rope), P, PG, P, I32, P, P, P, P, I32, P]
+    l.rk_rope_append_paged.restype = C.c_int
+    l.rk_paged_attn.argtypes = [G, P, I64, I64, I32, PG, P, I32, P, P, I32, SC, P, P, P, I32, P, SZ, P]
+    l.rk_paged_attn.restype = C.c_int
+    l.rk_prefix_workspace_bytes.argtypes = [G, I32, I32, I32]
+    l.rk_prefix_workspace_bytes.restype = SZ
+    l.rk_prefix_attn.argtypes = [G, P, I64, I64, I32, PG, P, I32, P, I32, P, I32, P, P, I32, SC, P, P, P, I32, P, SZ, P]
+    l.rk_prefix_attn.restype = C.c_int
+    l.rk_page_scores.argtypes = [G, P, I64, I64, I32, PG, P, I32, P, P, I32, P, I64, P, I32, P]
+    l.rk_page_scores.restype = C.c_int
+    l.rk_page_select.argtypes = [G, P, I64, I32, I32, P, P, I32, I32, I32, P, P, I32, P]
+    l.rk_page_select.restype = C.c_int
+    l.rk_sparse_workspace_bytes.argtypes = [G, I32, I32, I32]
+    l.rk_sparse_workspace_bytes.restype = SZ
+    l.rk_sparse_attn.argtypes = [G, P, I64, I64, I32, PG, P, I32, P, I32, P, P, SC, P, P, P, I32, P, SZ, P]
+    l.rk_sparse_attn.restype = C.c_int
     return l
 
 
@@ -192,6 +216,7 @@ except ImportError as _e:                  # not built (build.py), or for anothe
         """Takes no call: None sends each through the checks below."""
         setup = rk_partial_attn = rk_partial_attn_fixed = rk_gather_small_kv = rk_h2o_step = rk_full_attn = staticmethod(lambda *a: None)
         rk_rope_append = rk_rope_append_q8 = rk_full_attn_q8 = rk_gather_small_kv_q8 = rk_prompt_attn = setup
+        rk_rope_append_paged = rk_paged_attn = rk_prefix_attn = rk_page_scores = rk_page_select = rk_sparse_attn = setup
 
     warnings.warn("short calls are marshalled in Python and take the host about 4 us more: %s" % _e, RuntimeWarning)
 
@@ -290,7 +315,7 @@ def _stream(stream) -> int:
     return int(stream)
 
 
-_native.setup(_stream, _raw_stream, _device, _Geom, _H2oState, _Rope, _Kv8)
+_native.setup(_stream, _raw_stream, _device, _Geom, _H2oState, _Rope, _Kv8, _Pages)
 
 
 def workspace_bytes(geom: Geom, max_len: int, max_k: int) -> int:
@@ -987,3 +1012,207 @@ def rk_prompt_attn(geom: Geom, q, K, V, seq_lens, max_len: int, out, new_lens=No
             _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(max_len),
             C.byref(scores), _dev(out, torch.bfloat16, "out", (B, T, Hq, D)), _dev(lse, torch.float32, "lse", (B, T, Hq), optional=True),
             _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val), ws, nb)
+
+
+# ---- a cache in pages ----
+
+class Pages:
+    """A pool of pages (rk_pages): k, v bf16 [n_pages, Hkv, page, 128], rows contiguous; k_min, k_max bf16 [n_pages, Hkv, 128] or None.  The pages of
+    a sequence are a row of the table that every call takes, int32 [batch, pages of the longest sequence]."""
+
+    def __init__(self, k, v, k_min=None, k_max=None):
+        for t, n in ((k, "k"), (v, "v")):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.bfloat16:
+                raise ValueError("%s must be a bf16 tensor in GPU memory" % n)
+            if t.dim() != 4:
+                raise ValueError("%s must be [n_pages, n_kv_heads, page, head_dim], got %s" % (n, tuple(t.shape)))
+            if t.stride(3) != 1 or t.stride(2) != t.shape[3]:
+                raise ValueError("%s rows must be contiguous" % n)
+        if k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError("k and v must share shape and strides")
+        if (k_min is None) != (k_max is None):
+            raise ValueError("k_min and k_max go together")
+        n, H, page, D = k.shape
+        if n < 1 or n > 2 ** 31 - 1:
+            raise ValueError("a pool has between 1 and 2^31 - 1 pages, got %d" % n)
+        self.k, self.v, self.k_min, self.k_max = k, v, k_min, k_max
+        self.n_pages, self.n_kv_heads, self.page, self.head_dim = n, H, page, D
+        self._c = _Pages(k.data_ptr(), v.data_ptr(), _dev(k_min, torch.bfloat16, "k_min", (n, H, D), optional=True),
+                         _dev(k_max, torch.bfloat16, "k_max", (n, H, D), optional=True), k.stride(0), k.stride(1), n, page)
+        self.device_index = _same_device(k, v, k_min, k_max).index
+
+    @classmethod
+    def empty(cls, geom: Geom, n_pages: int, page: int = 32, bounds: bool = True, device="cuda") -> "Pages":
+        """A pool of n_pages pages, with bounds of their keys or without."""
+        if n_pages < 1 or page not in (16, 32, 64, 128):
+            raise ValueError("at least one page of 16, 32, 64 or 128 rows, got %s of %s" % (n_pages, page))
+        new = lambda *shape: torch.zeros(*shape, dtype=torch.bfloat16, device=device)  # noqa: E731
+        H, D = geom.n_kv_heads, geom.head_dim
+        return cls(new(n_pages, H, page, D), new(n_pages, H, page, D), *((new(n_pages, H, D), new(n_pages, H, D)) if bounds else ()))
+
+
+def _pool(geom: Geom, pages: Pages) -> torch.Tensor:
+    """One tensor of the pool, once it is known to be of this geometry."""
+    if not isinstance(pages, Pages):
+        raise ValueError("pages must be a Pages")
+    if (pages.n_kv_heads, pages.head_dim) != (geom.n_kv_heads, geom.head_dim):
+        raise ValueError("the pool is of another geometry")
+    return pages.k
+
+
+def _page_table(table, B: int, name: str = "table") -> tuple:
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("%s must be [batch, pages of a sequence]" % name)
+    return _dev(table, torch.int32, name), table.shape[1]
+
+
+def _queries(geom: Geom, q) -> tuple:
+    """Pointer, strides and tokens of q [B, T, Hq, D]."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be [batch, n_new, n_q_heads, head_dim]")
+    p, sb, st = _rows(q, geom.batch, q.shape[1], geom.n_q_heads, geom.head_dim, "q")
+    return p, sb, st, q.shape[1]
+
+
+def rk_rope_append_paged(geom: Geom, q, k, v, rope: Optional[Rope], pages: Pages, table, seq_lens, q_out, new_lens=None, positions=None,
+                         pred=None, pred_val: int = 0, stream=None) -> None:
+    """rk_rope_append into pages: table int32 [B, W]."""
+    rc = _native.rk_rope_append_paged(geom, q, k, v, rope, pages, table, seq_lens, q_out, new_lens, positions, pred, pred_val, stream)
+    if rc is not None:
+        return _check("rk_rope_append_paged", rc)
+    rows, r, pos, lens, new, qo = _new_rows(geom, q, k, v, rope, positions, seq_lens, new_lens, q_out)
+    dev = _same_device(k, q, v, None if rope is None else rope.table, _pool(geom, pages), table, seq_lens, q_out, new_lens, positions, pred)
+    tp, width = _page_table(table, geom.batch)
+    _launch("rk_rope_append_paged", dev, stream, C.byref(geom.c()), rows, r, pos, C.byref(pages._c), tp, width, lens, new, qo,
+            _dev(pred, torch.int32, "pred", (geom.batch,), optional=True), int(pred_val))
+
+
+class PrefixWorkspace:
+    """Scratch of rk_prefix_attn for up to n_new new tokens per sequence, a prefix of max_prefix rows and max_own rows behind it; nothing in it
+    outlives a call."""
+
+    def __init__(self, geom: Geom, n_new: int, max_prefix: int, max_own: int, device="cuda"):
+        self.geom, self.n_new, self.max_prefix, self.max_own = geom, int(n_new), int(max_prefix), int(max_own)
+        _scratch(self, "rk_prefix_workspace_bytes", (n_new, max_prefix, max_own), device)
+
+
+class SparseWorkspace:
+    """Scratch of rk_sparse_attn for up to n_new new tokens per sequence and k pages of `page` rows; nothing in it outlives a call."""
+
+    def __init__(self, geom: Geom, n_new: int, k: int, page: int, device="cuda"):
+        self.geom, self.n_new, self.k, self.page = geom, int(n_new), int(k), int(page)
+        _scratch(self, "rk_sparse_workspace_bytes", (n_new, k, page), device)
+
+
+def _scratch(ws, name: str, sizes: tuple, device) -> None:
+    ws.nbytes = int(getattr(lib, name)(C.byref(ws.geom.c()), *(int(x) for x in sizes)))
+    if ws.nbytes == 0:
+        raise RkError(name, -1)
+    ws.buf = torch.empty(ws.nbytes + 256, dtype=torch.uint8, device=device)
+    ws.device_index = ws.buf.device.index
+    ws.ptr = (ws.buf.data_ptr() + 255) // 256 * 256
+
+
+def _attention_rest(geom: Geom, T: int, first, end, cap, slopes, out, lse, pred, pred_val, workspace) -> tuple:
+    """The arguments that the attentions over pages end with, from the scores on."""
+    B, Hq, D = geom.batch, geom.n_q_heads, geom.head_dim
+    scores = _PromptScores(float(cap), _dev(slopes, torch.float32, "slopes", (Hq,), optional=True),
+                           _dev(first, torch.int32, "first", (B, T), optional=True), _dev(end, torch.int32, "end", (B, T), optional=True))
+    ws, nb = (None, 0) if workspace is None else (workspace.ptr, workspace.nbytes)
+    return (C.byref(scores), _dev(out, torch.bfloat16, "out", (B, T, Hq, D)), _dev(lse, torch.float32, "lse", (B, T, Hq), optional=True),
+            _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val), ws, nb)
+
+
+def rk_paged_attn(geom: Geom, q, pages: Pages, table, seq_lens, max_len: int, out, new_lens=None, first=None, end=None, cap: float = 0.0,
+                  slopes=None, lse=None, pred=None, pred_val: int = 0, workspace: PromptWorkspace = None, stream=None) -> None:
+    """rk_prompt_attn over a cache in pages: table int32 [B, W]."""
+    rc = _native.rk_paged_attn(geom, q, pages, table, seq_lens, max_len, out, new_lens, first, end, cap, slopes, lse, pred, pred_val, workspace, stream)
+    if rc is not None:
+        return _check("rk_paged_attn", rc)
+    B = geom.batch
+    dev = _same_device(_pool(geom, pages), q, table, seq_lens, out, new_lens, first, end, slopes, lse, pred, None if workspace is None else workspace.buf)
+    qp, sb, st, T = _queries(geom, q)
+    tp, width = _page_table(table, B)
+    if max_len > width * pages.page:
+        raise ValueError("max_len %d exceeds the table's %d pages of %d rows" % (max_len, width, pages.page))
+    _launch("rk_paged_attn", dev, stream, C.byref(geom.c()), qp, sb, st, T, C.byref(pages._c), tp, width,
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(max_len),
+            *_attention_rest(geom, T, first, end, cap, slopes, out, lse, pred, pred_val, workspace))
+
+
+def rk_prefix_attn(geom: Geom, q, pages: Pages, prefix_table, prefix_len, max_prefix: int, table, seq_lens, max_own: int, out, new_lens=None,
+                   first=None, end=None, cap: float = 0.0, slopes=None, lse=None, pred=None, pred_val: int = 0,
+                   workspace: PrefixWorkspace = None, stream=None) -> None:
+    """rk_paged_attn for sequences that share their first rows: prefix_table int32 [W'], prefix_len int32 [1]."""
+    rc = _native.rk_prefix_attn(geom, q, pages, prefix_table, prefix_len, max_prefix, table, seq_lens, max_own, out, new_lens, first, end, cap, slopes, lse,
+                                pred, pred_val, workspace, stream)
+    if rc is not None:
+        return _check("rk_prefix_attn", rc)
+    B = geom.batch
+    if workspace is None:
+        raise ValueError("a workspace is required")
+    dev = _same_device(_pool(geom, pages), q, prefix_table, prefix_len, table, seq_lens, out, new_lens, first, end, slopes, lse, pred, workspace.buf)
+    qp, sb, st, T = _queries(geom, q)
+    tp, width = _page_table(table, B)
+    if prefix_table.dim() != 1:
+        raise ValueError("prefix_table must be [pages of the prefix]")
+    if max_prefix > prefix_table.shape[0] * pages.page:
+        raise ValueError("max_prefix %d exceeds the prefix's %d pages of %d rows" % (max_prefix, prefix_table.shape[0], pages.page))
+    _launch("rk_prefix_attn", dev, stream, C.byref(geom.c()), qp, sb, st, T, C.byref(pages._c), _dev(prefix_table, torch.int32, "prefix_table"),
+            prefix_table.shape[0], _dev(prefix_len, torch.int32, "prefix_len", (1,)), int(max_prefix), tp, width,
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(max_own),
+            *_attention_rest(geom, T, first, end, cap, slopes, out, lse, pred, pred_val, workspace))
+
+
+def rk_page_scores(geom: Geom, q, pages: Pages, table, seq_lens, scores, new_lens=None, agg: int = RK_AGG_MAX, pred=None, pred_val: int = 0,
+                   stream=None) -> None:
+    """q bf16 [B, T, Hq, D] as in rk_paged_attn; scores fp32 [B, T, Hkv, pages]."""
+    rc = _native.rk_page_scores(geom, q, pages, table, seq_lens, scores, new_lens, agg, pred, pred_val, stream)
+    if rc is not None:
+        return _check("rk_page_scores", rc)
+    B, H = geom.batch, geom.n_kv_heads
+    dev = _same_device(_pool(geom, pages), q, table, seq_lens, scores, new_lens, pred)
+    if pages.k_min is None:
+        raise ValueError("the pool keeps no bounds of its pages")
+    qp, sb, st, T = _queries(geom, q)
+    tp, width = _page_table(table, B)
+    if scores.dim() != 4:
+        raise ValueError("scores must be [batch, n_new, n_kv_heads, pages]")
+    _launch("rk_page_scores", dev, stream, C.byref(geom.c()), qp, sb, st, T, C.byref(pages._c), tp, width,
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(agg),
+            _dev(scores, torch.float32, "scores", (B, T, H, scores.shape[3])), scores.shape[3],
+            _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val))
+
+
+def rk_page_select(geom: Geom, scores, page: int, seq_lens, k: int, idx, new_lens=None, keep_first: int = 0, keep_last: int = 1, pred=None,
+                   pred_val: int = 0, stream=None) -> None:
+    """scores fp32 [B, T, Hkv, pages] (rk_page_scores), pages of `page` rows; idx int32 [B, T, Hkv, k]."""
+    rc = _native.rk_page_select(geom, scores, page, seq_lens, k, idx, new_lens, keep_first, keep_last, pred, pred_val, stream)
+    if rc is not None:
+        return _check("rk_page_select", rc)
+    B, H = geom.batch, geom.n_kv_heads
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 4:
+        raise ValueError("scores must be [batch, n_new, n_kv_heads, pages]")
+    dev = _same_device(scores, seq_lens, idx, new_lens, pred)
+    T, width = scores.shape[1], scores.shape[3]
+    _launch("rk_page_select", dev, stream, C.byref(geom.c()), _dev(scores, torch.float32, "scores", (B, T, H, width)), width, T, int(page),
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(k), int(keep_first),
+            int(keep_last), _dev(idx, torch.int32, "idx", (B, T, H, k)), _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val))
+
+
+def rk_sparse_attn(geom: Geom, q, pages: Pages, table, idx, seq_lens, out, new_lens=None, first=None, end=None, cap: float = 0.0, slopes=None,
+                   lse=None, pred=None, pred_val: int = 0, workspace: SparseWorkspace = None, stream=None) -> None:
+    """rk_paged_attn over the pages idx int32 [B, T, Hkv, k] (rk_page_select)."""
+    rc = _native.rk_sparse_attn(geom, q, pages, table, idx, seq_lens, out, new_lens, first, end, cap, slopes, lse, pred, pred_val, workspace, stream)
+    if rc is not None:
+        return _check("rk_sparse_attn", rc)
+    B = geom.batch
+    dev = _same_device(_pool(geom, pages), q, table, idx, seq_lens, out, new_lens, first, end, slopes, lse, pred, None if workspace is None else workspace.buf)
+    qp, sb, st, T = _queries(geom, q)
+    tp, width = _page_table(table, B)
+    if idx.dim() != 4:
+        raise ValueError("idx must be [batch, n_new, n_kv_heads, k]")
+    _launch("rk_sparse_attn", dev, stream, C.byref(geom.c()), qp, sb, st, T, C.byref(pages._c), tp, width,
+            _dev(idx, torch.int32, "idx", (B, T, geom.n_kv_heads, idx.shape[3])), idx.shape[3],
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True),
+            *_attention_rest(geom, T, first, end, cap, slopes, out, lse, pred, pred_val, workspace))

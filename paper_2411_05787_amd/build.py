@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librefreshkv.so")
 BIND = os.path.join(HERE, "_rkbind.so")               # argument marshalling of the short calls (csrc/rk_bind.cpp), linked against LIB
 SOURCES = ["rk_api.hip", "rk_attn.hip", "rk_partial.hip", "rk_topk.hip", "rk_gather.hip", "rk_query_sim.hip", "rk_step.hip",
-           "rk_window.hip", "rk_h2o.hip", "rk_rope.hip", "rk_q8.hip", "rk_prompt.hip"]
+           "rk_window.hip", "rk_h2o.hip", "rk_rope.hip", "rk_q8.hip", "rk_prompt.hip", "rk_paged.hip", "rk_pages.hip"]
 # Packed fp32 VALU forms are switched off for every device compilation of this library.
 HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -20,7 +20,7 @@ HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",
                "-Wall", "-Wno-unused-function"]
 # Matrix instructions may leave their results in either half of the register file: a wavefront of rk_prompt's larger form holds 362 registers, and without this
 # all of them leave theirs in the half that other instructions do not reach (64 copies to a stage that has 218 instructions without them).
-SOURCE_FLAGS = {"rk_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+SOURCE_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("rk_prompt.hip", "rk_paged.hip")}
 
 
 def hipcc() -> str:

@@ -19,8 +19,8 @@ namespace {
 
 // binding.py's _stream, and the two functions of torch that give the current stream's handle (None where torch lacks them).
 PyObject *g_stream, *g_raw_stream, *g_device;
-// The ctypes classes of rk_geom, rk_h2o_state, rk_rope and rk_kv8: what is of another class is binding.py's to refuse.
-PyObject *g_geom, *g_h2o_state, *g_rope, *g_kv8;
+// The ctypes classes of rk_geom, rk_h2o_state, rk_rope, rk_kv8 and rk_pages: what is of another class is binding.py's to refuse.
+PyObject *g_geom, *g_h2o_state, *g_rope, *g_kv8, *g_pages;
 
 // One call's arguments: `ok` until one of them is not the common case's.
 struct Args {
@@ -94,7 +94,7 @@ struct Args {
         if (!ok) return {};
         return {t->data_ptr(), geom.batch > 1 ? t->stride(0) : 0, T > 1 ? t->stride(1) : 0};
     }
-    // The C structure that an object of binding.py (Rope, Kv8) keeps, and the device of what it points at.
+    // The C structure that an object of binding.py (Rope, Kv8, Pages) keeps, and the device of what it points at.
     template <class T> T held(int i, PyObject* type) {
         static PyObject *const name = PyUnicode_InternFromString("_c"), *const dev = PyUnicode_InternFromString("device_index");
         PyObject* c = ok ? PyObject_GetAttr(a[i], name) : nullptr;
@@ -112,6 +112,35 @@ struct Args {
         if (!g) PyErr_Clear();
         Py_XDECREF(g);
         return s;
+    }
+    rk_pages pool(int i) {                    // (of this geometry's heads)
+        static PyObject *const heads = PyUnicode_InternFromString("n_kv_heads"), *const dim = PyUnicode_InternFromString("head_dim");
+        const rk_pages s = held<rk_pages>(i, g_pages);
+        if ((int64_t)attribute(a[i], heads) != geom.n_kv_heads || (int64_t)attribute(a[i], dim) != geom.head_dim) ok = false;
+        return s;
+    }
+    // int32 [batch, width].
+    struct Table { const int32_t* ptr; int32_t width; };
+    Table table(int i) {
+        const at::Tensor* t = tensor(i);
+        if (!t || t->dim() != 2 || t->size(1) > INT32_MAX) { ok = false; return {}; }
+        const int64_t width = t->size(1);
+        return {(const int32_t*)dev(i, at::kInt, {geom.batch, width}), (int32_t)width};
+    }
+    // first, end, cap, slopes of an attention of T new tokens
+    rk_prompt_scores scores(int first, int end, int cap, int slopes, int64_t T) {
+        rk_prompt_scores s{};
+        if (!ok || !PyFloat_CheckExact(a[cap])) { ok = false; return s; }
+        s.cap = (float)PyFloat_AS_DOUBLE(a[cap]);
+        s.first = (const int32_t*)dev_or_null(first, at::kInt, {geom.batch, T});
+        s.end = (const int32_t*)dev_or_null(end, at::kInt, {geom.batch, T});
+        s.slopes = (const float*)dev_or_null(slopes, at::kFloat, {geom.n_q_heads});
+        return s;
+    }
+    int64_t tokens(int i) {                   // of q [B, T, Hq, D]
+        const at::Tensor* t = tensor(i);
+        if (!t || t->dim() != 4 || t->size(1) > INT32_MAX) { ok = false; return 0; }
+        return t->size(1);
     }
     struct Scratch { void* ptr; size_t bytes; };
     Scratch workspace(int i) {
@@ -263,10 +292,12 @@ PyObject* full_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// geom, q, k, v, rope, K, V, seq_lens, q_out, new_lens, positions, pred, pred_val, stream; with one cache of 8 bits for K and V: Q8
-template <bool Q8>
+// geom, q, k, v, rope, K, V, seq_lens, q_out, new_lens, positions, pred, pred_val, stream; with one cache of 8 bits for K and V: 1; with
+// pages and their table: 2
+template <int INTO>
 PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return with_args(a, n, Q8 ? 13 : 14, [](Args& x) -> PyObject* {
+    return with_args(a, n, INTO == 1 ? 13 : 14, [](Args& x) -> PyObject* {
+        constexpr bool Q8 = INTO == 1;
         constexpr int o = Q8 ? 6 : 7;         // seq_lens
         const rk_geom& g = x.geom;
         const at::Tensor* k = x.tensor(2);
@@ -280,7 +311,10 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const rk_rope rope = turned ? x.held<rk_rope>(4, g_rope) : rk_rope{};
         rk_kv kv{};
         rk_kv8 c8{};
-        if (Q8) c8 = x.cache8(5);
+        rk_pages pages{};
+        Args::Table table{};
+        if (INTO == 2) { pages = x.pool(5); table = x.table(6); }
+        else if (Q8) c8 = x.cache8(5);
         else kv = x.kv(5, 6, 0);
         auto* lens = (const int32_t*)x.dev(o, i32t, {g.batch});
         void* q_out = x.dev_or_null(o + 1, bf16, {g.batch, T, g.n_q_heads, g.head_dim});
@@ -291,6 +325,7 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* st = x.stream_here(o + 6);
         if (!x.ok) return nullptr;
         return status_of([&] {
+            if (INTO == 2) return rk_rope_append_paged(&g, &rows, turned ? &rope : nullptr, pos, &pages, table.ptr, table.width, lens, new_lens, q_out, pred, pred_val, st);
             return Q8 ? rk_rope_append_q8(&g, &rows, turned ? &rope : nullptr, pos, &c8, lens, new_lens, q_out, pred, pred_val, st)
                       : rk_rope_append(&g, &rows, turned ? &rope : nullptr, pos, kv, lens, new_lens, q_out, pred, pred_val, st);
         });
@@ -367,10 +402,139 @@ PyObject* prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// geom, q, pages, table, seq_lens, max_len, out, new_lens, first, end, cap, slopes, lse, pred, pred_val, workspace, stream
+PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return with_args(a, n, 17, [](Args& x) -> PyObject* {
+        const rk_geom& g = x.geom;
+        const int64_t T = x.tokens(1);
+        if (!x.ok) return nullptr;
+        const Args::Rows q = x.rows(1, T, g.n_q_heads);
+        const rk_pages pages = x.pool(2);
+        const Args::Table table = x.table(3);
+        auto* lens = (const int32_t*)x.dev(4, i32t, {g.batch});
+        const int32_t max_len = x.i32(5), pred_val = x.i32(14);
+        void* out = x.dev(6, bf16, {g.batch, T, g.n_q_heads, g.head_dim});
+        auto* new_lens = (const int32_t*)x.dev_or_null(7, i32t, {g.batch});
+        const rk_prompt_scores s = x.scores(8, 9, 10, 11, T);
+        auto* lse = (float*)x.dev_or_null(12, f32, {g.batch, T, g.n_q_heads});
+        auto* pred = (const int32_t*)x.dev_or_null(13, i32t, {g.batch});
+        const Args::Scratch ws = x.a[15] == Py_None ? Args::Scratch{nullptr, 0} : x.workspace_here(15);
+        void* st = x.stream_here(16);
+        if (!x.ok || max_len > (int64_t)table.width * pages.page) return nullptr;
+        return status_of([&] {
+            return rk_paged_attn(&g, q.ptr, q.b, q.t, (int32_t)T, &pages, table.ptr, table.width, lens, new_lens, max_len, &s, out, lse, pred, pred_val,
+                                 ws.ptr, ws.bytes, st);
+        });
+    });
+}
+
+// geom, q, pages, prefix_table, prefix_len, max_prefix, table, seq_lens, max_own, out, new_lens, first, end, cap, slopes, lse, pred, pred_val,
+// workspace, stream
+PyObject* prefix_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return with_args(a, n, 20, [](Args& x) -> PyObject* {
+        const rk_geom& g = x.geom;
+        const int64_t T = x.tokens(1);
+        const at::Tensor* pt = x.tensor(3);
+        if (!x.ok || pt->dim() != 1 || pt->size(0) > INT32_MAX) return nullptr;
+        const Args::Rows q = x.rows(1, T, g.n_q_heads);
+        const rk_pages pages = x.pool(2);
+        const int64_t width = pt->size(0);
+        auto* prefix = (const int32_t*)x.dev(3, i32t, {width});
+        auto* prefix_len = (const int32_t*)x.dev(4, i32t, {1});
+        const int32_t max_prefix = x.i32(5), max_own = x.i32(8), pred_val = x.i32(17);
+        const Args::Table table = x.table(6);
+        auto* lens = (const int32_t*)x.dev(7, i32t, {g.batch});
+        void* out = x.dev(9, bf16, {g.batch, T, g.n_q_heads, g.head_dim});
+        auto* new_lens = (const int32_t*)x.dev_or_null(10, i32t, {g.batch});
+        const rk_prompt_scores s = x.scores(11, 12, 13, 14, T);
+        auto* lse = (float*)x.dev_or_null(15, f32, {g.batch, T, g.n_q_heads});
+        auto* pred = (const int32_t*)x.dev_or_null(16, i32t, {g.batch});
+        const Args::Scratch ws = x.workspace_here(18);
+        void* st = x.stream_here(19);
+        if (!x.ok || max_prefix > width * pages.page) return nullptr;
+        return status_of([&] {
+            return rk_prefix_attn(&g, q.ptr, q.b, q.t, (int32_t)T, &pages, prefix, (int32_t)width, prefix_len, max_prefix, table.ptr, table.width, lens,
+                                  new_lens, max_own, &s, out, lse, pred, pred_val, ws.ptr, ws.bytes, st);
+        });
+    });
+}
+
+// geom, q, pages, table, seq_lens, scores, new_lens, agg, pred, pred_val, stream
+PyObject* page_scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return with_args(a, n, 11, [](Args& x) -> PyObject* {
+        const rk_geom& g = x.geom;
+        const int64_t T = x.tokens(1);
+        const at::Tensor* sc = x.tensor(5);
+        if (!x.ok || sc->dim() != 4) return nullptr;
+        const Args::Rows q = x.rows(1, T, g.n_q_heads);
+        const rk_pages pages = x.pool(2);
+        const Args::Table table = x.table(3);
+        auto* lens = (const int32_t*)x.dev(4, i32t, {g.batch});
+        const int64_t width = sc->size(3);
+        auto* scores = (float*)x.dev(5, f32, {g.batch, T, g.n_kv_heads, width});
+        auto* new_lens = (const int32_t*)x.dev_or_null(6, i32t, {g.batch});
+        const int32_t agg = x.i32(7), pred_val = x.i32(9);
+        auto* pred = (const int32_t*)x.dev_or_null(8, i32t, {g.batch});
+        void* st = x.stream_here(10);
+        if (!x.ok || !pages.k_min) return nullptr;
+        return status_of([&] {
+            return rk_page_scores(&g, q.ptr, q.b, q.t, (int32_t)T, &pages, table.ptr, table.width, lens, new_lens, agg, scores, width, pred, pred_val, st);
+        });
+    });
+}
+
+// geom, scores, page, seq_lens, k, idx, new_lens, keep_first, keep_last, pred, pred_val, stream
+PyObject* page_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return with_args(a, n, 12, [](Args& x) -> PyObject* {
+        const rk_geom& g = x.geom;
+        const int64_t T = x.tokens(1);
+        if (!x.ok) return nullptr;
+        const int64_t width = x.tensor(1)->size(3);
+        auto* scores = (const float*)x.dev(1, f32, {g.batch, T, g.n_kv_heads, width});
+        const int32_t page = x.i32(2), k = x.i32(4), first = x.i32(7), last = x.i32(8), pred_val = x.i32(10);
+        auto* lens = (const int32_t*)x.dev(3, i32t, {g.batch});
+        auto* idx = (int32_t*)x.dev(5, i32t, {g.batch, T, g.n_kv_heads, k});
+        auto* new_lens = (const int32_t*)x.dev_or_null(6, i32t, {g.batch});
+        auto* pred = (const int32_t*)x.dev_or_null(9, i32t, {g.batch});
+        void* st = x.stream_here(11);
+        if (!x.ok) return nullptr;
+        return status_of([&] { return rk_page_select(&g, scores, width, (int32_t)T, page, lens, new_lens, k, first, last, idx, pred, pred_val, st); });
+    });
+}
+
+// geom, q, pages, table, idx, seq_lens, out, new_lens, first, end, cap, slopes, lse, pred, pred_val, workspace, stream
+PyObject* sparse_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return with_args(a, n, 17, [](Args& x) -> PyObject* {
+        const rk_geom& g = x.geom;
+        const int64_t T = x.tokens(1);
+        const at::Tensor* it = x.tensor(4);
+        if (!x.ok || it->dim() != 4 || it->size(3) > INT32_MAX) return nullptr;
+        const Args::Rows q = x.rows(1, T, g.n_q_heads);
+        const rk_pages pages = x.pool(2);
+        const Args::Table table = x.table(3);
+        const int64_t k = it->size(3);
+        auto* idx = (const int32_t*)x.dev(4, i32t, {g.batch, T, g.n_kv_heads, k});
+        auto* lens = (const int32_t*)x.dev(5, i32t, {g.batch});
+        void* out = x.dev(6, bf16, {g.batch, T, g.n_q_heads, g.head_dim});
+        auto* new_lens = (const int32_t*)x.dev_or_null(7, i32t, {g.batch});
+        const rk_prompt_scores s = x.scores(8, 9, 10, 11, T);
+        auto* lse = (float*)x.dev_or_null(12, f32, {g.batch, T, g.n_q_heads});
+        auto* pred = (const int32_t*)x.dev_or_null(13, i32t, {g.batch});
+        const int32_t pred_val = x.i32(14);
+        const Args::Scratch ws = x.a[15] == Py_None ? Args::Scratch{nullptr, 0} : x.workspace_here(15);
+        void* st = x.stream_here(16);
+        if (!x.ok) return nullptr;
+        return status_of([&] {
+            return rk_sparse_attn(&g, q.ptr, q.b, q.t, (int32_t)T, &pages, table.ptr, table.width, idx, (int32_t)k, lens, new_lens, &s, out, lse, pred, pred_val,
+                                  ws.ptr, ws.bytes, st);
+        });
+    });
+}
+
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 7) { PyErr_SetString(PyExc_TypeError, "setup(stream, raw_stream, device, geom, h2o_state, rope, kv8)"); return nullptr; }
-    for (int i = 0; i < 7; ++i) Py_INCREF(a[i]);
-    g_stream = a[0]; g_raw_stream = a[1]; g_device = a[2]; g_geom = a[3]; g_h2o_state = a[4]; g_rope = a[5]; g_kv8 = a[6];
+    if (n != 8) { PyErr_SetString(PyExc_TypeError, "setup(stream, raw_stream, device, geom, h2o_state, rope, kv8, pages)"); return nullptr; }
+    for (int i = 0; i < 8; ++i) Py_INCREF(a[i]);
+    g_stream = a[0]; g_raw_stream = a[1]; g_device = a[2]; g_geom = a[3]; g_h2o_state = a[4]; g_rope = a[5]; g_kv8 = a[6]; g_pages = a[7];
     Py_RETURN_NONE;
 }
 
@@ -381,11 +545,17 @@ PyMethodDef methods[] = {
     {"rk_gather_small_kv", (PyCFunction)(void (*)(void))gather, METH_FASTCALL, nullptr},
     {"rk_h2o_step", (PyCFunction)(void (*)(void))h2o_step, METH_FASTCALL, nullptr},
     {"rk_full_attn", (PyCFunction)(void (*)(void))full_attn, METH_FASTCALL, nullptr},
-    {"rk_rope_append", (PyCFunction)(void (*)(void))rope_append<false>, METH_FASTCALL, nullptr},
-    {"rk_rope_append_q8", (PyCFunction)(void (*)(void))rope_append<true>, METH_FASTCALL, nullptr},
+    {"rk_rope_append", (PyCFunction)(void (*)(void))rope_append<0>, METH_FASTCALL, nullptr},
+    {"rk_rope_append_q8", (PyCFunction)(void (*)(void))rope_append<1>, METH_FASTCALL, nullptr},
     {"rk_full_attn_q8", (PyCFunction)(void (*)(void))full_attn_q8, METH_FASTCALL, nullptr},
     {"rk_gather_small_kv_q8", (PyCFunction)(void (*)(void))gather_q8, METH_FASTCALL, nullptr},
     {"rk_prompt_attn", (PyCFunction)(void (*)(void))prompt_attn, METH_FASTCALL, nullptr},
+    {"rk_rope_append_paged", (PyCFunction)(void (*)(void))rope_append<2>, METH_FASTCALL, nullptr},
+    {"rk_paged_attn", (PyCFunction)(void (*)(void))paged_attn, METH_FASTCALL, nullptr},
+    {"rk_prefix_attn", (PyCFunction)(void (*)(void))prefix_attn, METH_FASTCALL, nullptr},
+    {"rk_page_scores", (PyCFunction)(void (*)(void))page_scores, METH_FASTCALL, nullptr},
+    {"rk_page_select", (PyCFunction)(void (*)(void))page_select, METH_FASTCALL, nullptr},
+    {"rk_sparse_attn", (PyCFunction)(void (*)(void))sparse_attn, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rkbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

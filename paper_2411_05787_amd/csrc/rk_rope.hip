@@ -1,16 +1,18 @@
-// Rotary positions of new tokens, and their rows into the full cache: rk_rope_table, rk_rope_append, rk_rope_append_q8.
+// Rotary positions of new tokens, and their rows into the full cache: rk_rope_table, rk_rope_append, rk_rope_append_q8,
+// rk_rope_append_paged.
 //
 // A pass reads every new row once and writes it once; there is nothing to reuse but a token's cosines and sines, which all of its
 // heads share.  Eight lanes take a row of 256 bytes, two chunks of eight dims each: in the half layout the two halves of eight pairs, in the
 // interleaved one any.  So a pair never leaves its lane, a turn needs no exchange, and q_out may be q.
 #include "rk_q8.h"
+#include "rk_pages.h"
 
 namespace rk {
 
 struct RopeParams {
     const uint16_t *q, *k, *v;
     int64_t q_b, q_t, k_b, k_t, v_b, v_t;
-    const float* table;                       // NULL: nothing is turned
+    const float* rope;                        // the table of cosines and sines; NULL: nothing is turned
     int32_t max_pos, rot, interleaved;
     const int32_t* positions; const int32_t* seq_lens; const int32_t* new_lens;
     int32_t n_new, Hq, Hkv;
@@ -19,8 +21,11 @@ struct RopeParams {
     rk_kv8 c8;                                                   // the one of 8 bits
     const int32_t* pred; int32_t pred_val;
     int32_t rows_per_token;                   // that token_row takes
-    int32_t block_wgs;                        // 8 bits: workgroups ahead of those with q rows
+    int32_t block_wgs;                        // 8 bits and pages with bounds: workgroups ahead of those that take rows
+    rk_pages pages;                           // the one in pages
+    const int32_t* table; int32_t width, shift;
 };
+enum CacheOf { kInRows, kIn8Bits, kInPages, kInBoundedPages };      // where the new rows go; the last: keys by append_page
 
 // Products and sums are rounded one by one: what is quantised later must not depend on which of them a compiler fuses.
 __device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) {
@@ -43,7 +48,7 @@ __device__ __forceinline__ LaneDims lane_dims(int c, const RopeParams& p) {
 struct Turn { float c[8], s[8]; };
 __device__ __forceinline__ void load_turn(Turn& t, const RopeParams& p, int pos, const LaneDims& d) {
     const bool known = (uint32_t)pos < (uint32_t)p.max_pos;
-    const float* row = p.table + (int64_t)(known ? pos : 0) * p.rot;
+    const float* row = p.rope + (int64_t)(known ? pos : 0) * p.rot;
     const int a = p.interleaved ? d.lo >> 1 : d.lo, b = p.interleaved ? d.hi >> 1 : d.lo + 4;
     float4 x[4] = {};
     if (d.turn_lo) { x[0] = *reinterpret_cast<const float4*>(row + a); x[2] = *reinterpret_cast<const float4*>(row + (p.rot >> 1) + a); }
@@ -95,7 +100,7 @@ __device__ __forceinline__ int position_of(const RopeParams& p, int b, int i, in
 // token's cosines and sines among several rows of a lane saves reads that hit in L2 and costs registers and coalescing: 8192 tokens of 48
 // heads take 39.1 us with one row to eight lanes (204 MB, 5.2 TB/s, the rate of a plain copy), 44.9 with two or four, 47.4 with eight; one
 // token 2.8, 3.4 and (four) 4.2.
-template <bool Q8>
+template <CacheOf C>
 __device__ __forceinline__ void token_row(const RopeParams& p, int b, uint32_t team) {
     const int i = (int)(team / (uint32_t)p.rows_per_token), r = (int)(team - (uint32_t)i * (uint32_t)p.rows_per_token);
     const NewTokens nt = new_tokens(p, b);
@@ -109,14 +114,20 @@ __device__ __forceinline__ void token_row(const RopeParams& p, int b, uint32_t t
         from = p.q + (int64_t)b * p.q_b + (int64_t)i * p.q_t + (int64_t)r * kD;
         to = p.q_out + (((int64_t)b * p.n_new + i) * p.Hq + r) * kD;
     } else {
-        if (Q8 || at < 0 || at >= p.capacity) return;
-        const bool key = r < n_q + p.Hkv;
-        const int g = r - n_q - (key ? 0 : p.Hkv);
+        if (C == kIn8Bits || at < 0 || at >= p.capacity) return;
+        const bool key = C != kInBoundedPages && r < n_q + p.Hkv;
+        const int g = r - n_q - (key || C == kInBoundedPages ? 0 : p.Hkv);
         from = (key ? p.k + (int64_t)b * p.k_b + (int64_t)i * p.k_t : p.v + (int64_t)b * p.v_b + (int64_t)i * p.v_t) + (int64_t)g * kD;
-        to = (key ? p.ck : p.cv) + (int64_t)b * p.c_b + (int64_t)g * p.c_h + at * kD;
+        if constexpr (C == kInPages || C == kInBoundedPages) {
+            const int page = p.table[(int64_t)b * p.width + (at >> p.shift)];
+            if ((uint32_t)page >= (uint32_t)p.pages.n_pages) return;
+            to = (uint16_t*)(key ? p.pages.k : p.pages.v) + (int64_t)page * p.pages.stride_p + (int64_t)g * p.pages.stride_h + (at & ((1 << p.shift) - 1)) * kD;
+        } else {
+            to = (key ? p.ck : p.cv) + (int64_t)b * p.c_b + (int64_t)g * p.c_h + at * kD;
+        }
     }
     u32x4 lo = *reinterpret_cast<const u32x4*>(from + d.lo), hi = *reinterpret_cast<const u32x4*>(from + d.hi);
-    if (p.table != nullptr && r < n_q + p.Hkv) {
+    if (p.rope != nullptr && r < n_q + (C == kInBoundedPages ? 0 : p.Hkv)) {
         Turn t;
         load_turn(t, p, position_of(p, b, i, nt.start), d);
         turn_chunks(lo, hi, t, d, p.interleaved != 0);
@@ -179,7 +190,7 @@ __device__ __forceinline__ void append_block(const RopeParams& p, int b, int x, 
         from += (int64_t)g * kD;
         lo = *reinterpret_cast<const u32x4*>(from + d.lo);
         hi = *reinterpret_cast<const u32x4*>(from + d.hi);
-        if (!values && p.table != nullptr) {
+        if (!values && p.rope != nullptr) {
             Turn t;
             load_turn(t, p, position_of(p, b, i, nt.start), d);
             turn_chunks(lo, hi, t, d, p.interleaved != 0);
@@ -240,7 +251,7 @@ __device__ __forceinline__ void append_block(const RopeParams& p, int b, int x, 
 __global__ __launch_bounds__(256) void rope_append_kernel(const RopeParams p) {
     const int b = blockIdx.y;
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
-    token_row<false>(p, b, blockIdx.x * 32 + (threadIdx.x >> 3));
+    token_row<kInRows>(p, b, blockIdx.x * 32 + (threadIdx.x >> 3));
 }
 
 template <int FORMAT, int PASSES>
@@ -252,7 +263,101 @@ __global__ __launch_bounds__(256) void rope_append_q8_kernel(const RopeParams p)
         append_block<FORMAT, PASSES>(p, b, blockIdx.x / (2 * p.Hkv), kv >> 1, (kv & 1) != 0);
         return;
     }
-    token_row<true>(p, b, (blockIdx.x - (uint32_t)p.block_wgs) * 32 + (threadIdx.x >> 3));
+    token_row<kIn8Bits>(p, b, (blockIdx.x - (uint32_t)p.block_wgs) * 32 + (threadIdx.x >> 3));
+}
+
+// ---- pages with bounds of their keys ----
+// Two bf16 as signed 16-bit numbers in their order, -NaN < -infinity .. -0 < +0 .. +infinity < NaN, and back.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ s16x2 in_order(uint32_t x) { return __builtin_bit_cast(s16x2, x ^ ((x & 0x80008000u) >> 15) * 0x7fffu); }
+__device__ __forceinline__ uint32_t out_of_order(s16x2 v) { const uint32_t x = __builtin_bit_cast(uint32_t, v); return x ^ ((x & 0x80008000u) >> 15) * 0x7fffu; }
+
+// One workgroup: page number start / page + x of one (sequence, KV head).  Its new keys are turned and written, and the bounds are taken of all rows
+// that the page holds then: so they depend on the rows alone, also where a sequence has been shortened and continued.  (The rows that were there are
+// read for it: half a page on average.)
+__device__ __forceinline__ void append_page(const RopeParams& p, int b, int x, int g) {
+    const NewTokens nt = new_tokens(p, b);
+    if (nt.n == 0) return;
+    const int64_t start = max(nt.start, (int64_t)0), end = min((int64_t)p.seq_lens[b], (int64_t)p.capacity);
+    const int64_t number = (start >> p.shift) + x;
+    if (end <= start || number > (end - 1) >> p.shift) return;
+    const int page = p.table[(int64_t)b * p.width + number];
+    if ((uint32_t)page >= (uint32_t)p.pages.n_pages) return;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const LaneDims d = lane_dims(tid & 7, p);
+    uint16_t* keys = (uint16_t*)p.pages.k + (int64_t)page * p.pages.stride_p + (int64_t)g * p.pages.stride_h;
+    const int rows = (int)min(end - (number << p.shift), (int64_t)1 << p.shift);
+    s16x2 least[8], most[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { least[e] = s16x2{32767, 32767}; most[e] = s16x2{-32768, -32768}; }
+    for (int s = tid >> 3; s < rows; s += 32) {
+        const int64_t r = (number << p.shift) + s;
+        uint16_t* at = keys + (int64_t)s * kD;
+        u32x4 lo, hi;
+        if (r < start) {
+            lo = *reinterpret_cast<const u32x4*>(at + d.lo);
+            hi = *reinterpret_cast<const u32x4*>(at + d.hi);
+        } else {
+            const int i = (int)(r - nt.start);
+            const uint16_t* from = p.k + (int64_t)b * p.k_b + (int64_t)i * p.k_t + (int64_t)g * kD;
+            lo = *reinterpret_cast<const u32x4*>(from + d.lo);
+            hi = *reinterpret_cast<const u32x4*>(from + d.hi);
+            if (p.rope != nullptr) {
+                Turn t;
+                load_turn(t, p, position_of(p, b, i, nt.start), d);
+                turn_chunks(lo, hi, t, d, p.interleaved != 0);
+            }
+            *reinterpret_cast<u32x4*>(at + d.lo) = lo;
+            *reinterpret_cast<u32x4*>(at + d.hi) = hi;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const s16x2 v = in_order(e < 4 ? lo[e] : hi[e - 4]);
+            least[e] = __builtin_elementwise_min(least[e], v);
+            most[e] = __builtin_elementwise_max(most[e], v);
+        }
+    }
+    // over the rows of the wavefront (lanes 8 apart), then over the wavefronts
+    __shared__ uint32_t sLeast[4][8][8], sMost[4][8][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        auto both = [&](auto&& pick, s16x2 v) {
+            const uint32_t x = __builtin_bit_cast(uint32_t, v);
+            v = pick(v, __builtin_bit_cast(s16x2, (uint32_t)dpp_move<kDppRor8>((int)x)));
+            LanePair r = rows_xor16(__builtin_bit_cast(int, v));
+            v = pick(__builtin_bit_cast(s16x2, r.a), __builtin_bit_cast(s16x2, r.b));
+            r = halves_xor32(__builtin_bit_cast(int, v));
+            return pick(__builtin_bit_cast(s16x2, r.a), __builtin_bit_cast(s16x2, r.b));
+        };
+        least[e] = both([](s16x2 a, s16x2 c) { return __builtin_elementwise_min(a, c); }, least[e]);
+        most[e] = both([](s16x2 a, s16x2 c) { return __builtin_elementwise_max(a, c); }, most[e]);
+        if (lane < 8) { sLeast[w][lane][e] = __builtin_bit_cast(uint32_t, least[e]); sMost[w][lane][e] = __builtin_bit_cast(uint32_t, most[e]); }
+    }
+    __syncthreads();
+    if (tid < 64) {                           // lane 8 c + e: dword e of lane c's dims
+        const int c = tid >> 3, e = tid & 7;
+        const LaneDims dc = lane_dims(c, p);
+        s16x2 lo = __builtin_bit_cast(s16x2, sLeast[0][c][e]), hi = __builtin_bit_cast(s16x2, sMost[0][c][e]);
+#pragma unroll
+        for (int y = 1; y < 4; ++y) {
+            lo = __builtin_elementwise_min(lo, __builtin_bit_cast(s16x2, sLeast[y][c][e]));
+            hi = __builtin_elementwise_max(hi, __builtin_bit_cast(s16x2, sMost[y][c][e]));
+        }
+        const int64_t to = ((int64_t)page * p.Hkv + g) * kD + (e < 4 ? dc.lo + 2 * e : dc.hi + 2 * (e - 4));
+        *reinterpret_cast<uint32_t*>((uint16_t*)p.pages.k_min + to) = out_of_order(lo);
+        *reinterpret_cast<uint32_t*>((uint16_t*)p.pages.k_max + to) = out_of_order(hi);
+    }
+}
+
+template <bool BOUNDS>
+__global__ __launch_bounds__(256) void rope_append_paged_kernel(const RopeParams p) {
+    const int b = blockIdx.y;
+    if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
+    if (BOUNDS && (int)blockIdx.x < p.block_wgs) {
+        append_page(p, b, blockIdx.x / p.Hkv, blockIdx.x % p.Hkv);
+        return;
+    }
+    token_row<BOUNDS ? kInBoundedPages : kInPages>(p, b, (blockIdx.x - (uint32_t)p.block_wgs) * 32 + (threadIdx.x >> 3));
 }
 
 // One workgroup per position.
@@ -301,7 +406,7 @@ static RopeParams rope_params(const rk_geom* geom, const rk_new_rows* rows, cons
     p.q = (const uint16_t*)rows->q; p.k = (const uint16_t*)rows->k; p.v = (const uint16_t*)rows->v;
     p.q_b = rows->q_stride_b; p.q_t = rows->q_stride_t; p.k_b = rows->k_stride_b; p.k_t = rows->k_stride_t;
     p.v_b = rows->v_stride_b; p.v_t = rows->v_stride_t;
-    if (rope) { p.table = rope->table; p.max_pos = rope->max_pos; p.rot = rope->rot_dim; p.interleaved = rope->interleaved; }
+    if (rope) { p.rope = rope->table; p.max_pos = rope->max_pos; p.rot = rope->rot_dim; p.interleaved = rope->interleaved; }
     p.positions = positions; p.seq_lens = seq_lens; p.new_lens = new_lens;
     p.n_new = rows->n_new; p.Hq = geom->n_q_heads; p.Hkv = geom->n_kv_heads;
     p.q_out = (uint16_t*)q_out;
@@ -357,5 +462,27 @@ extern "C" int rk_rope_append_q8(const rk_geom* geom, const rk_new_rows* rows, c
                   : cache->block == 64 ? (e4m3 ? rope_append_q8_kernel<RK_Q8_E4M3, 2> : rope_append_q8_kernel<RK_Q8_INT8, 2>)
                                        : (e4m3 ? rope_append_q8_kernel<RK_Q8_E4M3, 1> : rope_append_q8_kernel<RK_Q8_INT8, 1>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(block_wgs + q_wgs), geom->batch), dim3(256), 0, (hipStream_t)stream, p);
+    return launch_status();
+}
+
+extern "C" int rk_rope_append_paged(const rk_geom* geom, const rk_new_rows* rows, const rk_rope* rope, const int32_t* positions,
+                                    const rk_pages* pages, const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens,
+                                    void* q_out, const int32_t* pred, int32_t pred_val, void* stream) {
+    int rc = check_rope(geom, rows, rope, seq_lens, q_out);
+    if (rc != RK_OK) return rc;
+    if ((rc = check_pages(pages, true, false)) != RK_OK || (rc = check_table(pages, table, table_width)) != RK_OK) return rc;
+    RopeParams p = rope_params(geom, rows, rope, positions, seq_lens, new_lens, q_out, pred, pred_val);
+    p.pages = *pages;
+    p.table = table; p.width = table_width; p.shift = page_shift(pages->page);
+    p.capacity = table_width * pages->page;
+    const bool bounds = pages->k_min != nullptr;
+    p.rows_per_token = (rows->q ? p.Hq : 0) + (bounds ? 1 : 2) * p.Hkv;
+    const int64_t touched = ((int64_t)p.n_new + pages->page - 2) / pages->page + 1;       // pages that n_new rows can touch
+    const int64_t page_wgs = bounds ? touched * p.Hkv : 0, row_wgs = ((int64_t)p.n_new * p.rows_per_token + 31) / 32;
+    if (page_wgs + row_wgs * 32 > INT32_MAX) return RK_ERR_UNSUPPORTED;
+    if (turned_over_others(geom, rows, q_out)) return RK_ERR_INVALID_ARG;
+    p.block_wgs = (int32_t)page_wgs;
+    auto kernel = bounds ? rope_append_paged_kernel<true> : rope_append_paged_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(page_wgs + row_wgs), geom->batch), dim3(256), 0, (hipStream_t)stream, p);
     return launch_status();
 }
