@@ -204,11 +204,11 @@ __device__ __forceinline__ void tile_output(const TileRows<FORMAT>& t, ColState&
 }
 
 // The workgroup's columns < ncols <= C merged over its W wavefronts: calls put(column, dim, o0, o1, L) for the pairs of dims (the unnormalised
-// output against the common maximum, and its sum) and stat(column, m, l).
+// output against the common maximum, and its sum) and stat(column, m, l).  tid: the thread's number among the W wavefronts'.
 template <int W, int C> struct ColMergeLds { float m[W][16], l[W][16]; float o[W][C][kD]; };
 template <int W, int C, class Put, class Stat>
-__device__ __forceinline__ void merge_columns(ColMergeLds<W, C>& lds, ColState& st, int ncols, Put&& put, Stat&& stat) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
+__device__ __forceinline__ void merge_columns(ColMergeLds<W, C>& lds, ColState& st, int ncols, Put&& put, Stat&& stat, const int tid = (int)threadIdx.x) {
+    const int lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
     const float l = sum_xor32(sum_xor16(st.l));
     if (g == 0) { lds.m[w][n] = st.m; lds.l[w][n] = l; }
     if (n < ncols) {

@@ -8,23 +8,41 @@
 
 namespace rk {
 
+// Where the partial results of a row are: numbers at, at + step, .. of them.
+struct PartSource { const float *o, *ml; const int32_t* parts; int32_t rows_of, cols, splits, row_tiles, rows, batch; };
+struct PartRow { int64_t at; int step, n; };
+__device__ __forceinline__ PartRow part_row(const PartSource& s, const PromptParams& p, int b, int g, int row) {
+    const int per = p.n_new * p.G;
+    if (s.rows_of == kRowsChosen) {
+        const int i = (uint32_t)row / (uint32_t)p.G;
+        return {(((int64_t)b * p.n_new + i) * p.Hkv + g) * s.splits * p.G + (row - i * p.G), p.G, s.splits};
+    }
+    const bool shared = s.rows_of == kRowsShared;
+    const int64_t pair = shared ? g : (int64_t)b * p.Hkv + g;
+    const int r = shared ? b * per + row : row;
+    if (s.cols) return {((int64_t)g * s.splits * (shared ? 1 : p.batch) + s.parts[2 * pair]) * s.rows + r, s.rows, s.parts[2 * pair + 1]};
+    return {(pair * s.rows + r) * s.splits, 1, s.parts[pair * s.row_tiles + r / kPromptRows]};
+}
+
 // ---- up to 16 rows in all ----
 // prompt_cols_kernel over units of 16 rows: each is a buffer of its own inside its page.  A wavefront looks its next 64 tiles up at once, a lane each, and
-// takes the page numbers from the lanes: no wait for a number of the table stands before a request.
-template <int W, int CAP, bool SLOPE, int ROWS>
-__global__ __launch_bounds__(W * 64, W == kColWaves ? 2 : 1)
-void paged_cols_kernel(const PromptParams p) {
+// takes the page numbers from the lanes: no wait for a number of the table stands before a request.  SUB: pairs side by side in a workgroup, W wavefronts and a
+// room each; all of its wavefronts come to one barrier, also those that have nothing to do (there: x0 < 0).
+template <int W, int CAP, bool SLOPE, int ROWS, int SUB = 1>
+__device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, const int y0, const int z0, unsigned char* room) {
+    auto leave = [&]() { if constexpr (SUB > 1) __syncthreads(); };
+    if (SUB > 1 && x0 < 0) { leave(); return; }
     constexpr bool CHOSEN = ROWS == kRowsChosen, SHARED = ROWS == kRowsShared;
     int b, g, split, slot, parts = p.splits, token = 0;
     if constexpr (CHOSEN) {                   // (KV heads fastest: those of all tokens that share rows meet in few caches)
-        g = (int)(blockIdx.x % (uint32_t)p.Hkv);
-        const int rest = (int)(blockIdx.x / (uint32_t)p.Hkv), bt = rest / p.splits;
+        g = (int)((uint32_t)x0 % (uint32_t)p.Hkv);
+        const int rest = (int)((uint32_t)x0 / (uint32_t)p.Hkv), bt = rest / p.splits;
         split = rest - bt * p.splits;
         b = bt / p.n_new; token = bt - b * p.n_new;
         slot = (bt * p.Hkv + g) * p.splits + split;
     } else {
-        g = blockIdx.y; b = SHARED ? 0 : (int)blockIdx.z; split = blockIdx.x;
-        slot = (int)(blockIdx.z * gridDim.x + blockIdx.x);
+        g = y0; b = SHARED ? 0 : z0; split = x0;
+        slot = z0 * p.splits + x0;
         if (!SHARED && p.ragged != 0) {
             AttnParams a;
             a.ragged_batch = p.ragged; a.nch = p.splits; a.share_cap = kMaxSplits; a.cap2 = p.cap_rows; a.max_rows2 = p.max_len;
@@ -33,14 +51,15 @@ void paged_cols_kernel(const PromptParams p) {
             b = r.b; split = r.c; parts = r.nchunks;
         }
     }
-    if (!SHARED && p.pred != nullptr && p.pred[b] != p.pred_val) return;
+    if (!SHARED && p.pred != nullptr && p.pred[b] != p.pred_val) { leave(); return; }
     const Tokens tok = SHARED ? Tokens{} : tokens_of(p, b);
     const int n_rows = SHARED ? p.rows : CHOSEN ? (token < tok.n ? p.G : 0) : tok.n * p.G;
-    if (n_rows == 0) return;
+    if (n_rows == 0) { leave(); return; }
+    const int tid = SUB > 1 ? threadIdx.x % (W * 64) : threadIdx.x;
     const int64_t bg = SHARED ? g : (int64_t)b * p.Hkv + g;
     const bool partial = p.splits > 1 || p.joined != 0;
-    if (!CHOSEN && partial && split == 0 && threadIdx.x == 0) { p.parts[2 * bg] = slot; p.parts[2 * bg + 1] = parts; }
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, gr = lane >> 4;
+    if (!CHOSEN && partial && split == 0 && tid == 0) { p.parts[2 * bg] = slot; p.parts[2 * bg + 1] = parts; }
+    const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, gr = lane >> 4;
     bool real = col < n_rows;
     const int r0 = (CHOSEN ? token * p.G : 0) + min(col, n_rows - 1);
     const Query me = SHARED ? shared_query(p, g, r0, real) : paged_query<ROWS>(p, tok, b, g, r0);
@@ -97,21 +116,24 @@ void paged_cols_kernel(const PromptParams p) {
             x.row[c] = __builtin_amdgcn_readlane(first[c], n);
             int rows = min(hi - x.row[c], 16);
             asm("" : "+s"(rows));
-            x.rows[c] = pg < 0 ? 0 : max(rows, 0);
-            x.at[c] = pg < 0 ? 0 : (int64_t)pg * p.s_p + (int64_t)(x.row[c] & in_page) * kD;
+            rows = max(rows, 0) & ~(pg >> 31);
+            asm("" : "+s"(rows));             // (no branch)
+            x.rows[c] = rows;
+            x.at[c] = (int64_t)max(pg, 0) * p.s_p + (int64_t)((x.row[c] & in_page) * kD);
         }
         return x;
     };
     auto buffer = [&](const uint16_t* base, const Tile& x, int c) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base + x.at[c]), 0, x.rows[c] * (kD * 2), 0x00020000);
     };
+    constexpr int kAux = CHOSEN ? 0 : kStreamAux;
     TileRows<kBf16> rows;
     auto ask_keys = [&](const Tile& x) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const __amdgpu_buffer_rsrc_t r = buffer(k, x, c);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) rows.k[c][s] = __builtin_amdgcn_raw_buffer_load_b128(r, col * (kD * 2) + operand_dim<false>(s, gr) * 2, 0, kStreamAux);
+            for (int s = 0; s < 4; ++s) rows.k[c][s] = __builtin_amdgcn_raw_buffer_load_b128(r, col * (kD * 2) + operand_dim<false>(s, gr) * 2, 0, kAux);
         }
     };
     auto ask_values = [&](const Tile& x) {
@@ -119,7 +141,7 @@ void paged_cols_kernel(const PromptParams p) {
         for (int c = 0; c < 2; ++c) {
             const __amdgpu_buffer_rsrc_t r = buffer(v, x, c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) rows.v[4 * c + e] = __builtin_amdgcn_raw_buffer_load_b128(r, (4 * gr + e) * (kD * 2) + 16 * col, 0, kStreamAux);
+            for (int e = 0; e < 4; ++e) rows.v[4 * c + e] = __builtin_amdgcn_raw_buffer_load_b128(r, (4 * gr + e) * (kD * 2) + 16 * col, 0, kAux);
         }
     };
 
@@ -147,9 +169,9 @@ void paged_cols_kernel(const PromptParams p) {
                 s[x][i] = fmaf(bend<CAP>(s[x][i], form), form.a, form.b);
                 if constexpr (SLOPE) s[x][i] = fmaf(-slope, fabsf((float)(me.pos - now.row[x] - 4 * gr) - (float)i), s[x][i]);
             }
-        bool masked = false;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) masked = masked || now.rows[x] < 16 || now.row[x] < in_lo || now.row[x] + 16 > in_hi;
+        // (one sign of them all, and no branch for each)
+        const int inside = min(min(now.rows[0], now.rows[1]) - 16, min(min(now.row[0], now.row[1]) - in_lo, in_hi - 16 - max(now.row[0], now.row[1])));
+        const bool masked = inside < 0;
         auto sees = [&](int x, int j) { return now.rows[x] != 0 && j >= me.lo && j < me.hi; };
         if (masked) {
             asm volatile("" ::: "memory");    // (a branch: most tiles have nothing to mask)
@@ -191,8 +213,7 @@ void paged_cols_kernel(const PromptParams p) {
         now = next;
     }
 
-    __shared__ __attribute__((aligned(16))) ColMergeLds<W, 16> lds;
-    __shared__ float sInv[16];
+    ColMergeLds<W, 16>& lds = *reinterpret_cast<ColMergeLds<W, 16>*>(room);
     if (partial) {
         // (columns of one pair and part side by side)
         const int64_t at = CHOSEN ? (int64_t)slot * p.G : ((int64_t)g * p.splits * (SHARED ? 1 : p.batch) + slot) * (SHARED ? p.rows : p.n_new * p.G);
@@ -202,12 +223,13 @@ void paged_cols_kernel(const PromptParams p) {
                       },
                       [&](int x, float m, float l) {
                           *reinterpret_cast<float2*>(p.part_ml + (at + x) * 2) = make_float2(m * kLog2e, l);
-                      });
+                      }, tid);
         return;
     }
-    if constexpr (SHARED) return;             // (never: the shared rows' results are joined)
+    if constexpr (SHARED || SUB > 1) return;  // (never: those results are joined)
     auto out_row = [&](int x) { const int i = x / p.G; return ((int64_t)b * p.n_new + token + i) * p.Hq + g * p.G + (x - i * p.G); };
     float* o = &lds.o[0][0][0];
+    __shared__ float sInv[16];
     merge_columns(lds, st, n_rows,
                   [&](int x, int d, float o0, float o1, float) { o[x * kD + d] = o0; o[x * kD + d + 1] = o1; },
                   [&](int x, float m, float l) {
@@ -221,50 +243,88 @@ void paged_cols_kernel(const PromptParams p) {
     }
 }
 
-// Where the partial results of a row are: numbers at, at + step, .. of them.
-struct PartSource { const float *o, *ml; const int32_t* parts; int32_t rows_of, cols, splits, row_tiles, rows, batch; };
-struct PartRow { int64_t at; int step, n; };
-__device__ __forceinline__ PartRow part_row(const PartSource& s, const PromptParams& p, int b, int g, int row) {
-    const int per = p.n_new * p.G;
-    if (s.rows_of == kRowsChosen) {
-        const int i = (uint32_t)row / (uint32_t)p.G;
-        return {(((int64_t)b * p.n_new + i) * p.Hkv + g) * s.splits * p.G + (row - i * p.G), p.G, s.splits};
-    }
-    const bool shared = s.rows_of == kRowsShared;
-    const int64_t pair = shared ? g : (int64_t)b * p.Hkv + g;
-    const int r = shared ? b * per + row : row;
-    if (s.cols) return {((int64_t)g * s.splits * (shared ? 1 : p.batch) + s.parts[2 * pair]) * s.rows + r, s.rows, s.parts[2 * pair + 1]};
-    return {(pair * s.rows + r) * s.splits, 1, s.parts[pair * s.row_tiles + r / kPromptRows]};
+template <int W, int CAP, bool SLOPE, int ROWS>
+__global__ __launch_bounds__(W * 64, W == kColWaves ? 2 : 1)
+void paged_cols_kernel(const PromptParams p) {
+    __shared__ __attribute__((aligned(16))) unsigned char room[sizeof(ColMergeLds<W, 16>)];
+    paged_cols<W, CAP, SLOPE, ROWS>(p, (int)blockIdx.x, (int)blockIdx.y, (int)blockIdx.z, room);
 }
 
-// Joins the parts of a row, sum_s 2^(m_s - m) (l_s, o_s): a wavefront each.  SOURCES = 2: those over the shared rows, then those over the sequence's own.
-template <int SOURCES>
+// ---- a shared prefix ----
+// The first `shared_wgs` workgroups go over the shared rows for the queries of all sequences, the others over each sequence's own: in one launch, as the former are
+// bound by the matrix cores and the latter by what they wait for.  Both leave partial results.  OWN: wavefronts to a pair where a sequence's own are
+// columns (two: two pairs to a workgroup), 0: row tiles.
+template <int CAP, bool SLOPE, bool ALL_COLS, int OWN>
+__global__ __launch_bounds__(256, 2)
+void prefix_kernel(const PromptParams all, const PromptParams own, const int32_t shared_wgs, const int32_t own_parts) {
+    constexpr int kCols = (int)sizeof(ColMergeLds<kColWaves, 16>), kRoom = ALL_COLS ? kCols : tile_lds(1);
+    static_assert(kRoom >= kCols && 2 * sizeof(ColMergeLds<2, 16>) <= (size_t)kRoom, "room");
+    __shared__ __attribute__((aligned(16))) unsigned char room[kRoom];
+    if ((int)blockIdx.x < shared_wgs) {
+        if constexpr (ALL_COLS) paged_cols<kColWaves, CAP, SLOPE, kRowsShared>(all, (int)(blockIdx.x % (uint32_t)all.splits), (int)(blockIdx.x / (uint32_t)all.splits), 0, room);
+        else prompt_tile<1, CAP, SLOPE, kRowsShared>(all, blockIdx.x, room);
+        return;
+    }
+    const int x = (int)blockIdx.x - shared_wgs;
+    if constexpr (OWN != 0) {
+        constexpr int SUB = kColWaves / OWN;
+        const int sub = SUB == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (OWN * 64)), y = SUB * x + sub;
+        const int rest = y / own.splits, b = rest / own.Hkv;
+        paged_cols<OWN, CAP, SLOPE, kRowsPaged, SUB>(own, y < own_parts ? y - rest * own.splits : -1, rest - b * own.Hkv, b, room + sub * sizeof(ColMergeLds<OWN, 16>));
+    } else {
+        prompt_tile<1, CAP, SLOPE, kRowsPaged>(own, (uint32_t)x, room);
+    }
+}
+
+// Joins the parts of a row, sum_s 2^(m_s - m) (l_s, o_s).   SOURCES = 2: those over the shared rows, then those over the sequence's own.
+// TEAM wavefronts to a row: one, or where there are many parts four, of which each adds every fourth.
+template <int SOURCES, int TEAM>
 __global__ __launch_bounds__(256)
 void paged_merge_kernel(const PromptParams p, const PartSource s0, const PartSource s1) {
-    constexpr int N = SOURCES * kMaxSplits;
-    const int g = blockIdx.y, b = blockIdx.z, w = threadIdx.x >> 6, lane = threadIdx.x & 63, row = blockIdx.x * 4 + w;
+    constexpr int N = SOURCES * kMaxSplits, kRound = 8;
+    const int g = blockIdx.y, b = blockIdx.z, w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int row = TEAM == 1 ? blockIdx.x * 4 + w : blockIdx.x, mine = TEAM == 1 ? 0 : w;
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
     __shared__ float sW[4][N];
+    // (requested with the sequence's length: of a row that there is not, any numbers, which nothing is made of)
+    const int safe_row = min(row, p.n_new * p.G - 1);
+    const PartRow r0 = part_row(s0, p, b, g, safe_row);
+    PartRow r1{0, 0, 0};
+    if constexpr (SOURCES == 2) r1 = part_row(s1, p, b, g, safe_row);
+    asm volatile("" :: "s"(__builtin_amdgcn_readfirstlane(r0.n)), "s"(__builtin_amdgcn_readfirstlane(r1.n)));
     const Tokens tok = tokens_of(p, b);
     if (row >= tok.n * p.G) return;
-    const PartRow r0 = part_row(s0, p, b, g, row);
-    PartRow r1{0, 0, 0};
-    if constexpr (SOURCES == 2) r1 = part_row(s1, p, b, g, row);
     if (SOURCES == 1 && p.joined == 0 && !s0.cols && s0.rows_of == kRowsPaged && r0.n == 1) return;      // (the output is there already)
+    // what a lane takes of both sources' statistics, and the first outputs, requested together
+    const int n = r0.n + r1.n;
     float m[N / 64], l[N / 64], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < N / 64; ++i) {
-        const int s = lane + 64 * i;
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (s < r0.n) ml = *reinterpret_cast<const float2*>(s0.ml + (r0.at + (int64_t)s * r0.step) * 2);
-        else if (SOURCES == 2 && s - r0.n < r1.n) ml = *reinterpret_cast<const float2*>(s1.ml + (r1.at + (int64_t)(s - r0.n) * r1.step) * 2);
-        m[i] = ml.x; l[i] = ml.y;
-        top = fmaxf(top, ml.x);
+        m[i] = -INFINITY; l[i] = 0.f;
+        if (64 * i >= n) continue;            // (the same for the whole wavefront)
+        const int s = min(lane + 64 * i, n - 1);
+        const bool second = SOURCES == 2 && s >= r0.n;
+        const float2 ml = *reinterpret_cast<const float2*>(second ? s1.ml + (r1.at + (int64_t)(s - r0.n) * r1.step) * 2 : s0.ml + (r0.at + (int64_t)s * r0.step) * 2);
+        m[i] = lane + 64 * i < n ? ml.x : -INFINITY; l[i] = ml.y;
     }
+    const float2* from0 = reinterpret_cast<const float2*>(s0.o + r0.at * kD) + lane;
+    const float2* from1 = SOURCES == 2 ? reinterpret_cast<const float2*>(s1.o + r1.at * kD) + lane : nullptr;
+    float2 v[kRound];
+    auto request = [&](int s) {
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            const int x = min(s + TEAM * i, n - 1);
+            v[i] = SOURCES == 2 && x >= r0.n ? from1[(int64_t)(x - r0.n) * r1.step * (kD / 2)] : from0[(int64_t)x * r0.step * (kD / 2)];
+        }
+    };
+    request(mine);
+#pragma unroll
+    for (int i = 0; i < N / 64; ++i) top = fmaxf(top, m[i]);
     top = wave_max(top);
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N / 64; ++i) {
+        if (64 * i >= n) continue;
         const float a = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top);
         sum = fmaf(a, l[i], sum);
         sW[w][lane + 64 * i] = a;
@@ -272,21 +332,23 @@ void paged_merge_kernel(const PromptParams p, const PartSource s0, const PartSou
     sum = wave_sum(sum);
     wave_lds_sync();
     float o0 = 0.f, o1 = 0.f;
-    auto add = [&](const float* from_o, const PartRow& r, int w0) {
-        const float2* from = reinterpret_cast<const float2*>(from_o + r.at * kD) + lane;
-        for (int s = 0; s < r.n; s += 8) {
-            float2 v[8];
+    for (int s = mine; s < n; s += TEAM * kRound) {
+        if (s != mine) request(s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = from[(int64_t)min(s + i, r.n - 1) * r.step * (kD / 2)];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float a = s + i < r.n ? sW[w][w0 + s + i] : 0.f;
-                if (a != 0.f) { o0 = fmaf(a, v[i].x, o0); o1 = fmaf(a, v[i].y, o1); }      // (a part without rows left nothing)
-            }
+        for (int i = 0; i < kRound; ++i) {
+            const float a = s + TEAM * i < n ? sW[w][s + TEAM * i] : 0.f;
+            if (a != 0.f) { o0 = fmaf(a, v[i].x, o0); o1 = fmaf(a, v[i].y, o1); }      // (a part without rows left nothing)
         }
-    };
-    add(s0.o, r0, 0);
-    if constexpr (SOURCES == 2) add(s1.o, r1, r0.n);
+    }
+    if constexpr (TEAM > 1) {
+        __shared__ float2 sO[TEAM][64];
+        sO[w][lane] = make_float2(o0, o1);
+        __syncthreads();
+        if (w != 0) return;
+        o0 = o1 = 0.f;
+#pragma unroll
+        for (int y = 0; y < TEAM; ++y) { o0 += sO[y][lane].x; o1 += sO[y][lane].y; }
+    }
     const int i = (uint32_t)row / (uint32_t)p.G;
     const int64_t to = ((int64_t)b * p.n_new + i) * p.Hq + g * p.G + (row - i * p.G);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -304,7 +366,8 @@ template <int W, int ROWS> static PagedKernel cols_form(int cap, bool slope) {
         default: return slope ? paged_cols_kernel<W, kNoCap, true, ROWS> : paged_cols_kernel<W, kNoCap, false, ROWS>;
     }
 }
-template <int ROWS> static PagedKernel tile_form(int cap, bool slope) {
+static PagedKernel tile_form(int cap, bool slope) {
+    constexpr int ROWS = kRowsPaged;
     switch (cap) {
         case kNearCap: return slope ? prompt_tile_kernel<1, kNearCap, true, ROWS> : prompt_tile_kernel<1, kNearCap, false, ROWS>;
         case kFarCap: return slope ? prompt_tile_kernel<1, kFarCap, true, ROWS> : prompt_tile_kernel<1, kFarCap, false, ROWS>;
@@ -365,13 +428,13 @@ static PartSource source_of(const PromptParams& p, int rows_of, int rows) {
     return {p.part_o, p.part_ml, p.parts, rows_of, p.cols, p.splits, p.row_tiles, rows, p.batch};
 }
 static void set_plan(PromptParams& p, const PromptPlan& plan) { p.splits = plan.splits; p.row_tiles = plan.row_tiles; p.split_tiles = plan.split_tiles; }
-template <int ROWS>
-static int launch_rows(PromptParams& p, const PromptPlan& plan, int64_t pairs, int cap, bool slope, hipStream_t st) {
+// rk_prompt_attn's launches, over pages.
+static int launch_paged(PromptParams& p, const PromptPlan& plan, int64_t pairs, int cap, bool slope, hipStream_t st) {
     if (plan.cols) {
-        auto kernel = plan.alone && ROWS == kRowsPaged ? cols_form<kColAlone, kRowsPaged>(cap, slope) : cols_form<kColWaves, ROWS>(cap, slope);
-        hipLaunchKernelGGL(kernel, dim3(plan.splits, p.Hkv, ROWS == kRowsShared ? 1 : p.batch), dim3((plan.alone && ROWS == kRowsPaged ? kColAlone : kColWaves) * 64), 0, st, p);
+        auto kernel = plan.alone ? cols_form<kColAlone, kRowsPaged>(cap, slope) : cols_form<kColWaves, kRowsPaged>(cap, slope);
+        hipLaunchKernelGGL(kernel, dim3(plan.splits, p.Hkv, p.batch), dim3((plan.alone ? kColAlone : kColWaves) * 64), 0, st, p);
     } else {
-        auto kernel = plan.wide && ROWS == kRowsPaged ? prompt_tile_kernel<2, kNoCap, false, kRowsPaged> : tile_form<ROWS>(cap, slope);
+        auto kernel = plan.wide ? prompt_tile_kernel<2, kNoCap, false, kRowsPaged> : tile_form(cap, slope);
         const int64_t total = pairs * plan.row_tiles * plan.splits;
         // (the second workgroup of a compute unit in the opposite order: see rk_prompt_attn)
         p.first_round = !plan.wide && total <= 2 * kComputeUnits ? (int)((kComputeUnits + pairs - 1) / pairs) : INT32_MAX;
@@ -379,7 +442,34 @@ static int launch_rows(PromptParams& p, const PromptPlan& plan, int64_t pairs, i
     }
     return launch_status();
 }
-static dim3 merge_grid(const PromptParams& p) { return dim3((unsigned)((p.n_new * p.G + 3) / 4), p.Hkv, p.batch); }
+using PrefixKernel = void (*)(const PromptParams, const PromptParams, const int32_t, const int32_t);
+template <bool ALL_COLS, int OWN_COLS> static PrefixKernel prefix_form(int cap, bool slope) {
+    switch (cap) {
+        case kNearCap: return slope ? prefix_kernel<kNearCap, true, ALL_COLS, OWN_COLS> : prefix_kernel<kNearCap, false, ALL_COLS, OWN_COLS>;
+        case kFarCap: return slope ? prefix_kernel<kFarCap, true, ALL_COLS, OWN_COLS> : prefix_kernel<kFarCap, false, ALL_COLS, OWN_COLS>;
+        default: return slope ? prefix_kernel<kNoCap, true, ALL_COLS, OWN_COLS> : prefix_kernel<kNoCap, false, ALL_COLS, OWN_COLS>;
+    }
+}
+// The workgroups over the shared rows: one to a compute unit, beside those over the sequences' own.
+static PromptPlan shared_plan(int64_t pairs, int64_t rows, int64_t max_len) {
+    PromptPlan f = prompt_plan_of(pairs, rows, max_len, false, false);
+    f.alone = false;
+    if (f.cols) return f;
+    f.split_tiles = 4;
+    int64_t s = kComputeUnits / (pairs * f.row_tiles);
+    const int64_t most = (max_len + f.split_tiles * kPromptTile - 1) / (f.split_tiles * kPromptTile);
+    if (s > most) s = most;
+    if (s > kMaxSplits) s = kMaxSplits;
+    f.splits = (int)(s < 1 ? 1 : s);
+    return f;
+}
+template <int SOURCES>
+static int launch_merge(const PromptParams& p, const PartSource& s0, const PartSource& s1, hipStream_t st) {
+    const int rows = p.n_new * p.G, parts = s0.splits + (SOURCES == 2 ? s1.splits : 0);
+    if (parts > 16) hipLaunchKernelGGL((paged_merge_kernel<SOURCES, 4>), dim3((unsigned)rows, p.Hkv, p.batch), dim3(256), 0, st, p, s0, s1);
+    else hipLaunchKernelGGL((paged_merge_kernel<SOURCES, 1>), dim3((unsigned)((rows + 3) / 4), p.Hkv, p.batch), dim3(256), 0, st, p, s0, s1);
+    return launch_status();
+}
 
 }  // namespace rk
 
@@ -405,10 +495,9 @@ extern "C" int rk_paged_attn(const rk_geom* geom, const void* q, int64_t q_strid
         p.ragged = plan.cols ? ragged_batch_of(geom) : 0;
     }
     hipStream_t st = (hipStream_t)stream;
-    if ((rc = launch_rows<kRowsPaged>(p, plan, pairs, cap, slope, st)) != RK_OK || plan.splits == 1) return rc;
+    if ((rc = launch_paged(p, plan, pairs, cap, slope, st)) != RK_OK || plan.splits == 1) return rc;
     const PartSource s = source_of(p, kRowsPaged, (int)rows);
-    hipLaunchKernelGGL(paged_merge_kernel<1>, merge_grid(p), dim3(256), 0, st, p, s, s);
-    return launch_status();
+    return launch_merge<1>(p, s, s, st);
 }
 
 extern "C" size_t rk_prefix_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t max_prefix, int32_t max_own) {
@@ -440,20 +529,24 @@ extern "C" int rk_prefix_attn(const rk_geom* geom, const void* q, int64_t q_stri
     all.rows = (int32_t)all_rows;
     const int cap = cap_of(scores);
     const bool slope = (scores && scores->slopes) || (geom->scale == 0.f && cap == kNoCap);
-    PromptPlan plan_all = prompt_plan_of(own.Hkv, all_rows, own.most_shared, false, false);
+    const PromptPlan plan_all = shared_plan(own.Hkv, all_rows, own.most_shared);
     PromptPlan plan_own = prompt_plan_of(pairs, rows, own.most_own, false, false);
-    plan_all.alone = plan_own.alone = false;
-    if (pairs * plan_own.row_tiles * plan_own.splits > INT32_MAX / 2 || own.Hkv * (int64_t)plan_all.row_tiles * plan_all.splits > INT32_MAX / 2) return RK_ERR_UNSUPPORTED;
+    plan_own.alone = false;
+    const int64_t wgs_all = (int64_t)own.Hkv * plan_all.row_tiles * plan_all.splits, wgs_own = pairs * plan_own.row_tiles * plan_own.splits;
+    if (wgs_all + wgs_own > INT32_MAX / 2) return RK_ERR_UNSUPPORTED;
     set_plan(all, plan_all);
     set_plan(own, plan_own);
     const size_t first = paged_scratch(own.Hkv, all_rows, own.most_shared);
     if (workspace_bytes < first || !place_parts(all, plan_all, own.Hkv, all_rows, (char*)workspace, first) ||
         !place_parts(own, plan_own, pairs, rows, (char*)workspace + first, workspace_bytes - first)) return RK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    if ((rc = launch_rows<kRowsShared>(all, plan_all, own.Hkv, cap, slope, st)) != RK_OK) return rc;
-    if ((rc = launch_rows<kRowsPaged>(own, plan_own, pairs, cap, slope, st)) != RK_OK) return rc;
-    hipLaunchKernelGGL(paged_merge_kernel<2>, merge_grid(own), dim3(256), 0, st, own, source_of(all, kRowsShared, (int)all_rows), source_of(own, kRowsPaged, (int)rows));
-    return launch_status();
+    // (a sequence has no more rows than the batch: columns all, columns of a sequence, or neither)
+    const bool two = plan_own.cols && plan_own.splits == 1 && wgs_own > kComputeUnits;
+    auto kernel = plan_all.cols ? prefix_form<true, kColWaves>(cap, slope) : !plan_own.cols ? prefix_form<false, 0>(cap, slope)
+                  : two ? prefix_form<false, 2>(cap, slope) : prefix_form<false, kColWaves>(cap, slope);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs_all + (two ? (wgs_own + 1) / 2 : wgs_own))), dim3(256), 0, st, all, own, (int32_t)wgs_all, (int32_t)wgs_own);
+    if ((rc = launch_status()) != RK_OK) return rc;
+    return launch_merge<2>(own, source_of(all, kRowsShared, (int)all_rows), source_of(own, kRowsPaged, (int)rows), st);
 }
 
 extern "C" size_t rk_sparse_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t k, int32_t page) {
@@ -484,6 +577,5 @@ extern "C" int rk_sparse_attn(const rk_geom* geom, const void* q, int64_t q_stri
     hipLaunchKernelGGL((cols_form<kColWaves, kRowsChosen>(cap, slope)), dim3((unsigned)(pairs * plan.splits)), dim3(kColWaves * 64), 0, st, p);
     if ((rc = launch_status()) != RK_OK || plan.splits == 1) return rc;
     const PartSource s = source_of(p, kRowsChosen, p.G);
-    hipLaunchKernelGGL(paged_merge_kernel<1>, merge_grid(p), dim3(256), 0, st, p, s, s);
-    return launch_status();
+    return launch_merge<1>(p, s, s, st);
 }

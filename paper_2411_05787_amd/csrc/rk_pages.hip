@@ -19,64 +19,104 @@ struct ScoreParams {
     const int32_t* pred; int32_t pred_val;
 };
 
-__global__ __launch_bounds__(256)
+// P: blocks of 16 pages to a wavefront.  One: the workgroup's wavefronts have 16 pages each.  Four, for many tokens: all have the same 64 and every
+// fourth four tokens, so that a query is read and its signs parted once for 64 pages.
+template <int P>
+__global__ __launch_bounds__(256, P == 1 ? 4 : 2)
 void page_score_kernel(const ScoreParams p) {
-    const int g = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, gr = lane >> 4;
-    if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
+    const int g = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, gr = lane >> 4;
     const int block = (int)(blockIdx.x % (uint32_t)p.page_blocks), t_first = (int)(blockIdx.x / (uint32_t)p.page_blocks) * p.chunk;
+    const int most = (int)min((int64_t)p.width, p.s_stride);      // pages that are looked at
+    const int j0 = block * 64 + (P == 1 ? w * 16 : 0);
+    int page[P];                              // (requested before the sequence's length is known)
+#pragma unroll
+    for (int x = 0; x < P; ++x) {
+        const int j = j0 + 16 * x + n;
+        page[x] = p.table[(int64_t)b * p.width + min(j, p.width - 1)];
+        if (j >= most) page[x] = -1;
+    }
+    if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
     const int raw = p.seq_lens[b], n_tok = p.new_lens != nullptr ? min(max(p.new_lens[b], 0), p.n_new) : p.n_new;
     const int64_t start = (int64_t)raw - n_tok;
-    const int t_end = min(t_first + p.chunk, n_tok), j0 = block * 64 + w * 16;
-    const int most = (int)min((int64_t)p.width, p.s_stride);      // pages that are looked at
+    const int t_end = min(t_first + p.chunk, n_tok);
     // pages that token i sees
     auto pages_of = [&](int i) { return (int)min(((start + i) >> p.shift) + 1, (int64_t)most); };
     if (t_first >= t_end || start + t_end - 1 < 0 || j0 >= pages_of(t_end - 1)) return;
-    const int j = j0 + n, page = j < most ? p.table[(int64_t)b * p.width + j] : -1;
-    const bool there = (uint32_t)page < (uint32_t)p.n_pages;
-    const int64_t at = ((int64_t)(there ? page : 0) * p.Hkv + g) * kD + 8 * gr;
-    bf16x8 hi[4], lo[4];
+    bf16x8 hi[P][4], lo[P][4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        hi[s] = *reinterpret_cast<const bf16x8*>(p.k_max + at + 32 * s);
-        lo[s] = *reinterpret_cast<const bf16x8*>(p.k_min + at + 32 * s);
+    for (int x = 0; x < P; ++x) {
+        const int64_t at = ((int64_t)((uint32_t)page[x] < (uint32_t)p.n_pages ? page[x] : 0) * p.Hkv + g) * kD + 8 * gr;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            hi[x][s] = *reinterpret_cast<const bf16x8*>(p.k_max + at + 32 * s);
+            lo[x][s] = *reinterpret_cast<const bf16x8*>(p.k_min + at + 32 * s);
+        }
     }
-    for (int t0 = t_first; t0 < t_end; t0 += 4) {
-        const int i = t0 + gr;
-        float best = -INFINITY;
-        bool none = false;
-        for (int h0 = 0; h0 < p.G; h0 += 4) {
-            const uint16_t* qr = p.q + (int64_t)b * p.q_b + (int64_t)min(t0 + (n >> 2), t_end - 1) * p.q_t + (int64_t)(g * p.G + min(h0 + (n & 3), p.G - 1)) * kD + 8 * gr;
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    const uint16_t* q0 = p.q + (int64_t)b * p.q_b + (int64_t)(g * p.G) * kD + 8 * gr;
+    u32x4 q[4];
+    auto ask = [&](int t0, int h0) {
+        const uint16_t* qr = q0 + (int64_t)min(t0 + (n >> 2), t_end - 1) * p.q_t + (int64_t)min(h0 + (n & 3), p.G - 1) * kD;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(qr + 32 * s);
-                u32x4 up, down;
+        for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const u32x4*>(qr + 32 * s);
+    };
+    const int step = P == 1 ? 4 : 16, t_mine = t_first + (P == 1 ? 0 : 4 * w);
+    if (t_mine < t_end) ask(t_mine, 0);
+    for (int t0 = t_mine; t0 < t_end; t0 += step) {
+        const int i = t0 + gr;
+        float best[P];
+        bool none[P];
+#pragma unroll
+        for (int x = 0; x < P; ++x) { best[x] = -INFINITY; none[x] = false; }
+        for (int h0 = 0; h0 < p.G; h0 += 4) {
+            u32x4 up[4], down[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t negative = ((x[e] & 0x80008000u) >> 15) * 0xffffu;      // the halves whose sign is set, in full
-                    down[e] = x[e] & negative;
-                    up[e] = x[e] & ~negative;
+                    const uint32_t negative = ((q[s][e] & 0x80008000u) >> 15) * 0xffffu;      // the halves whose sign is set, in full
+                    down[s][e] = q[s][e] & negative;
+                    up[s][e] = q[s][e] & ~negative;
                 }
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, up), hi[s], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, down), lo[s], acc, 0, 0, 0);
+            const bool more = h0 + 4 < p.G;
+            ask(more ? t0 : min(t0 + step, t_end - 1), more ? h0 + 4 : 0);       // (the next one's, beside the products)
+            f32x4 acc[P];
+#pragma unroll
+            for (int x = 0; x < P; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+#pragma unroll
+                for (int x = 0; x < P; ++x) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, up[s]), hi[x][s], acc[x], 0, 0, 0);
+#pragma unroll
+                for (int x = 0; x < P; ++x) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, down[s]), lo[x][s], acc[x], 0, 0, 0);
             }
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                if (h0 + x < p.G) {
-                    const float one = acc[x] * p.scale;
-                    best = aggregate(best, one, h0 + x, p.agg);
-                    none = none || (one != one && (h0 + x == 0 || p.agg != RK_AGG_FIRST));      // (a maximum would pass over it)
-                }
+            for (int x = 0; x < P; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    if (h0 + y < p.G) {
+                        const float one = acc[x][y] * p.scale;
+                        best[x] = aggregate(best[x], one, h0 + y, p.agg);
+                        none[x] = none[x] || (one != one && (h0 + y == 0 || p.agg != RK_AGG_FIRST));      // (a maximum would pass over it)
+                    }
         }
-        if (none) best = __uint_as_float(0x7fc00000u);
-        if (p.agg == RK_AGG_MEAN) best /= (float)p.G;
-        if (i < t_end && start + i >= 0 && j < pages_of(i)) p.scores[(((int64_t)b * p.n_new + i) * p.Hkv + g) * p.s_stride + j] = there ? best : -INFINITY;
+        if (i >= t_end || start + i < 0) continue;
+        const int seen = pages_of(i);
+        float* to = p.scores + (((int64_t)b * p.n_new + i) * p.Hkv + g) * p.s_stride + j0 + n;
+#pragma unroll
+        for (int x = 0; x < P; ++x) {
+            if (p.agg == RK_AGG_MEAN) best[x] /= (float)p.G;
+            if (none[x]) best[x] = __uint_as_float(0x7fc00000u);
+            if ((uint32_t)page[x] >= (uint32_t)p.n_pages) best[x] = -INFINITY;
+            if (j0 + 16 * x + n < seen) to[16 * x] = best[x];
+        }
     }
 }
 
 // ---- the pages with the largest ----
-// A workgroup to a row: the k-th largest key digit by digit, then the pages above it and the first of those that equal it, in their order.
-constexpr int kSelectThreads = 256;
+// W wavefronts to a row of up to 64 W R scores, which stay in registers, R to a lane; bound by its chain of instructions.  The threshold is built bit by bit
+// from the top: the largest T with k keys or more at or above it, and as soon as there are k exactly the pages are found (mostly after a third of the 32
+// steps).  Rows of more scores than 16384 go to the long form.
+constexpr int kSelectThreads = 256, kSelectMost = 16 * 16 * 64;
 struct SelectParams {
     const float* scores; int64_t s_stride;
     const int32_t *seq_lens, *new_lens;
@@ -85,27 +125,109 @@ struct SelectParams {
     const int32_t* pred; int32_t pred_val;
 };
 
-__global__ __launch_bounds__(kSelectThreads)
-void page_select_kernel(const SelectParams p) {
-    const int g = (int)(blockIdx.x % (uint32_t)p.Hkv), bt = (int)(blockIdx.x / (uint32_t)p.Hkv), b = bt / p.n_new, i = bt - b * p.n_new;
-    if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
+// A row: its token's pages n and its own one, how many are wanted of them, its scores and results.  wanted < 0: there is no such token.
+struct SelectRow { int n, last, wanted; const float* scores; int32_t* idx; };
+__device__ __forceinline__ SelectRow select_row(const SelectParams& p, int row) {
+    const int bt = (int)((uint32_t)row / (uint32_t)p.Hkv), b = bt / p.n_new, i = bt - b * p.n_new;
+    SelectRow x{0, 0, -1, p.scores + (int64_t)row * p.s_stride, p.idx + (int64_t)row * p.k};
+    if (p.pred != nullptr && p.pred[b] != p.pred_val) return x;
     const int n_tok = p.new_lens != nullptr ? min(max(p.new_lens[b], 0), p.n_new) : p.n_new;
-    if (i >= n_tok) return;
+    if (i >= n_tok) return x;
     const int64_t pos = (int64_t)p.seq_lens[b] - n_tok + i;
-    const int last = pos < 0 ? -1 : (int)(pos >> p.shift), n = (int)min((int64_t)last + 1, p.s_stride), k = min(p.k, n);
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const float* row = p.scores + ((int64_t)bt * p.Hkv + g) * p.s_stride;
-    int32_t* out = p.idx + ((int64_t)bt * p.Hkv + g) * p.k;
-    for (int x = k + tid; x < p.k; x += kSelectThreads) out[x] = -1;
+    x.last = pos < 0 ? -1 : (int)(pos >> p.shift);
+    x.n = (int)min((int64_t)x.last + 1, p.s_stride);
+    x.wanted = min(p.k, x.n);
+    return x;
+}
+// (what is kept in any case, and what is no number, counts as +infinity; one zero; above 0 in any case)
+__device__ __forceinline__ uint32_t select_key(const SelectParams& p, const SelectRow& x, int j, float s) {
+    return j < p.keep_first || j > x.last - p.keep_last || !(s <= INFINITY) ? key_of(INFINITY) : key_of(s + 0.f);
+}
+
+template <int W, int R>
+__global__ __launch_bounds__(W * 64)
+void page_select_kernel(const SelectParams p) {
+    const SelectRow row = select_row(p, (int)blockIdx.x);
+    if (row.wanted < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = row.n, k = row.wanted;
+    for (int x = k + tid; x < p.k; x += W * 64) row.idx[x] = -1;
     if (k == n) {
-        for (int x = tid; x < n; x += kSelectThreads) out[x] = x;
+        for (int x = tid; x < n; x += W * 64) row.idx[x] = x;
         return;
     }
-    // (what is kept in any case, and what is no number, counts as +infinity; one zero)
-    auto key = [&](int j) {
-        const float x = row[j];
-        return j < p.keep_first || j > last - p.keep_last || !(x <= INFINITY) ? key_of(INFINITY) : key_of(x + 0.f);
+    uint32_t x[R];
+    {
+        float s[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] = row.scores[min((w * R + r) * 64 + lane, n - 1)];
+#pragma unroll
+        for (int r = 0; r < R; ++r) { const int j = (w * R + r) * 64 + lane; x[r] = j < n ? select_key(p, row, j, s[r]) : 0u; }
+    }
+    __shared__ int sCount[2][W], sBase[W][2];
+    int turn = 0;
+    // keys of the row at or above v
+    auto count = [&](uint32_t v) {
+        int c = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) c += __popcll(__ballot(x[r] >= v));
+        if constexpr (W > 1) {
+            if (lane == 0) sCount[turn][w] = c;
+            lds_barrier();
+            c = 0;
+#pragma unroll
+            for (int y = 0; y < W; ++y) c += sCount[turn][y];
+            turn ^= 1;                        // (the next count's words: these may still be read)
+            c = __builtin_amdgcn_readfirstlane(c);
+        }
+        return c;
     };
+    uint32_t at = 0;
+    int above = -1;                           // keys above `at`, where some that equal it stay out
+    bool exact = false;
+    for (int bit = 31; bit >= 0 && !exact; --bit) {
+        const uint32_t v = at | 1u << bit;
+        const int c = count(v);
+        if (c >= k) { at = v; exact = c == k; }
+    }
+    if (!exact) above = at == 0xffffffffu ? 0 : count(at + 1);
+    const int left = exact ? 0 : k - above;   // of the keys that equal `at`
+    int done = 0, ties = 0;
+    if constexpr (W > 1) {
+        int a = 0, t = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            a += __popcll(__ballot(exact ? x[r] >= at : x[r] > at));
+            t += __popcll(__ballot(!exact && x[r] == at));
+        }
+        if (lane == 0) { sBase[w][0] = a; sBase[w][1] = t; }
+        lds_barrier();
+        for (int y = 0; y < w; ++y) { done += sBase[y][0]; ties += sBase[y][1]; }
+        done = __builtin_amdgcn_readfirstlane(done);
+        ties = __builtin_amdgcn_readfirstlane(ties);
+    }
+    const unsigned long long below = (1ull << lane) - 1ull;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool in = exact ? x[r] >= at : x[r] > at, tie = !exact && x[r] == at;
+        const unsigned long long am = __ballot(in), tm = __ballot(tie);
+        const int t = ties + __popcll(tm & below);
+        if (in || (tie && t < left)) row.idx[done + __popcll(am & below) + min(t, left)] = (w * R + r) * 64 + lane;
+        done += __popcll(am); ties += __popcll(tm);
+    }
+}
+
+// The long form: a workgroup to a row, which is read again for every eight bits of the threshold.
+__global__ __launch_bounds__(kSelectThreads)
+void page_select_long_kernel(const SelectParams p) {
+    const SelectRow row = select_row(p, (int)blockIdx.x);
+    if (row.wanted < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = row.n, k = row.wanted;
+    for (int x = k + tid; x < p.k; x += kSelectThreads) row.idx[x] = -1;
+    if (k == n) {
+        for (int x = tid; x < n; x += kSelectThreads) row.idx[x] = x;
+        return;
+    }
+    auto key = [&](int j) { return select_key(p, row, j, row.scores[j]); };
     __shared__ uint32_t hist[256];
     __shared__ uint32_t sPrefix;
     __shared__ int sLeft, sCount[kSelectThreads / 64][2];
@@ -147,7 +269,7 @@ void page_select_kernel(const SelectParams p) {
             done += sCount[y][0]; ties += sCount[y][1];
         }
         a += __popcll(am & below); t += __popcll(tm & below);
-        if (above || (tie && t < left)) out[a + min(t, left)] = j;
+        if (above || (tie && t < left)) row.idx[a + min(t, left)] = j;
         __syncthreads();
     }
 }
@@ -176,12 +298,14 @@ extern "C" int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stri
     const int64_t most = table_width < s_stride ? table_width : s_stride;
     p.page_blocks = (int)((most + 63) / 64);
     const int64_t wgs = (int64_t)p.page_blocks * p.Hkv * geom->batch;
-    int64_t chunks = 4 * kComputeUnits / wgs;
-    if (chunks > (n_new + 3) / 4) chunks = (n_new + 3) / 4;
+    const bool many = n_new >= 16;
+    const int unit = many ? 16 : 4;           // tokens of a workgroup's round
+    int64_t chunks = (many ? 2 : 4) * kComputeUnits / wgs;
+    if (chunks > (n_new + unit - 1) / unit) chunks = (n_new + unit - 1) / unit;
     if (chunks < 1) chunks = 1;
-    p.chunk = (int)(((n_new + chunks - 1) / chunks + 3) / 4 * 4);
+    p.chunk = (int)(((n_new + chunks - 1) / chunks + unit - 1) / unit * unit);
     chunks = (n_new + p.chunk - 1) / p.chunk;
-    hipLaunchKernelGGL(page_score_kernel, dim3((unsigned)(p.page_blocks * chunks), p.Hkv, geom->batch), dim3(256), 0, (hipStream_t)stream, p);
+    hipLaunchKernelGGL((many ? page_score_kernel<4> : page_score_kernel<1>), dim3((unsigned)(p.page_blocks * chunks), p.Hkv, geom->batch), dim3(256), 0, (hipStream_t)stream, p);
     return launch_status();
 }
 
@@ -199,6 +323,10 @@ extern "C" int rk_page_select(const rk_geom* geom, const float* scores, int64_t 
     p.scores = scores; p.s_stride = s_stride; p.seq_lens = seq_lens; p.new_lens = new_lens;
     p.shift = page_shift(page); p.n_new = n_new; p.Hkv = geom->n_kv_heads; p.k = k; p.keep_first = keep_first; p.keep_last = keep_last;
     p.idx = idx; p.pred = pred; p.pred_val = pred_val;
-    hipLaunchKernelGGL(page_select_kernel, dim3((unsigned)rows), dim3(kSelectThreads), 0, (hipStream_t)stream, p);
+    const int64_t n = s_stride;
+    auto kernel = n <= 256 ? page_select_kernel<1, 4> : n <= 512 ? page_select_kernel<1, 8> : n <= 1024 ? page_select_kernel<1, 16> : n <= 4096 ? page_select_kernel<4, 16>
+                  : n <= kSelectMost ? page_select_kernel<16, 16> : page_select_long_kernel;
+    const int threads = n <= 1024 ? 64 : n <= 4096 ? 256 : n <= kSelectMost ? 1024 : kSelectThreads;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, (hipStream_t)stream, p);
     return launch_status();
 }

@@ -171,18 +171,20 @@ constexpr int kBlockRows = 32;
 constexpr int kKRow = kD * 2 + 16, kVRow = kD * 2 + 64;     // bytes from row to row in LDS: the reads of a phase fall on different banks
 constexpr int kKBlock = kBlockRows * kKRow, kVBlock = kBlockRows * kVRow;
 
-// In pages: a block is two units of 16 rows, each a buffer of its own inside a page, and blocks start at multiples of 32 rows.  The table's entries
-// of 64 pages are in the lanes of a register, those of the next 64 in another: no wait for a page number stands before a request.
-template <int QB, int CAP, bool SLOPE, int ROWS = kRowsPlain>
-__global__ __launch_bounds__(256, QB == 1 ? 2 : 1)
-void prompt_tile_kernel(const PromptParams p) {
+// In pages: a block is two units of 16 rows, each inside a page, and blocks start at multiples of 32 rows.  Where the pages of the next 64 table entries are
+// is in the lanes of two registers, the entries behind those in another: no wait for a page number stands before a request.  Units are read whole (a
+// page has all its rows, whatever they hold), the first page's in the place of one that is none.
+constexpr int tile_lds(int qb) { return 4 * qb * (kKBlock + kVBlock); }
+template <int QB, int CAP, bool SLOPE, int ROWS>
+__device__ __forceinline__ void prompt_tile(const PromptParams& p, const uint32_t wg, unsigned char* sK) {
     constexpr bool PAGED = ROWS != kRowsPlain, SHARED = ROWS == kRowsShared;
+    constexpr int kDeep = PAGED ? 2 : 1;      // stages between a block's request and its way into LDS
     constexpr int kRows = kPromptRows * QB, kSlots = 16 * QB, kRing = 4 * QB, kAheadK = 2 + QB, kAheadV = QB;
     // Consecutive workgroups go round the 8 dies, and the (sequence, KV head) pairs run fastest: a die sees few pairs (one, where there are 8; the
     // same head of every sequence), whose rows its L2 keeps, and of each sequence as many row tiles as any other die.  The last tokens', which see
     // most, come first.
-    const int pairs = SHARED ? p.Hkv : p.Hkv * p.batch, bg = (int)(blockIdx.x % (uint32_t)pairs);
-    int rest = (int)(blockIdx.x / (uint32_t)pairs);
+    const int pairs = SHARED ? p.Hkv : p.Hkv * p.batch, bg = (int)(wg % (uint32_t)pairs);
+    int rest = (int)(wg / (uint32_t)pairs);
     if (rest >= p.first_round) rest = p.row_tiles * p.splits - 1 - (rest - p.first_round);
     const int tile = p.row_tiles - 1 - rest / p.splits, split = rest % p.splits;
     const int b = SHARED ? 0 : bg / p.Hkv, g = bg - b * p.Hkv;
@@ -192,55 +194,72 @@ void prompt_tile_kernel(const PromptParams p) {
     if (tile * kRows >= n_rows) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const int row0 = tile * kRows + w * 32 * QB + n;
+    unsigned char* const sV = sK + kRing * kKBlock;
+    __shared__ int sLo[4], sHi[4], sInLo[4], sInHi[4], sBad;
     bool real[QB];
     Query me[QB];
-#pragma unroll
-    for (int x = 0; x < QB; ++x) {
-        real[x] = row0 + 32 * x < n_rows;
-        const int r = min(row0 + 32 * x, n_rows - 1);
-        me[x] = SHARED ? shared_query(p, g, r, real[x]) : PAGED ? paged_query<ROWS>(p, tok, b, g, r) : query_of(p, tok, b, g, r);
-    }
-
-    __shared__ __attribute__((aligned(16))) unsigned char sK[kRing * kKBlock], sV[kRing * kVBlock];
-    __shared__ int sLo[4], sHi[4], sInLo[4], sInHi[4], sBad;
-
-    int w_lo = INT32_MAX, w_hi = INT32_MIN, in_lo = INT32_MIN, in_hi = INT32_MAX;
-#pragma unroll
-    for (int x = 0; x < QB; ++x) {
-        if (!real[x]) continue;
-        if (me[x].lo < me[x].hi) { w_lo = min(w_lo, me[x].lo); w_hi = max(w_hi, me[x].hi); }
-        in_lo = max(in_lo, me[x].lo); in_hi = min(in_hi, me[x].hi);
-    }
-    w_lo = wave_min(w_lo); w_hi = wave_max_i(w_hi); in_lo = wave_max_i(in_lo); in_hi = wave_min(in_hi);
-    if (lane == 0) { sLo[w] = w_lo; sHi[w] = w_hi; sInLo[w] = in_lo; sInHi[w] = in_hi; }
-    if (tid == 0) sBad = 0;
-
+    int in_lo, in_hi;
     bf16x8 q[QB][8];
-#pragma unroll
-    for (int x = 0; x < QB; ++x) {
-        const uint16_t* qr = p.q + (int64_t)(SHARED ? me[x].b : b) * p.q_b + (int64_t)me[x].token * p.q_t + (int64_t)me[x].head * kD;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) q[x][s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s + 8 * h);
-    }
-    ScoreForm form = score_form<CAP>(p, kLog2e);
-    if (!SLOPE && form.a < 0.f) {             // raw products are compared below: their order has to be the scores'
-        form.a = -form.a;
-#pragma unroll
-        for (int x = 0; x < QB; ++x)
-#pragma unroll
-            for (int s = 0; s < 8; ++s) q[x][s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[x][s]) ^ 0x80008000u);
-    }
+    ScoreForm form;
     float slope2[QB];
-    if constexpr (SLOPE) {
+    // What the rows are and see, their queries on their way, and what the wavefronts tell one another of them.
+    auto ask_queries = [&]() {
 #pragma unroll
-        for (int x = 0; x < QB; ++x) slope2[x] = p.slopes != nullptr ? p.slopes[me[x].head] * kLog2e : 0.f;
+        for (int x = 0; x < QB; ++x) {
+            real[x] = row0 + 32 * x < n_rows;
+            const int r = min(row0 + 32 * x, n_rows - 1);
+            me[x] = SHARED ? shared_query(p, g, r, real[x]) : PAGED ? paged_query<ROWS>(p, tok, b, g, r) : query_of(p, tok, b, g, r);
+        }
+        int w_lo = INT32_MAX, w_hi = INT32_MIN;
+        in_lo = INT32_MIN; in_hi = INT32_MAX;
+#pragma unroll
+        for (int x = 0; x < QB; ++x) {
+            if (!real[x]) continue;
+            if (me[x].lo < me[x].hi) { w_lo = min(w_lo, me[x].lo); w_hi = max(w_hi, me[x].hi); }
+            in_lo = max(in_lo, me[x].lo); in_hi = min(in_hi, me[x].hi);
+        }
+        w_lo = wave_min(w_lo); w_hi = wave_max_i(w_hi); in_lo = wave_max_i(in_lo); in_hi = wave_min(in_hi);
+        if (lane == 0) { sLo[w] = w_lo; sHi[w] = w_hi; sInLo[w] = in_lo; sInHi[w] = in_hi; }
+        if (tid == 0) sBad = 0;
+#pragma unroll
+        for (int x = 0; x < QB; ++x) {
+            const uint16_t* qr = p.q + (int64_t)(SHARED ? me[x].b : b) * p.q_b + (int64_t)me[x].token * p.q_t + (int64_t)me[x].head * kD;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) q[x][s] = *reinterpret_cast<const bf16x8*>(qr + 16 * s + 8 * h);
+        }
+        form = score_form<CAP>(p, kLog2e);
+        if (!SLOPE && form.a < 0.f) {         // raw products are compared below: their order has to be the scores'
+            form.a = -form.a;
+#pragma unroll
+            for (int x = 0; x < QB; ++x)
+#pragma unroll
+                for (int s = 0; s < 8; ++s) q[x][s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[x][s]) ^ 0x80008000u);
+        }
+        if constexpr (SLOPE) {
+#pragma unroll
+            for (int x = 0; x < QB; ++x) slope2[x] = p.slopes != nullptr ? p.slopes[me[x].head] * kLog2e : 0.f;
+        }
+    };
+    int lo = 0, hi = 0;
+    // SHARED: the whole prefix, whose first blocks are requested before anything is known of the queries; where there are ranges, what they leave.
+    if constexpr (SHARED) {
+        hi = shared_rows(p);
+        if (p.first != nullptr) {
+            ask_queries();
+            __syncthreads();
+            lo = min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])) & -kBlockRows;
+            hi = max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3]));
+            __syncthreads();                  // (they are written once more)
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        hi = __builtin_amdgcn_readfirstlane(hi);
+    } else {
+        ask_queries();
+        __syncthreads();
+        const int first_seen = __builtin_amdgcn_readfirstlane(min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])));
+        lo = PAGED ? first_seen & -kBlockRows : first_seen;
+        hi = __builtin_amdgcn_readfirstlane(max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3])));
     }
-    __syncthreads();
-    const int first_seen = __builtin_amdgcn_readfirstlane(min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])));
-    const int lo = PAGED ? first_seen & -kBlockRows : first_seen;
-    const int hi = __builtin_amdgcn_readfirstlane(max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3])));
-    const int all_lo = __builtin_amdgcn_readfirstlane(max(max(sInLo[0], sInLo[1]), max(sInLo[2], sInLo[3])));
-    const int all_hi = __builtin_amdgcn_readfirstlane(min(min(sInHi[0], sInHi[1]), min(sInHi[2], sInHi[3])));
     const int tiles = hi > lo ? (int)(((int64_t)hi - lo + kPromptTile - 1) / kPromptTile) : 0;
     const int parts = max(1, min(p.splits, (int)((uint32_t)(tiles + p.split_tiles - 1) / (uint32_t)p.split_tiles)));
     if (split >= parts) return;
@@ -250,8 +269,15 @@ void prompt_tile_kernel(const PromptParams p) {
     const int t0 = __builtin_amdgcn_readfirstlane(each * split + rest_tiles * split / parts);
     const int t1 = __builtin_amdgcn_readfirstlane(each * (split + 1) + rest_tiles * (split + 1) / parts);
     const int b0 = 2 * t0, b1 = 2 * t1, end = min(hi, lo + b1 * kBlockRows);       // blocks
-    // the blocks whose stage has nothing to mask and nothing to clean: safe .. safe + n_safe - 1
-    const int safe = (int)(((int64_t)all_lo - lo + kBlockRows - 1) >> 5), n_safe = max((int)(((int64_t)all_hi - lo) >> 5) - kAheadV - safe, 0);
+    int all_lo, all_hi, safe, n_safe;
+    auto know_ranges = [&]() {
+        all_lo = __builtin_amdgcn_readfirstlane(max(max(sInLo[0], sInLo[1]), max(sInLo[2], sInLo[3])));
+        all_hi = __builtin_amdgcn_readfirstlane(min(min(sInHi[0], sInHi[1]), min(sInHi[2], sInHi[3])));
+        // the blocks whose stage has nothing to mask and nothing to clean: safe .. safe + n_safe - 1
+        safe = (int)(((int64_t)all_lo - lo + kBlockRows - 1) >> 5);
+        n_safe = max((int)(((int64_t)all_hi - lo) >> 5) - kAheadV - safe, 0);
+    };
+    if constexpr (!SHARED) know_ranges();
     float m[QB], l[QB], from[QB], limit[QB], alpha[QB];
     f32x16 o[QB][4];
 #pragma unroll
@@ -278,15 +304,23 @@ void prompt_tile_kernel(const PromptParams p) {
         const __amdgpu_buffer_rsrc_t rsrc = buffer(rows + (int64_t)(lo + i * kBlockRows) * kD, bytes_of(i));
         return Staged{__builtin_amdgcn_raw_buffer_load_b128(rsrc, tid * 16, 0, 0), __builtin_amdgcn_raw_buffer_load_b128(rsrc, tid * 16, 4096, 0)};
     };
-    // PAGED: where a block's two units are, in elements from the head's first page, and how much of them there is.  Asked for in the blocks' order.
-    struct Place { int64_t at[2]; int bytes[2]; };
+    // PAGED: where a block's two units are, in bytes from the head's first page.  Asked for in the blocks' order.
+    struct Place { int64_t at[2]; };
     const int32_t* table = PAGED ? p.table + (SHARED ? 0 : (int64_t)b * p.width) : nullptr;
     auto entries = [&](int from) { return table[min(from + lane, p.width - 1)]; };
-    int e0 = 0, entry = 0, entry_next = 0;
+    int e0 = 0, entry_next = 0;
+    uint32_t where_lo = 0, where_hi = 0;      // this lane's entry: its page's place, the highest bit set where it is none
     uint32_t gone = 0;                        // units without a page: bits 2 d and 2 d + 1 of the block d behind the stage's
+    auto keep = [&](int page) {
+        const bool there = (uint32_t)page < (uint32_t)p.n_pages;
+        const uint64_t at = there ? (uint64_t)page * (uint64_t)(p.s_p * 2) : 0;
+        where_lo = (uint32_t)at;
+        where_hi = (uint32_t)(at >> 32) | (there ? 0u : 0x80000000u);
+        asm volatile("" : "+v"(where_lo), "+v"(where_hi));      // (here before a branch ends: a request that is in flight at one would be waited for behind it)
+    };
     if constexpr (PAGED) {
         e0 = (lo + b0 * kBlockRows) >> p.shift;
-        if (b0 < b1) { entry = entries(e0); entry_next = entries(e0 + 64); }
+        if (b0 < b1) { keep(entries(e0)); entry_next = entries(e0 + 64); }
     }
     auto place = [&](int i, int behind) {
         Place x;
@@ -296,30 +330,44 @@ void prompt_tile_kernel(const PromptParams p) {
             int e = (r >> p.shift) - e0;
             if (e >= 64) {
                 e0 += 64; e -= 64;
-                entry = entry_next;
-                asm volatile("" : "+v"(entry));       // (here before the branch ends: see request)
+                keep(entry_next);
                 entry_next = entries(e0 + 64);
             }
-            const int page = __builtin_amdgcn_readlane(entry, e);
-            const bool there = (uint32_t)page < (uint32_t)p.n_pages;
-            int have = min(end - r, 16);
-            asm("" : "+s"(have));
-            have = max(have, 0);
-            gone |= (uint32_t)(!there && have > 0) << (2 * behind + c);
-            x.at[c] = there ? (int64_t)page * p.s_p + (r & ((1 << p.shift) - 1)) * kD : 0;
-            x.bytes[c] = there ? have * (kD * 2) : 0;
+            const uint32_t hi32 = __builtin_amdgcn_readlane(where_hi, e);
+            gone |= (hi32 >> 31) << (2 * behind + c);
+            x.at[c] = (int64_t)((uint64_t)(hi32 & 0x7fffffffu) << 32 | (uint32_t)__builtin_amdgcn_readlane(where_lo, e)) + (uint32_t)((r & ((1 << p.shift) - 1)) * (kD * 2));
         }
         return x;
     };
-    auto request_at = [&](const uint16_t* rows, const Place& x) {
-        return Staged{__builtin_amdgcn_raw_buffer_load_b128(buffer(rows + x.at[0], x.bytes[0]), tid * 16, 0, 0),
-                      __builtin_amdgcn_raw_buffer_load_b128(buffer(rows + x.at[1], x.bytes[1]), tid * 16, 0, 0)};
-    };
+    auto load16 = [&](const uint16_t* rows, int64_t at) { return *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(rows) + at + (uint32_t)(tid * 16)); };
+    auto request_at = [&](const uint16_t* rows, const Place& x) { return Staged{load16(rows, x.at[0]), load16(rows, x.at[1])}; };
+    Staged ks[kAheadK], vs[kAheadV], kr[kDeep], vr[kDeep];      // (kr, vr: of every second stage its own)
+    Place pl[kAheadK + kDeep];
+    if (PAGED && b0 < b1) {
+#pragma unroll
+        for (int c = 0; c < kAheadK + kDeep; ++c) pl[c] = place(b0 + c, c);
+#pragma unroll
+        for (int c = 0; c < kAheadK; ++c) ks[c] = request_at(k_rows, pl[c]);
+#pragma unroll
+        for (int c = 0; c < kAheadV; ++c) vs[c] = request_at(v_rows, pl[c]);
+#pragma unroll
+        for (int c = 0; c < kDeep; ++c) { kr[c] = request_at(k_rows, pl[kAheadK + c]); vr[c] = request_at(v_rows, pl[kAheadV + c]); }
+    }
+    if constexpr (SHARED) {
+        __builtin_amdgcn_sched_barrier(0);
+        ask_queries();
+        lds_barrier();                        // (what is on its way stays so)
+        know_ranges();
+    }
     const int k_slot = (tid >> 4) * kKRow + (tid & 15) * 16, v_slot = (tid >> 4) * kVRow + (tid & 15) * 16;
     auto write_k = [&](const Staged& s, int at, int c) { *reinterpret_cast<u32x4*>(sK + at + k_slot + c * 16 * kKRow) = s.r[c]; };
     auto write_v = [&](const Staged& s, int at, int c) { *reinterpret_cast<u32x4*>(sV + at + v_slot + c * 16 * kVRow) = s.r[c]; };
     auto outside = [&](int i) { const int j0 = lo + i * kBlockRows; return j0 < all_lo || j0 + kBlockRows > all_hi; };
-    auto clean = [&](Staged& v, int i) {      // V's block i, where a row sees a part of it only
+    auto clean = [&](Staged& v, int i, int behind) {      // V's block i, where a row sees a part of it only
+        if constexpr (PAGED) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) if (gone >> (2 * behind + c) & 1u) v.r[c] = u32x4{0u, 0u, 0u, 0u};
+        }
         if (!outside(i)) return;
         if (has_non_finite(v.r[0]) || has_non_finite(v.r[1])) {
             sBad = 1;
@@ -411,25 +459,24 @@ void prompt_tile_kernel(const PromptParams p) {
     // of block i - 1's weights (values at v_at) in the other, block i's weights all along or, where scores take work of their own, in the first
     // half, and that and the next maximum in the second.  Keys of block i + 2 are at k_next.  Beside it keys of block i + kAheadK are written to
     // k_to and values of block i + kAheadV to v_to, those of the blocks behind them requested.
-    Staged kr, vr;
     const uint16_t *k_next_rows = k_rows, *v_next_rows = v_rows;      // of the blocks that are requested next
     auto wait_lds = [](auto n) { __builtin_amdgcn_s_waitcnt(0xc07f | decltype(n)::value << 8); };
-    auto stage = [&](Ahead& now, Ahead& ahead, const Weights& behind, Weights& made, int i, int& v_bytes, Place& v_place, int k_at, int k_next, int k_to, int v_at, int v_to, bool fenced, bool fence) {
+    auto stage = [&](Ahead& now, Ahead& ahead, const Weights& behind, Weights& made, Staged& kr, Staged& vr, int i, int& v_bytes, Place& v_place, int k_at, int k_next, int k_to, int v_at, int v_to, bool fenced, bool fence) {
         constexpr int kPer = CAP != kNoCap || SLOPE ? 2 : 1, kHalf = kSlots / 2, kTail = kHalf + 2;
-        if ((uint32_t)(i - safe) >= (uint32_t)n_safe || (PAGED && (gone & 3u) != 0)) {
+        if ((uint32_t)(i - safe) >= (uint32_t)n_safe || (PAGED && (gone & (3u << 2 * kAheadV | 3u)) != 0)) {
             asm volatile("" ::: "memory");    // (a branch: most blocks have nothing of it)
             mask(now, i);
-            clean(vr, i + kAheadV);
+            clean(vr, i + kAheadV, kAheadV);
         }
         const bool grew = follow(now);
         const int k_bytes = PAGED ? 0 : bytes_of(i + kAheadK + 1);
-        __amdgpu_buffer_rsrc_t k_in, v_in, k_in2, v_in2;
+        __amdgpu_buffer_rsrc_t k_in, v_in;
+        Place k_place, v_now;
         if constexpr (PAGED) {
             gone >>= 2;                       // (behind the mask: the bits are the next block's now)
-            const Place at = place(i + kAheadK + 1, kAheadK);
-            k_in = buffer(k_rows + at.at[0], at.bytes[0]); k_in2 = buffer(k_rows + at.at[1], at.bytes[1]);
-            v_in = buffer(v_rows + v_place.at[0], v_place.bytes[0]); v_in2 = buffer(v_rows + v_place.at[1], v_place.bytes[1]);
-            v_place = at;
+            k_place = place(i + kAheadK + kDeep, kAheadK + kDeep - 1);
+            v_now = v_place;
+            v_place = k_place;
         } else {
             k_in = buffer(k_next_rows, k_bytes), v_in = buffer(v_next_rows, v_bytes);
             v_bytes = k_bytes;                // (of V that block is requested two stages later)
@@ -463,7 +510,7 @@ void prompt_tile_kernel(const PromptParams p) {
                 if (k == 4 * QB) wait_lds(std::integral_constant<int, 4>{});
                 if (k == kHalf) wait_lds(std::integral_constant<int, 4>{});
                 if (k == kHalf + 4 * QB) wait_lds(std::integral_constant<int, 0>{});
-                if (k == kHalf) __builtin_amdgcn_s_waitcnt(0xf70);      // (vmcnt 0: all that the last stage requested, before the first of it is written)
+                if (k == kHalf) __builtin_amdgcn_s_waitcnt(PAGED ? 0xf74 : 0xf70);      // (vmcnt 0, 4: all that is written now, before the first of it is)
             }
             if (k < kHalf) {
                 ahead.s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[k / QB], q[x][k / QB], ahead.s[x], 0, 0, 0);
@@ -477,8 +524,8 @@ void prompt_tile_kernel(const PromptParams p) {
             if (k >= kSlots - 4 * QB && (k % QB) == 0) { const int j = (k - (kSlots - 4 * QB)) / QB; ahead.k[j] = key(k_next, j); }
             if (k >= kHalf && k < kHalf + 4) { if (k - kHalf < 2) write_k(kr, k_to, k - kHalf); else write_v(vr, v_to, k - kHalf - 2); }
             if constexpr (PAGED) {
-                if (k >= kHalf + 4 && k < kHalf + 6) kr.r[k - kHalf - 4] = __builtin_amdgcn_raw_buffer_load_b128(k == kHalf + 4 ? k_in : k_in2, tid * 16, 0, 0);
-                if (k >= kHalf + 6 && k < kHalf + 8) vr.r[k - kHalf - 6] = __builtin_amdgcn_raw_buffer_load_b128(k == kHalf + 6 ? v_in : v_in2, tid * 16, 0, 0);
+                if (k >= kHalf + 4 && k < kHalf + 6) kr.r[k - kHalf - 4] = load16(k_rows, k_place.at[k - kHalf - 4]);
+                if (k >= kHalf + 6 && k < kHalf + 8) vr.r[k - kHalf - 6] = load16(v_rows, v_now.at[k - kHalf - 6]);
             } else {
                 if (k >= kHalf + 4 && k < kHalf + 6) kr.r[k - kHalf - 4] = __builtin_amdgcn_raw_buffer_load_b128(k_in, tid * 16, (k - kHalf - 4) * 4096, 0);
                 if (k >= kHalf + 6 && k < kHalf + 8) vr.r[k - kHalf - 6] = __builtin_amdgcn_raw_buffer_load_b128(v_in, tid * 16, (k - kHalf - 6) * 4096, 0);
@@ -537,24 +584,19 @@ void prompt_tile_kernel(const PromptParams p) {
         int kt[kTiles], vt[kTiles];           // of the block's own tile, the next one, ..
 #pragma unroll
         for (int c = 0; c < kTiles; ++c) { kt[c] = c * kKTile; vt[c] = c * kVTile; }
-        Staged ks[kAheadK], vs[kAheadV];
-        Place pl[kAheadK + 1];
-        if constexpr (PAGED) {
+        if constexpr (!PAGED) {
 #pragma unroll
-            for (int c = 0; c <= kAheadK; ++c) pl[c] = place(b0 + c, c);
+            for (int c = 0; c < kAheadK; ++c) ks[c] = request(k_rows, b0 + c);
+#pragma unroll
+            for (int c = 0; c < kAheadV; ++c) vs[c] = request(v_rows, b0 + c);
         }
-#pragma unroll
-        for (int c = 0; c < kAheadK; ++c) ks[c] = PAGED ? request_at(k_rows, pl[c]) : request(k_rows, b0 + c);
-#pragma unroll
-        for (int c = 0; c < kAheadV; ++c) vs[c] = PAGED ? request_at(v_rows, pl[c]) : request(v_rows, b0 + c);
         for (int x = tid; x < kVBlock / 16; x += 256) *reinterpret_cast<u32x4*>(sV + (kRing - 1) * kVBlock + 16 * x) = u32x4{0u, 0u, 0u, 0u};      // (nothing lies behind the first block)
 #pragma unroll
         for (int c = 0; c < kAheadK; ++c) { write_k(ks[c], c * kKBlock, 0); write_k(ks[c], c * kKBlock, 1); }
 #pragma unroll
-        for (int c = 0; c < kAheadV; ++c) { clean(vs[c], b0 + c); write_v(vs[c], c * kVBlock, 0); write_v(vs[c], c * kVBlock, 1); }
-        kr = PAGED ? request_at(k_rows, pl[kAheadK]) : request(k_rows, b0 + kAheadK);
-        vr = PAGED ? request_at(v_rows, pl[kAheadV]) : request(v_rows, b0 + kAheadV);
-        Place v_even_at = pl[kAheadV + 1], v_odd_at = pl[kAheadV + 2];
+        for (int c = 0; c < kAheadV; ++c) { clean(vs[c], b0 + c, c); write_v(vs[c], c * kVBlock, 0); write_v(vs[c], c * kVBlock, 1); }
+        if constexpr (!PAGED) { kr[0] = request(k_rows, b0 + kAheadK); vr[0] = request(v_rows, b0 + kAheadV); }
+        Place v_even_at = pl[kAheadV + kDeep], v_odd_at = pl[kAheadV + kDeep + 1];
         int v_even = bytes_of(b0 + kAheadV + 1), v_odd = bytes_of(b0 + kAheadV + 2);
         k_next_rows += (int64_t)(lo + (b0 + kAheadK + 1) * kBlockRows) * kD; v_next_rows += (int64_t)(lo + (b0 + kAheadV + 1) * kBlockRows) * kD;
         __syncthreads();
@@ -564,11 +606,11 @@ void prompt_tile_kernel(const PromptParams p) {
         for (int i = b0; i < b1; i += 2) {
             constexpr int last = kTiles - 1;
             if constexpr (QB == 1) {
-                stage(even, odd, po, pe, i, v_even, v_even_at, kt[0] + kKBlock, kt[1], kt[1] + kKBlock, vt[last] + kVBlock, vt[0] + kVBlock, true, true);
-                stage(odd, even, pe, po, i + 1, v_odd, v_odd_at, kt[1], kt[1] + kKBlock, kt[0], vt[0], vt[1], true, true);
+                stage(even, odd, po, pe, kr[0], vr[0], i, v_even, v_even_at, kt[0] + kKBlock, kt[1], kt[1] + kKBlock, vt[last] + kVBlock, vt[0] + kVBlock, true, true);
+                stage(odd, even, pe, po, kr[kDeep - 1], vr[kDeep - 1], i + 1, v_odd, v_odd_at, kt[1], kt[1] + kKBlock, kt[0], vt[0], vt[1], true, true);
             } else {
-                stage(even, odd, po, pe, i, v_even, v_even_at, kt[0] + kKBlock, kt[1], kt[2 % kTiles], vt[last] + kVBlock, vt[1], true, false);
-                stage(odd, even, pe, po, i + 1, v_odd, v_odd_at, kt[1], kt[1] + kKBlock, kt[2 % kTiles] + kKBlock, vt[0], vt[1] + kVBlock, false, true);
+                stage(even, odd, po, pe, kr[0], vr[0], i, v_even, v_even_at, kt[0] + kKBlock, kt[1], kt[2 % kTiles], vt[last] + kVBlock, vt[1], true, false);
+                stage(odd, even, pe, po, kr[kDeep - 1], vr[kDeep - 1], i + 1, v_odd, v_odd_at, kt[1], kt[1] + kKBlock, kt[2 % kTiles] + kKBlock, vt[0], vt[1] + kVBlock, false, true);
             }
             const int k0 = kt[0], v0 = vt[0];
 #pragma unroll
@@ -630,6 +672,13 @@ void prompt_tile_kernel(const PromptParams p) {
                 *reinterpret_cast<uint2*>(to + 32 * d + 8 * r) =
                     make_uint2(pack_bf16(o[x][d][4 * r] * inv, o[x][d][4 * r + 1] * inv), pack_bf16(o[x][d][4 * r + 2] * inv, o[x][d][4 * r + 3] * inv));
     }
+}
+
+template <int QB, int CAP, bool SLOPE, int ROWS = kRowsPlain>
+__global__ __launch_bounds__(256, QB == 1 ? 2 : 1)
+void prompt_tile_kernel(const PromptParams p) {
+    __shared__ __attribute__((aligned(16))) unsigned char room[tile_lds(QB)];
+    prompt_tile<QB, CAP, SLOPE, ROWS>(p, blockIdx.x, room);
 }
 
 // ---- up to 16 rows in all ----
