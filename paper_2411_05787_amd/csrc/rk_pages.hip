@@ -3,6 +3,8 @@
 
 namespace rk {
 
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
 // ---- bounds of the scores ----
 // For a query q and a page whose keys lie between k_min and k_max in every dim,
 //     sum_d max(q_d k_min_d, q_d k_max_d) = sum_d max(q_d, 0) k_max_d + min(q_d, 0) k_min_d,
@@ -13,43 +15,77 @@ struct ScoreParams {
     const uint16_t* q; int64_t q_b, q_t;
     const uint16_t *k_min, *k_max;
     const int32_t *table, *seq_lens, *new_lens;
-    int32_t width, shift, n_pages, n_new, Hq, Hkv, G, agg, chunk, page_blocks;
+    int32_t width, shift, n_pages, n_new, batch, Hq, Hkv, G, agg, chunk, chunks, page_blocks;
     float scale;
     float* scores; int64_t s_stride;
     const int32_t* pred; int32_t pred_val;
 };
 
-// P: blocks of 16 pages to a wavefront.  One: the workgroup's wavefronts have 16 pages each.  Four, for many tokens: all have the same 64 and every
-// fourth four tokens, so that a query is read and its signs parted once for 64 pages.
-template <int P>
-__global__ __launch_bounds__(256, P == 1 ? 4 : 2)
+// P: blocks of 16 pages to a wavefront, all of whose bounds are requested at once.  TOKENS: the workgroup's wavefronts have the same pages and every fourth four
+// tokens, so that a query is read and its signs parted once for 16 P pages; otherwise they have pages of their own and all tokens.
+template <int P, bool TOKENS, int AGG>
+__global__ __launch_bounds__(256, P < 4 ? 4 : 2)
 void page_score_kernel(const ScoreParams p) {
-    const int g = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, gr = lane >> 4;
-    const int block = (int)(blockIdx.x % (uint32_t)p.page_blocks), t_first = (int)(blockIdx.x / (uint32_t)p.page_blocks) * p.chunk;
+    // Workgroups go round the 8 dies, eight of a KV head and then eight of the next: a head's bounds lie Hkv rows apart, which is few of an L2's channels, so
+    // that every die has all heads under way at once.
+    const uint32_t round = blockIdx.x >> 3, part = round / (uint32_t)p.Hkv * 8 + (blockIdx.x & 7u), part_b = part / (uint32_t)p.page_blocks;
+    const int g = (int)(round % (uint32_t)p.Hkv), lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, gr = lane >> 4;
+    const int block = (int)(part - part_b * (uint32_t)p.page_blocks), b = (int)(part_b / (uint32_t)p.chunks), t_first = (int)(part_b - b * (uint32_t)p.chunks) * p.chunk;
+    if (b >= p.batch) return;
     const int most = (int)min((int64_t)p.width, p.s_stride);      // pages that are looked at
-    const int j0 = block * 64 + (P == 1 ? w * 16 : 0);
+    const int j0 = TOKENS ? block * 16 * P : (block * 4 + w) * 16 * P;
     int page[P];                              // (requested before the sequence's length is known)
 #pragma unroll
-    for (int x = 0; x < P; ++x) {
-        const int j = j0 + 16 * x + n;
-        page[x] = p.table[(int64_t)b * p.width + min(j, p.width - 1)];
-        if (j >= most) page[x] = -1;
-    }
+    for (int x = 0; x < P; ++x) page[x] = p.table[(int64_t)b * p.width + min(j0 + 16 * x + n, p.width - 1)];
     if (p.pred != nullptr && p.pred[b] != p.pred_val) return;
     const int raw = p.seq_lens[b], n_tok = p.new_lens != nullptr ? min(max(p.new_lens[b], 0), p.n_new) : p.n_new;
     const int64_t start = (int64_t)raw - n_tok;
     const int t_end = min(t_first + p.chunk, n_tok);
     // pages that token i sees
     auto pages_of = [&](int i) { return (int)min(((start + i) >> p.shift) + 1, (int64_t)most); };
-    if (t_first >= t_end || start + t_end - 1 < 0 || j0 >= pages_of(t_end - 1)) return;
+    if (t_first >= t_end || start + t_end - 1 < 0) return;
+    const int some = pages_of(t_end - 1);     // that any of the tokens sees
+    if (j0 >= some) return;
     bf16x8 hi[P][4], lo[P][4];
+    if constexpr (TOKENS) {                   // by way of LDS: each bound is requested once, a row by 16 lanes
+        constexpr int kRow = kD * 2 + 16;     // (16 rows of an operand fall on different banks)
+        __shared__ __attribute__((aligned(16))) unsigned char sBounds[2][16 * P * kRow];
+        const int seg = (threadIdx.x & 15) * 16, row0 = threadIdx.x >> 4;
+        u32x4 u[2][P];
 #pragma unroll
-    for (int x = 0; x < P; ++x) {
-        const int64_t at = ((int64_t)((uint32_t)page[x] < (uint32_t)p.n_pages ? page[x] : 0) * p.Hkv + g) * kD + 8 * gr;
+        for (int x = 0; x < P; ++x) {         // row 16 x + row0 is page j0 + 16 x + row0
+            const int j = j0 + 16 * x + row0, pg = p.table[(int64_t)b * p.width + min(j, p.width - 1)];
+            const int64_t at = ((int64_t)((uint32_t)pg < (uint32_t)p.n_pages && j < some ? pg : 0) * p.Hkv + g) * (kD * 2) + seg;
+            u[0][x] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(p.k_max) + at);
+            u[1][x] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(p.k_min) + at);
+        }
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            hi[x][s] = *reinterpret_cast<const bf16x8*>(p.k_max + at + 32 * s);
-            lo[x][s] = *reinterpret_cast<const bf16x8*>(p.k_min + at + 32 * s);
+        for (int x = 0; x < P; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) *reinterpret_cast<u32x4*>(&sBounds[y][(16 * x + row0) * kRow + seg]) = u[y][x];
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < P; ++x)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                hi[x][s] = *reinterpret_cast<const bf16x8*>(&sBounds[0][(16 * x + n) * kRow + 64 * s + 16 * gr]);
+                lo[x][s] = *reinterpret_cast<const bf16x8*>(&sBounds[1][(16 * x + n) * kRow + 64 * s + 16 * gr]);
+            }
+    } else {
+#pragma unroll
+        for (int x = 0; x < P; ++x) {
+            const bool there = (uint32_t)page[x] < (uint32_t)p.n_pages && j0 + 16 * x + n < some;
+            const int64_t at = ((int64_t)(there ? page[x] : 0) * p.Hkv + g) * kD + 8 * gr;
+            if (x > 0 && j0 + 16 * x >= some) {       // (none of the block's pages is there)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) hi[x][s] = lo[x][s] = bf16x8{};
+                continue;
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                hi[x][s] = *reinterpret_cast<const bf16x8*>(p.k_max + at + 32 * s);
+                lo[x][s] = *reinterpret_cast<const bf16x8*>(p.k_min + at + 32 * s);
+            }
         }
     }
     const uint16_t* q0 = p.q + (int64_t)b * p.q_b + (int64_t)(g * p.G) * kD + 8 * gr;
@@ -59,25 +95,27 @@ void page_score_kernel(const ScoreParams p) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const u32x4*>(qr + 32 * s);
     };
-    const int step = P == 1 ? 4 : 16, t_mine = t_first + (P == 1 ? 0 : 4 * w);
+    constexpr int step = TOKENS ? 16 : 4;
+    const int t_mine = t_first + (TOKENS ? 4 * w : 0), heads = AGG == RK_AGG_FIRST ? 1 : p.G;
     if (t_mine < t_end) ask(t_mine, 0);
     for (int t0 = t_mine; t0 < t_end; t0 += step) {
         const int i = t0 + gr;
         float best[P];
-        bool none[P];
 #pragma unroll
-        for (int x = 0; x < P; ++x) { best[x] = -INFINITY; none[x] = false; }
-        for (int h0 = 0; h0 < p.G; h0 += 4) {
+        for (int x = 0; x < P; ++x) best[x] = AGG == RK_AGG_MAX ? -INFINITY : 0.f;
+        for (int h0 = 0; h0 < heads; h0 += 4) {
             u32x4 up[4], down[4];
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t negative = ((q[s][e] & 0x80008000u) >> 15) * 0xffffu;      // the halves whose sign is set, in full
-                    down[s][e] = q[s][e] & negative;
-                    up[s][e] = q[s][e] & ~negative;
+                    const uint32_t word = q[s][e];
+                    const s16x2 signs = __builtin_bit_cast(s16x2, word) >> 15;        // (a half in full where it is set)
+                    const uint32_t negative = __builtin_bit_cast(uint32_t, signs);
+                    down[s][e] = word & negative;
+                    up[s][e] = word & ~negative;
                 }
-            const bool more = h0 + 4 < p.G;
+            const bool more = h0 + 4 < heads;
             ask(more ? t0 : min(t0 + step, t_end - 1), more ? h0 + 4 : 0);       // (the next one's, beside the products)
             f32x4 acc[P];
 #pragma unroll
@@ -89,27 +127,31 @@ void page_score_kernel(const ScoreParams p) {
 #pragma unroll
                 for (int x = 0; x < P; ++x) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, down[s]), lo[x][s], acc[x], 0, 0, 0);
             }
+            // (heads beyond the group repeat its last one: once more for a maximum, nothing for a sum)
 #pragma unroll
             for (int x = 0; x < P; ++x)
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    if (h0 + y < p.G) {
-                        const float one = acc[x][y] * p.scale;
-                        best[x] = aggregate(best[x], one, h0 + y, p.agg);
-                        none[x] = none[x] || (one != one && (h0 + y == 0 || p.agg != RK_AGG_FIRST));      // (a maximum would pass over it)
-                    }
+                for (int y = 0; y < 4; ++y) {
+                    const float one = acc[x][y] * p.scale;
+                    if constexpr (AGG == RK_AGG_MAX) best[x] = __builtin_elementwise_maximum(best[x], one);      // (no number stays none)
+                    else if constexpr (AGG == RK_AGG_MEAN) { if (h0 + y < p.G) best[x] += one; }
+                    else if (y == 0) best[x] = one;
+                }
         }
         if (i >= t_end || start + i < 0) continue;
         const int seen = pages_of(i);
         float* to = p.scores + (((int64_t)b * p.n_new + i) * p.Hkv + g) * p.s_stride + j0 + n;
 #pragma unroll
         for (int x = 0; x < P; ++x) {
-            if (p.agg == RK_AGG_MEAN) best[x] /= (float)p.G;
-            if (none[x]) best[x] = __uint_as_float(0x7fc00000u);
+            if constexpr (AGG == RK_AGG_MEAN) best[x] /= (float)p.G;
             if ((uint32_t)page[x] >= (uint32_t)p.n_pages) best[x] = -INFINITY;
             if (j0 + 16 * x + n < seen) to[16 * x] = best[x];
         }
     }
+}
+using ScoreKernel = void (*)(const ScoreParams);
+template <int P, bool TOKENS> static ScoreKernel score_kernel(int agg) {
+    return agg == RK_AGG_MAX ? page_score_kernel<P, TOKENS, RK_AGG_MAX> : agg == RK_AGG_MEAN ? page_score_kernel<P, TOKENS, RK_AGG_MEAN> : page_score_kernel<P, TOKENS, RK_AGG_FIRST>;
 }
 
 // ---- the pages with the largest ----
@@ -147,22 +189,24 @@ __device__ __forceinline__ uint32_t select_key(const SelectParams& p, const Sele
 template <int W, int R>
 __global__ __launch_bounds__(W * 64)
 void page_select_kernel(const SelectParams p) {
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // (the whole row of scores, requested before its token's pages are known)
+    float s[R];
+    const float* scores = p.scores + (int64_t)blockIdx.x * p.s_stride;
+#pragma unroll
+    for (int r = 0; r < R; ++r) s[r] = scores[min((w * R + r) * 64 + lane, (int)p.s_stride - 1)];
+    __builtin_amdgcn_sched_barrier(0);
     const SelectRow row = select_row(p, (int)blockIdx.x);
     if (row.wanted < 0) return;
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = row.n, k = row.wanted;
+    const int n = row.n, k = row.wanted;
     for (int x = k + tid; x < p.k; x += W * 64) row.idx[x] = -1;
     if (k == n) {
         for (int x = tid; x < n; x += W * 64) row.idx[x] = x;
         return;
     }
     uint32_t x[R];
-    {
-        float s[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r] = row.scores[min((w * R + r) * 64 + lane, n - 1)];
-#pragma unroll
-        for (int r = 0; r < R; ++r) { const int j = (w * R + r) * 64 + lane; x[r] = j < n ? select_key(p, row, j, s[r]) : 0u; }
-    }
+    for (int r = 0; r < R; ++r) { const int j = (w * R + r) * 64 + lane; x[r] = j < n ? select_key(p, row, j, s[r]) : 0u; }
     __shared__ int sCount[2][W], sBase[W][2];
     int turn = 0;
     // keys of the row at or above v
@@ -296,16 +340,24 @@ extern "C" int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stri
     p.scale = geom->scale; p.scores = scores; p.s_stride = s_stride;
     p.pred = pred; p.pred_val = pred_val;
     const int64_t most = table_width < s_stride ? table_width : s_stride;
-    p.page_blocks = (int)((most + 63) / 64);
-    const int64_t wgs = (int64_t)p.page_blocks * p.Hkv * geom->batch;
+    const int64_t pairs = (int64_t)p.Hkv * geom->batch;
     const bool many = n_new >= 16;
+    // pages to a workgroup: few tokens, 64 or, where those of all pairs still fill the chip, 256
+    const bool wide = many || pairs * ((most + 255) / 256) >= kComputeUnits;
+    const int per = many || !wide ? 64 : 256;
+    p.page_blocks = (int)((most + per - 1) / per);
+    const int64_t wgs = p.page_blocks * pairs;
     const int unit = many ? 16 : 4;           // tokens of a workgroup's round
-    int64_t chunks = (many ? 2 : 4) * kComputeUnits / wgs;
+    int64_t chunks = 2 * kComputeUnits / wgs;
     if (chunks > (n_new + unit - 1) / unit) chunks = (n_new + unit - 1) / unit;
     if (chunks < 1) chunks = 1;
     p.chunk = (int)(((n_new + chunks - 1) / chunks + unit - 1) / unit * unit);
-    chunks = (n_new + p.chunk - 1) / p.chunk;
-    hipLaunchKernelGGL((many ? page_score_kernel<4> : page_score_kernel<1>), dim3((unsigned)(p.page_blocks * chunks), p.Hkv, geom->batch), dim3(256), 0, (hipStream_t)stream, p);
+    p.chunks = (int)((n_new + p.chunk - 1) / p.chunk);
+    p.batch = geom->batch;
+    const int64_t total = ((int64_t)p.page_blocks * p.chunks * p.batch + 7) / 8 * 8 * p.Hkv;
+    if (total > INT32_MAX / 256) return RK_ERR_UNSUPPORTED;
+    auto kernel = many ? score_kernel<4, true>(agg) : wide ? score_kernel<4, false>(agg) : score_kernel<1, false>(agg);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(256), 0, (hipStream_t)stream, p);
     return launch_status();
 }
 
@@ -324,7 +376,7 @@ extern "C" int rk_page_select(const rk_geom* geom, const float* scores, int64_t 
     p.shift = page_shift(page); p.n_new = n_new; p.Hkv = geom->n_kv_heads; p.k = k; p.keep_first = keep_first; p.keep_last = keep_last;
     p.idx = idx; p.pred = pred; p.pred_val = pred_val;
     const int64_t n = s_stride;
-    auto kernel = n <= 256 ? page_select_kernel<1, 4> : n <= 512 ? page_select_kernel<1, 8> : n <= 1024 ? page_select_kernel<1, 16> : n <= 4096 ? page_select_kernel<4, 16>
+    auto kernel = n <= 192 ? page_select_kernel<1, 3> : n <= 384 ? page_select_kernel<1, 6> : n <= 640 ? page_select_kernel<1, 10> : n <= 1024 ? page_select_kernel<1, 16> : n <= 4096 ? page_select_kernel<4, 16>
                   : n <= kSelectMost ? page_select_kernel<16, 16> : page_select_long_kernel;
     const int threads = n <= 1024 ? 64 : n <= 4096 ? 256 : n <= kSelectMost ? 1024 : kSelectThreads;
     hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, (hipStream_t)stream, p);
