@@ -204,10 +204,12 @@ __device__ __forceinline__ void tile_output(const TileRows<FORMAT>& t, ColState&
 }
 
 // The workgroup's columns < ncols <= C merged over its W wavefronts: calls put(column, dim, o0, o1, L) for the pairs of dims (the unnormalised
-// output against the common maximum, and its sum) and stat(column, m, l).  tid: the thread's number among the W wavefronts'.
+// output against the common maximum, and its sum) and stat(column, m, l).  tid: the thread's number among the W wavefronts';
+// unit: kLog2e where maxima are in natural units, 1 where they are in those of ln 2.
 template <int W, int C> struct ColMergeLds { float m[W][16], l[W][16]; float o[W][C][kD]; };
 template <int W, int C, class Put, class Stat>
-__device__ __forceinline__ void merge_columns(ColMergeLds<W, C>& lds, ColState& st, int ncols, Put&& put, Stat&& stat, const int tid = (int)threadIdx.x) {
+__device__ __forceinline__ void merge_columns(ColMergeLds<W, C>& lds, ColState& st, int ncols, Put&& put, Stat&& stat, const int tid = (int)threadIdx.x,
+                                              const float unit = kLog2e) {
     const int lane = tid & 63, w = tid >> 6, n = lane & 15, g = lane >> 4;
     const float l = sum_xor32(sum_xor16(st.l));
     if (g == 0) { lds.m[w][n] = st.m; lds.l[w][n] = l; }
@@ -228,7 +230,7 @@ __device__ __forceinline__ void merge_columns(ColMergeLds<W, C>& lds, ColState& 
         float L = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            const float a = lds.m[i][c] == -INFINITY ? 0.f : fast_exp2((lds.m[i][c] - M) * kLog2e);
+            const float a = lds.m[i][c] == -INFINITY ? 0.f : fast_exp2((lds.m[i][c] - M) * unit);
             const float2 v = *reinterpret_cast<const float2*>(&lds.o[i][c][d]);
             // (a wavefront without rows has nothing; NaN statistics stay NaN)
             L = fmaf(a, lds.l[i][c], L); o0 = fmaf(a, v.x, o0); o1 = fmaf(a, v.y, o1);

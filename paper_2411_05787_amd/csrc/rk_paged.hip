@@ -28,6 +28,15 @@ __device__ __forceinline__ PartRow part_row(const PartSource& s, const PromptPar
 // prompt_cols_kernel over units of 16 rows: each is a buffer of its own inside its page.  A wavefront looks its next 64 tiles up at once, a lane each, and
 // takes the page numbers from the lanes: no wait for a number of the table stands before a request.  SUB: pairs side by side in a workgroup, W wavefronts and a
 // room each; all of its wavefronts come to one barrier, also those that have nothing to do (there: x0 < 0).
+// The running maximum is in units of ln 2 and follows the true one only when that has grown by more than 8 (see prompt_tile).  A chosen token's rows are no more
+// than 8: the upper eight columns repeat them, and hold the weights' low parts beside the high ones of the lower, so that one matrix instruction takes both; and as
+// tokens share rows, which come out of the L2 then, its keys are read in whole rows and turned into the operand's layout by way of LDS: straight into it, every 16
+// lanes of a request touch 16 lines (500 tokens of 28 heads over 4, 32 pages of 64 rows each: @@ us).
+constexpr int kTurnRow = kD * 2 + 16, kTurn = kTileRows * kTurnRow;      // (rows of LDS: 16 of an operand fall on different banks)
+template <int W, int ROWS> constexpr int cols_lds() {
+    constexpr int merge = (int)sizeof(ColMergeLds<W, 16>), turn = ROWS == kRowsChosen ? W * kTurn : 0;
+    return merge > turn ? merge : turn;
+}
 template <int W, int CAP, bool SLOPE, int ROWS, int SUB = 1>
 __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, const int y0, const int z0, unsigned char* room) {
     auto leave = [&]() { if constexpr (SUB > 1) __syncthreads(); };
@@ -60,8 +69,9 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
     const bool partial = p.splits > 1 || p.joined != 0;
     if (!CHOSEN && partial && split == 0 && tid == 0) { p.parts[2 * bg] = slot; p.parts[2 * bg + 1] = parts; }
     const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, gr = lane >> 4;
-    bool real = col < n_rows;
-    const int r0 = (CHOSEN ? token * p.G : 0) + min(col, n_rows - 1);
+    const int mine = CHOSEN ? col & 7 : col;
+    bool real = mine < n_rows;
+    const int r0 = (CHOSEN ? token * p.G : 0) + min(mine, n_rows - 1);
     const Query me = SHARED ? shared_query(p, g, r0, real) : paged_query<ROWS>(p, tok, b, g, r0);
     const bool some = real && me.lo < me.hi;
     const int seen = wave_min(some ? me.lo : INT32_MAX), hi = wave_max_i(some ? me.hi : INT32_MIN);
@@ -74,16 +84,22 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
 #pragma unroll
     for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const bf16x8*>(qr + operand_dim<false>(s, gr));
     __builtin_amdgcn_sched_barrier(0);
-    const ScoreForm form = score_form<CAP>(p, 1.f);       // (natural units, as the columns' running state has them)
-    const float slope = SLOPE && p.slopes != nullptr ? p.slopes[me.head] : 0.f;
+    ScoreForm form = score_form<CAP>(p, kLog2e);
+    if (!SLOPE && form.a < 0.f) {             // raw products are compared below: their order has to be the scores'
+        form.a = -form.a;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) q[s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[s]) ^ 0x80008000u);
+    }
+    const float slope = SLOPE && p.slopes != nullptr ? p.slopes[me.head] * kLog2e : 0.f;
     const uint16_t* k = p.k + (int64_t)g * p.s_h;
     const uint16_t* v = p.v + (int64_t)g * p.s_h;
     const int32_t* table = p.table + (SHARED ? 0 : (int64_t)b * p.width);
     const int32_t* idx = CHOSEN ? p.idx + (((int64_t)b * p.n_new + token) * p.Hkv + g) * p.n_idx : nullptr;
     const int step = parts * W, in_page = (1 << p.shift) - 1;
 
-    // this lane's of the wavefront's next 64 tiles: each unit's page (-1: none) and first row
-    int page[2], first[2];
+    // this lane's of the wavefront's next 64 tiles: each unit's first row, and where it is in bytes from the head's first page (the highest bit: there is none)
+    int first[2];
+    uint32_t at_lo[2], at_hi[2];
     auto look = [&](int t) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -101,30 +117,34 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
                 first[c] = there ? (int)at : 0;
                 j = there ? j : 0;
             }
-            const int x = there ? table[j] : -1;
-            page[c] = (uint32_t)x < (uint32_t)p.n_pages ? x : -1;
+            const int page = there ? table[j] : -1;
+            there = (uint32_t)page < (uint32_t)p.n_pages;
+            const uint64_t where = there ? (uint64_t)page * (uint64_t)(p.s_p * 2) + (uint32_t)((first[c] & in_page) * (kD * 2)) : 0;
+            at_lo[c] = (uint32_t)where;
+            at_hi[c] = (uint32_t)(where >> 32) | (there ? 0u : 0x80000000u);
         }
-        asm volatile("" : "+v"(page[0]), "+v"(page[1]));      // (here before the loop goes on: see request_keys)
+        // (here before the loop goes on: a request that may be in flight or not would be waited for with all others)
+        asm volatile("" : "+v"(at_lo[0]), "+v"(at_hi[0]), "+v"(at_lo[1]), "+v"(at_hi[1]));
     };
-    // A tile: its units' first rows, how many rows of each there are (0: none), and where they are in elements from the head's first page.
+    // A tile: its units' first rows, how many rows of each there are (0: none), and where they are in bytes from the head's first page.
     struct Tile { int row[2], rows[2]; int64_t at[2]; };
     auto tile_at = [&](int n) {
         Tile x;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            const int pg = __builtin_amdgcn_readlane(page[c], n);
+            const uint32_t hi32 = __builtin_amdgcn_readlane(at_hi[c], n);
             x.row[c] = __builtin_amdgcn_readlane(first[c], n);
             int rows = min(hi - x.row[c], 16);
             asm("" : "+s"(rows));
-            rows = max(rows, 0) & ~(pg >> 31);
+            rows = max(rows, 0) & ~((int)hi32 >> 31);
             asm("" : "+s"(rows));             // (no branch)
             x.rows[c] = rows;
-            x.at[c] = (int64_t)max(pg, 0) * p.s_p + (int64_t)((x.row[c] & in_page) * kD);
+            x.at[c] = (int64_t)((uint64_t)(hi32 & 0x7fffffffu) << 32 | (uint32_t)__builtin_amdgcn_readlane(at_lo[c], n));
         }
         return x;
     };
     auto buffer = [&](const uint16_t* base, const Tile& x, int c) {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base + x.at[c]), 0, x.rows[c] * (kD * 2), 0x00020000);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(base) + x.at[c]), 0, x.rows[c] * (kD * 2), 0x00020000);
     };
     constexpr int kAux = CHOSEN ? 0 : kStreamAux;
     TileRows<kBf16> rows;
@@ -133,7 +153,7 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
         for (int c = 0; c < 2; ++c) {
             const __amdgpu_buffer_rsrc_t r = buffer(k, x, c);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) rows.k[c][s] = __builtin_amdgcn_raw_buffer_load_b128(r, col * (kD * 2) + operand_dim<false>(s, gr) * 2, 0, kAux);
+            for (int s = 0; s < 4; ++s) rows.k[c][s] = CHOSEN ? __builtin_amdgcn_raw_buffer_load_b128(r, (4 * gr + s) * (kD * 2) + 16 * col, 0, kAux) : __builtin_amdgcn_raw_buffer_load_b128(r, col * (kD * 2) + operand_dim<false>(s, gr) * 2, 0, kAux);
         }
     };
     auto ask_values = [&](const Tile& x) {
@@ -158,6 +178,15 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
     queries_here(q);
     for (; t < tiles; t += step) {
         float s[2][4];
+        if constexpr (CHOSEN) {
+            unsigned char* turn = room + w * kTurn;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) *reinterpret_cast<u32x4*>(turn + (16 * (e >> 2) + 4 * gr + (e & 3)) * kTurnRow + 16 * col) = rows.k[e >> 2][e & 3];
+            wave_lds_sync();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rows.k[e >> 2][e & 3] = *reinterpret_cast<const u32x4*>(turn + (16 * (e >> 2) + col) * kTurnRow + 64 * (e & 3) + 16 * gr);
+            wave_lds_sync();
+        }
         tile_scores<kBf16>(rows, q, s);
         if (++n == 64) { look(t + step); n = 0; }
         const Tile next = tile_at(n);         // (past the last tile: nothing)
@@ -166,8 +195,8 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[x][i] = fmaf(bend<CAP>(s[x][i], form), form.a, form.b);
-                if constexpr (SLOPE) s[x][i] = fmaf(-slope, fabsf((float)(me.pos - now.row[x] - 4 * gr) - (float)i), s[x][i]);
+                s[x][i] = bend<CAP>(s[x][i], form);
+                if constexpr (SLOPE) s[x][i] = fmaf(-slope, fabsf((float)(me.pos - now.row[x] - 4 * gr) - (float)i), fmaf(s[x][i], form.a, form.b));
             }
         // (one sign of them all, and no branch for each)
         const int inside = min(min(now.rows[0], now.rows[1]) - 16, min(min(now.row[0], now.row[1]) - in_lo, in_hi - 16 - max(now.row[0], now.row[1])));
@@ -180,9 +209,30 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[x][i] = sees(x, now.row[x] + 4 * gr + i) ? s[x][i] : -INFINITY;
         }
-        tile_softmax(st, s);
+        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        mx = max_xor32(max_xor16(mx));
+        if constexpr (!SLOPE) mx = fmaf(mx, form.a, form.b);
+        if (__any(mx > st.m + 8.f)) {
+            const float to = mx > st.m + 8.f ? mx : st.m, alpha = to == -INFINITY ? 1.f : fast_exp2(st.m - to);
+            st.m = to;
+            st.l *= alpha;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) st.o[i] *= alpha;
+        }
+        const float from = (SLOPE ? 0.f : form.b) - (st.m == -INFINITY ? 0.f : st.m);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { s[x][i] = fast_exp2(SLOPE ? s[x][i] + from : fmaf(s[x][i], form.a, from)); st.l += s[x][i]; }
         bf16x8 ph, pl;
         weight_operands(s, ph, pl);
+        if constexpr (CHOSEN) {
+            const u32x4 h = __builtin_bit_cast(u32x4, ph), l = __builtin_bit_cast(u32x4, pl);
+            u32x4 both;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) both[e] = col < 8 ? h[e] : l[e];
+            ph = __builtin_bit_cast(bf16x8, both);
+        }
         bool bad = false;
         if (masked) {
 #pragma unroll
@@ -192,15 +242,25 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
                 for (int e = 0; e < 8; ++e) drop_non_finite(rows.v[e]);
             }
         }
-        tile_output<kBf16>(rows, st, ph, pl);
+        if constexpr (CHOSEN) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 o[4];
+                value_operands<kBf16>(rows, h, o);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st.o[4 * h + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o[i]), ph, st.o[4 * h + i], 0, 0, 0);
+            }
+        } else {
+            tile_output<kBf16>(rows, st, ph, pl);
+        }
         if (__any(bad)) {
 #pragma unroll
             for (int x = 0; x < 2; ++x)
                 for (int i = 0; i < now.rows[x]; ++i) {
-                    if (!sees(x, now.row[x] + i)) continue;
+                    if (!sees(x, now.row[x] + i) || (CHOSEN && col >= 8)) continue;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const u32x4 u = *reinterpret_cast<const u32x4*>(v + now.at[x] + (int64_t)i * kD + 8 * (4 * gr + r));
+                        const u32x4 u = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(v) + now.at[x] + (int64_t)i * (kD * 2) + 16 * (4 * gr + r));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             st.o[2 * e][r] += only_non_finite(bf16_lo(u[e]));
@@ -213,6 +273,13 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
         now = next;
     }
 
+    if constexpr (CHOSEN) {                   // the low parts' products to the high ones'
+        __syncthreads();                      // (other wavefronts' keys are in the room still)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st.o[i][r] += dpp_move_f<kDppRor8>(st.o[i][r]);
+    }
     ColMergeLds<W, 16>& lds = *reinterpret_cast<ColMergeLds<W, 16>*>(room);
     if (partial) {
         // (columns of one pair and part side by side)
@@ -222,8 +289,8 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
                           *reinterpret_cast<float2*>(p.part_o + (at + x) * kD + d) = make_float2(o0, o1);
                       },
                       [&](int x, float m, float l) {
-                          *reinterpret_cast<float2*>(p.part_ml + (at + x) * 2) = make_float2(m * kLog2e, l);
-                      }, tid);
+                          *reinterpret_cast<float2*>(p.part_ml + (at + x) * 2) = make_float2(m, l);
+                      }, tid, 1.f);
         return;
     }
     if constexpr (SHARED || SUB > 1) return;  // (never: those results are joined)
@@ -234,8 +301,8 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
                   [&](int x, int d, float o0, float o1, float) { o[x * kD + d] = o0; o[x * kD + d + 1] = o1; },
                   [&](int x, float m, float l) {
                       sInv[x] = l == 0.f ? 0.f : 1.f / l;
-                      if (p.lse != nullptr) p.lse[out_row(x)] = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l) * (1.f / kLog2e);
-                  });
+                      if (p.lse != nullptr) p.lse[out_row(x)] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.f / kLog2e);
+                  }, tid, 1.f);
     __syncthreads();
     for (int x = threadIdx.x; x < n_rows * (kD / 2); x += W * 64) {
         const int r = x / (kD / 2), d = 2 * (x % (kD / 2));
@@ -246,7 +313,7 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
 template <int W, int CAP, bool SLOPE, int ROWS>
 __global__ __launch_bounds__(W * 64, W == kColWaves ? 2 : 1)
 void paged_cols_kernel(const PromptParams p) {
-    __shared__ __attribute__((aligned(16))) unsigned char room[sizeof(ColMergeLds<W, 16>)];
+    __shared__ __attribute__((aligned(16))) unsigned char room[cols_lds<W, ROWS>()];
     paged_cols<W, CAP, SLOPE, ROWS>(p, (int)blockIdx.x, (int)blockIdx.y, (int)blockIdx.z, room);
 }
 
