@@ -15,7 +15,7 @@ struct ScoreParams {
     const uint16_t* q; int64_t q_b, q_t;
     const uint16_t *k_min, *k_max;
     const int32_t *table, *seq_lens, *new_lens;
-    int32_t width, shift, n_pages, n_new, batch, Hq, Hkv, G, agg, chunk, chunks, page_blocks;
+    int32_t width, shift, n_pages, n_new, Hq, Hkv, G, agg, chunk, chunks, page_blocks;
     float scale;
     float* scores; int64_t s_stride;
     const int32_t* pred; int32_t pred_val;
@@ -26,12 +26,9 @@ struct ScoreParams {
 template <int P, bool TOKENS, int AGG>
 __global__ __launch_bounds__(256, P < 4 ? 4 : 2)
 void page_score_kernel(const ScoreParams p) {
-    // Workgroups go round the 8 dies, eight of a KV head and then eight of the next: a head's bounds lie Hkv rows apart, which is few of an L2's channels, so
-    // that every die has all heads under way at once.
-    const uint32_t round = blockIdx.x >> 3, part = round / (uint32_t)p.Hkv * 8 + (blockIdx.x & 7u), part_b = part / (uint32_t)p.page_blocks;
-    const int g = (int)(round % (uint32_t)p.Hkv), lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, gr = lane >> 4;
+    const uint32_t part = blockIdx.x / (uint32_t)p.Hkv, part_b = part / (uint32_t)p.page_blocks;
+    const int g = (int)(blockIdx.x - part * (uint32_t)p.Hkv), lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, gr = lane >> 4;
     const int block = (int)(part - part_b * (uint32_t)p.page_blocks), b = (int)(part_b / (uint32_t)p.chunks), t_first = (int)(part_b - b * (uint32_t)p.chunks) * p.chunk;
-    if (b >= p.batch) return;
     const int most = (int)min((int64_t)p.width, p.s_stride);      // pages that are looked at
     const int j0 = TOKENS ? block * 16 * P : (block * 4 + w) * 16 * P;
     int page[P];                              // (requested before the sequence's length is known)
@@ -353,8 +350,7 @@ extern "C" int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stri
     if (chunks < 1) chunks = 1;
     p.chunk = (int)(((n_new + chunks - 1) / chunks + unit - 1) / unit * unit);
     p.chunks = (int)((n_new + p.chunk - 1) / p.chunk);
-    p.batch = geom->batch;
-    const int64_t total = ((int64_t)p.page_blocks * p.chunks * p.batch + 7) / 8 * 8 * p.Hkv;
+    const int64_t total = (int64_t)p.page_blocks * p.chunks * geom->batch * p.Hkv;
     if (total > INT32_MAX / 256) return RK_ERR_UNSUPPORTED;
     auto kernel = many ? score_kernel<4, true>(agg) : wide ? score_kernel<4, false>(agg) : score_kernel<1, false>(agg);
     hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(256), 0, (hipStream_t)stream, p);
