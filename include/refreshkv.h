@@ -739,7 +739,7 @@ int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64
  * table[b * table_width + r / page]; the calls below take the table (device int32 [batch, table_width]) beside the pool.  Sequences may name
  * the same pages (a prefix that they share) as long as none is appended to.  A number outside [0, n_pages) names no page: rows there are not
  * written, and nobody sees them.  Rows from table_width * page on do not exist.
- *   k, v         bf16 [n_pages, n_kv_heads, page, 128], strides in elements (non-negative multiples of 8, below 2^40), 16-byte aligned
+ *   k, v         bf16 [n_pages, n_kv_heads, page, 128], strides in elements (non-negative multiples of 8, the pool within 2^46 of them), 16-byte aligned
  *   k_min, k_max bf16 [n_pages, n_kv_heads, 128] contiguous, 16-byte aligned, or both NULL: the least and the largest of a page's keys in each dim, in
  *                the order -NaN < -infinity < .. < -0 < +0 < .. < +infinity < NaN (rk_rope_append_paged keeps them, rk_page_scores reads them)
  *   page         16, 32, 64 or 128 (RK_ERR_UNSUPPORTED otherwise) */

@@ -351,7 +351,7 @@ extern "C" int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stri
     p.chunk = (int)(((n_new + chunks - 1) / chunks + unit - 1) / unit * unit);
     p.chunks = (int)((n_new + p.chunk - 1) / p.chunk);
     const int64_t total = (int64_t)p.page_blocks * p.chunks * geom->batch * p.Hkv;
-    if (total > INT32_MAX / 256) return RK_ERR_UNSUPPORTED;
+    if (!fits_launch(total, 256)) return RK_ERR_UNSUPPORTED;
     auto kernel = many ? score_kernel<4, true>(agg) : wide ? score_kernel<4, false>(agg) : score_kernel<1, false>(agg);
     hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(256), 0, (hipStream_t)stream, p);
     return launch_status();
@@ -366,7 +366,7 @@ extern "C" int rk_page_select(const rk_geom* geom, const float* scores, int64_t 
     if (((uintptr_t)scores & 3u) || ((uintptr_t)idx & 3u)) return RK_ERR_INVALID_ARG;
     if (page != 16 && page != 32 && page != 64 && page != 128) return RK_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)geom->batch * n_new * geom->n_kv_heads;
-    if (rows > INT32_MAX / 2) return RK_ERR_UNSUPPORTED;
+    if (!fits_launch(rows, 1024)) return RK_ERR_UNSUPPORTED;
     SelectParams p{};
     p.scores = scores; p.s_stride = s_stride; p.seq_lens = seq_lens; p.new_lens = new_lens;
     p.shift = page_shift(page); p.n_new = n_new; p.Hkv = geom->n_kv_heads; p.k = k; p.keep_first = keep_first; p.keep_last = keep_last;

@@ -479,7 +479,7 @@ extern "C" int rk_rope_append_paged(const rk_geom* geom, const rk_new_rows* rows
     p.rows_per_token = (rows->q ? p.Hq : 0) + (bounds ? 1 : 2) * p.Hkv;
     const int64_t touched = ((int64_t)p.n_new + pages->page - 2) / pages->page + 1;       // pages that n_new rows can touch
     const int64_t page_wgs = bounds ? touched * p.Hkv : 0, row_wgs = ((int64_t)p.n_new * p.rows_per_token + 31) / 32;
-    if (page_wgs + row_wgs * 32 > INT32_MAX) return RK_ERR_UNSUPPORTED;
+    if (!fits_launch(page_wgs + row_wgs, 256)) return RK_ERR_UNSUPPORTED;
     if (turned_over_others(geom, rows, q_out)) return RK_ERR_INVALID_ARG;
     p.block_wgs = (int32_t)page_wgs;
     auto kernel = bounds ? rope_append_paged_kernel<true> : rope_append_paged_kernel<false>;

@@ -276,6 +276,9 @@ PAGED = {
     "split_rows": dict(B=1, Hq=2, H=1, T=40, lens=[5000], new=None, page=16),
     "split_far_cap": dict(B=1, Hq=2, H=1, T=33, lens=[2500], new=None, page=32, masks="docs", cap=500.0),
     "beyond_the_table": dict(B=1, Hq=2, H=1, T=30, lens=[100], new=None, page=16, width=6),
+    "step_negative": dict(B=3, Hq=4, H=2, T=1, lens=[-5, 40, -2 ** 31], new=None, page=16, slopes=True),
+    "drafted_short": dict(B=2, Hq=4, H=1, T=4, lens=[2, 40], new=None, page=16),                    # more new tokens than rows
+    "chunk_negative": dict(B=3, Hq=4, H=2, T=50, lens=[-2 ** 31, 20, 90], new=None, page=32, cap=3.0),
 }
 
 
@@ -330,6 +333,8 @@ SPARSE = {
     "many": dict(B=1, Hq=1, H=1, T=2, lens=[9000], new=None, page=16, k=400),
     "beyond_the_table": dict(B=1, Hq=2, H=1, T=1, lens=[300], new=None, page=32, width=5, k=4),
     "no_tokens": dict(B=2, Hq=2, H=1, T=2, lens=[0, 40], new=[0, 2], page=32, k=2),
+    "negative": dict(B=3, Hq=4, H=2, T=3, lens=[-9, 2, -2 ** 31], new=None, page=16, k=2),
+    "eight_heads": dict(B=2, Hq=16, H=2, T=3, lens=[200, 190], new=None, page=16, k=5),
 }
 
 
@@ -363,6 +368,11 @@ PREFIX = {
     "many_rows": dict(B=70, Hq=8, H=1, T=1, lens=[300 + 3 * i for i in range(70)], new=None, page=32, prefix=300),
     "long": dict(B=3, Hq=2, H=2, T=1, lens=[9100, 9001, 9050], new=None, page=16, prefix=9000),
     "no_prefix": dict(B=2, Hq=4, H=2, T=1, lens=[100, 50], new=None, page=16, prefix=0),
+    "both_ways": dict(B=3, Hq=4, H=2, T=20, lens=[200, 150, 120], new=None, page=16, prefix=90, masks="both_ways"),
+    "documents": dict(B=6, Hq=4, H=1, T=7, lens=[200, 150, 120, 99, 200, 140], new=None, page=32, prefix=90, masks="docs", slopes=True),
+    "negative": dict(B=3, Hq=4, H=2, T=2, lens=[-7, 150, -2 ** 31], new=None, page=16, prefix=90),
+    "many_pairs": dict(B=80, Hq=16, H=8, T=1, lens=[100 + i for i in range(80)], new=None, page=16, prefix=100),
+    "many_pairs_odd": dict(B=129, Hq=2, H=2, T=1, lens=[60 + 2 * i for i in range(129)], new=[i % 2 for i in range(129)], page=16, prefix=33),
 }
 
 
@@ -379,3 +389,41 @@ def test_prefix(rk, name):
     rk.rk_prefix_attn(geom, q, pages, pt, i32([x.prefix]), P, table, lens, own, out, lse=lse, workspace=rk.PrefixWorkspace(geom, x.T, P, own), **args)
     torch.cuda.synchronize()
     x.check(out, lse, x.B * x.T * x.G <= 16, name)
+
+
+@gpu
+def test_prefix_length_is_bounded(rk):
+    """*prefix_len beyond max_prefix counts as that, a negative one as 0; max_own bounds the rows behind it."""
+    x = Inputs(B=3, Hq=4, H=2, T=1, lens=[200, 150, 96], new=None, page=16, prefix=96)
+    geom, pages, q, table, lens, args = x.device(rk)
+    ws = rk.PrefixWorkspace(geom, 1, 96, 200)
+    pt = i32(x.prefix_table)
+
+    def run(value, most, own):
+        out, lse = x.blank()
+        rk.rk_prefix_attn(geom, q, pages, pt, i32([value]), most, table, lens, own, out, lse=lse, workspace=ws, **args)
+        return out, lse
+    for a, b in ((run(10 ** 9, 96, 200), run(96, 96, 200)), (run(-5, 96, 200), run(0, 96, 200)), (run(96, 80, 200), run(80, 96, 200))):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    out, lse = run(96, 96, 30)                                                   # rows 126 and on are not seen
+    args["end"] = i32([[min(n, 126)] for n in x.lens])
+    args["first"] = i32([[0]] * 3)
+    assert all(torch.equal(u, v) for u, v in zip((out, lse), run(96, 96, 200)))
+
+
+@gpu
+def test_a_page_chosen_twice_counts_twice(rk):
+    x = Inputs(B=1, Hq=4, H=2, T=2, lens=[300], new=None, page=16).choose(6)
+    x.idx[0, :, :, :] = np.array([3, 7, 3, 17, 3, 7])
+    geom, pages, q, table, lens, args = x.device(rk)
+    out, lse = x.blank()
+    rk.rk_sparse_attn(geom, q, pages, table, i32(x.idx), lens, out, lse=lse, workspace=rk.SparseWorkspace(geom, 2, 6, 16), **args)
+    for g in range(2):
+        K, V, _ = x.rows(0, g)
+        for i in range(2):
+            seen = np.concatenate([np.arange(16 * j, 16 * j + 16) for j in (3, 7, 3, 17, 3, 7)])
+            for h in (2 * g, 2 * g + 1):
+                want, wl, s, size = o.attention(x.q[0, i, h].double().numpy(), K, V, seen, 298 + i, SCALE)
+                # (as Inputs.check, with weights of at most 1 / 96 of each other's sum)
+                assert abs(float(lse[0, i, h]) - wl) <= 140 * 2.0 ** -24 * size.max() + 2.0 ** -20 * (1 + abs(wl))
+                assert np.abs(out[0, i, h].double().cpu().numpy() - want).max() <= 2.0 ** -8 * np.abs(want).max() + (2.0 ** -16 + 300 * 2.0 ** -24 * size.max()) * np.abs(V).max()
