@@ -31,7 +31,9 @@ __device__ __forceinline__ PartRow part_row(const PartSource& s, const PromptPar
 // The running maximum is in units of ln 2 and follows the true one only when that has grown by more than 8 (see prompt_tile).  A chosen token's rows are no more
 // than 8: the upper eight columns repeat them, and hold the weights' low parts beside the high ones of the lower, so that one matrix instruction takes both; and as
 // tokens share rows, which come out of the L2 then, its keys are read in whole rows and turned into the operand's layout by way of LDS: straight into it, every 16
-// lanes of a request touch 16 lines (500 tokens of 28 heads over 4, 32 pages of 64 rows each: @@ us).
+// lanes of a request touch 16 lines (500 tokens of 28 heads over 4, 32 pages of 64 rows each: 163 us so, 126 in whole rows; requests that pass the caches by, as
+// where each row is read once: 294 and 169 us, before that step).  The form without a cap or bias has room for three wavefronts to a SIMD without spilling (124 -> 120 us).
+// What is left there is what the L2s miss: 2.1 GB are asked for, 0.8 GB come from behind them, at 6.5 TB/s.
 constexpr int kTurnRow = kD * 2 + 16, kTurn = kTileRows * kTurnRow;      // (rows of LDS: 16 of an operand fall on different banks)
 template <int W, int ROWS> constexpr int cols_lds() {
     constexpr int merge = (int)sizeof(ColMergeLds<W, 16>), turn = ROWS == kRowsChosen ? W * kTurn : 0;
@@ -311,7 +313,7 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
 }
 
 template <int W, int CAP, bool SLOPE, int ROWS>
-__global__ __launch_bounds__(W * 64, W == kColWaves ? 2 : 1)
+__global__ __launch_bounds__(W * 64, ROWS == kRowsChosen && CAP == kNoCap && !SLOPE ? 3 : W == kColWaves ? 2 : 1)
 void paged_cols_kernel(const PromptParams p) {
     __shared__ __attribute__((aligned(16))) unsigned char room[cols_lds<W, ROWS>()];
     paged_cols<W, CAP, SLOPE, ROWS>(p, (int)blockIdx.x, (int)blockIdx.y, (int)blockIdx.z, room);
@@ -319,8 +321,9 @@ void paged_cols_kernel(const PromptParams p) {
 
 // ---- a shared prefix ----
 // The first `shared_wgs` workgroups go over the shared rows for the queries of all sequences, the others over each sequence's own: in one launch, as the former are
-// bound by the matrix cores and the latter by what they wait for.  Both leave partial results.  OWN: wavefronts to a pair where a sequence's own are
-// columns (two: two pairs to a workgroup), 0: row tiles.
+// bound by the matrix cores and the latter by what they wait for (one token of 64 sequences of 32 heads over 8 behind 8192 rows, 200-1000 rows of their own: 51 us
+// in two launches, 41 in one).  Both leave partial results.  OWN: wavefronts to a pair where a sequence's own are columns, 0: row tiles.  Two, and two pairs to a
+// workgroup, where one workgroup to a pair would be more than the chip has room for beside the shared ones (there: 33.7 -> 31.1 us).
 template <int CAP, bool SLOPE, bool ALL_COLS, int OWN>
 __global__ __launch_bounds__(256, 2)
 void prefix_kernel(const PromptParams all, const PromptParams own, const int32_t shared_wgs, const int32_t own_parts) {
@@ -344,7 +347,9 @@ void prefix_kernel(const PromptParams all, const PromptParams own, const int32_t
 }
 
 // Joins the parts of a row, sum_s 2^(m_s - m) (l_s, o_s).   SOURCES = 2: those over the shared rows, then those over the sequence's own.
-// TEAM wavefronts to a row: one, or where there are many parts four, of which each adds every fourth.
+// TEAM wavefronts to a row: one, or where there are more than 16 parts four, of which each adds every fourth.  One token of 32 heads over 8, one sequence of
+// 32768 rows (the call, one and four): 31.9 and 27.3 us, behind a prefix of 8192 rows 26.7 and 18.2; where rows are many it is equal (64 sequences behind 8192 rows, 7.2
+// and 7.4 us, half of it the launch and the rest the partial results' 17 MB).
 template <int SOURCES, int TEAM>
 __global__ __launch_bounds__(256)
 void paged_merge_kernel(const PromptParams p, const PartSource s0, const PartSource s1) {
@@ -517,7 +522,8 @@ template <bool ALL_COLS, int OWN_COLS> static PrefixKernel prefix_form(int cap, 
         default: return slope ? prefix_kernel<kNoCap, true, ALL_COLS, OWN_COLS> : prefix_kernel<kNoCap, false, ALL_COLS, OWN_COLS>;
     }
 }
-// The workgroups over the shared rows: one to a compute unit, beside those over the sequences' own.
+// The workgroups over the shared rows: one to a compute unit, beside those over the sequences' own (one token of 64 sequences behind 8192 rows: 33.8 us, with
+// two to a compute unit, which both wait for the matrix cores and leave twice the partial results, 44.0).
 static PromptPlan shared_plan(int64_t pairs, int64_t rows, int64_t max_len) {
     PromptPlan f = prompt_plan_of(pairs, rows, max_len, false, false);
     f.alone = false;

@@ -21,11 +21,17 @@ struct ScoreParams {
     const int32_t* pred; int32_t pred_val;
 };
 
-// P: blocks of 16 pages to a wavefront, all of whose bounds are requested at once.  TOKENS: the workgroup's wavefronts have the same pages and every fourth four
-// tokens, so that a query is read and its signs parted once for 16 P pages; otherwise they have pages of their own and all tokens.
-template <int P, bool TOKENS, int AGG>
-__global__ __launch_bounds__(256, P < 4 ? 4 : 2)
+// 64 pages to a wavefront, all of whose bounds are requested at once.  TOKENS: the workgroup's wavefronts have the same pages, by way of LDS, and every fourth four
+// tokens, so that a bound is requested once in whole rows and a query is read and its signs parted once for 64 pages; it also makes four times the
+// workgroups.  Otherwise they have pages of their own and all tokens, which leaves the barrier out and asks for four times as much before the first wait.
+// 32 heads over 8, TOKENS against the other: one token, 1 sequence of 1024 pages 4.0 and 7.1 us, 4 sequences 5.1 and 7.6, 8 sequences 10.2 and 9.3, 16
+// sequences 16.5 and 14.3 (33.6 MB of bounds: 2.3 TB/s of scattered rows of 256 bytes); 16 tokens of 16 sequences 20.3 and 18.9, 32 of 8 15.2 and 17.2, 128 of 16 63.7 and
+// 64.6, 256 of 16 111 and 118; 1000 tokens of 28 heads over 4, 313 pages 11.9 and 20.4.
+constexpr int kScoreBlocks = 4;               // of 16 pages
+template <bool TOKENS, int AGG>
+__global__ __launch_bounds__(256, 2)
 void page_score_kernel(const ScoreParams p) {
+    constexpr int P = kScoreBlocks;
     const uint32_t part = blockIdx.x / (uint32_t)p.Hkv, part_b = part / (uint32_t)p.page_blocks;
     const int g = (int)(blockIdx.x - part * (uint32_t)p.Hkv), lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, gr = lane >> 4;
     const int block = (int)(part - part_b * (uint32_t)p.page_blocks), b = (int)(part_b / (uint32_t)p.chunks), t_first = (int)(part_b - b * (uint32_t)p.chunks) * p.chunk;
@@ -147,14 +153,16 @@ void page_score_kernel(const ScoreParams p) {
     }
 }
 using ScoreKernel = void (*)(const ScoreParams);
-template <int P, bool TOKENS> static ScoreKernel score_kernel(int agg) {
-    return agg == RK_AGG_MAX ? page_score_kernel<P, TOKENS, RK_AGG_MAX> : agg == RK_AGG_MEAN ? page_score_kernel<P, TOKENS, RK_AGG_MEAN> : page_score_kernel<P, TOKENS, RK_AGG_FIRST>;
+template <bool TOKENS> static ScoreKernel score_kernel(int agg) {
+    return agg == RK_AGG_MAX ? page_score_kernel<TOKENS, RK_AGG_MAX> : agg == RK_AGG_MEAN ? page_score_kernel<TOKENS, RK_AGG_MEAN> : page_score_kernel<TOKENS, RK_AGG_FIRST>;
 }
 
 // ---- the pages with the largest ----
 // W wavefronts to a row of up to 64 W R scores, which stay in registers, R to a lane; bound by its chain of instructions.  The threshold is built bit by bit
 // from the top: the largest T with k keys or more at or above it, and as soon as there are k exactly the pages are found (mostly after a third of the 32
-// steps).  Rows of more scores than 16384 go to the long form.
+// steps).  One wavefront needs no exchange for its counts, four have a quarter of the compares each: 128 rows of 313 scores 4.8 us with one, 6.0 with four, of 600 6.6
+// and 6.3, of 1000 9.7 and 7.4; where the rows fill the chip the exchange only costs: 1024 rows of 1000 scores 10.3 and 9.1 us, 2048 rows 10.9 and 12.7, 16384
+// rows 36 and 63.  So one up to 640 scores, four beyond that for up to 1024 rows.  Rows of more scores than 16384 go to the long form.
 constexpr int kSelectThreads = 256, kSelectMost = 16 * 16 * 64;
 struct SelectParams {
     const float* scores; int64_t s_stride;
@@ -338,13 +346,12 @@ extern "C" int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stri
     p.pred = pred; p.pred_val = pred_val;
     const int64_t most = table_width < s_stride ? table_width : s_stride;
     const int64_t pairs = (int64_t)p.Hkv * geom->batch;
-    const bool many = n_new >= 16;
-    // pages to a workgroup: few tokens, 64 or, where those of all pairs still fill the chip, 256
-    const bool wide = many || pairs * ((most + 255) / 256) >= kComputeUnits;
-    const int per = many || !wide ? 64 : 256;
+    // (few tokens, and pages that fill the chip 256 to a workgroup: a wavefront's own; otherwise 64 to a workgroup: see the kernel)
+    const bool tokens = n_new > 16 || pairs * ((most + 255) / 256) < kComputeUnits;
+    const int per = tokens ? 64 : 256;
     p.page_blocks = (int)((most + per - 1) / per);
     const int64_t wgs = p.page_blocks * pairs;
-    const int unit = many ? 16 : 4;           // tokens of a workgroup's round
+    const int unit = tokens ? 16 : 4;           // tokens of a workgroup's round
     int64_t chunks = 2 * kComputeUnits / wgs;
     if (chunks > (n_new + unit - 1) / unit) chunks = (n_new + unit - 1) / unit;
     if (chunks < 1) chunks = 1;
@@ -352,7 +359,7 @@ extern "C" int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stri
     p.chunks = (int)((n_new + p.chunk - 1) / p.chunk);
     const int64_t total = (int64_t)p.page_blocks * p.chunks * geom->batch * p.Hkv;
     if (!fits_launch(total, 256)) return RK_ERR_UNSUPPORTED;
-    auto kernel = many ? score_kernel<4, true>(agg) : wide ? score_kernel<4, false>(agg) : score_kernel<1, false>(agg);
+    auto kernel = tokens ? score_kernel<true>(agg) : score_kernel<false>(agg);
     hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(256), 0, (hipStream_t)stream, p);
     return launch_status();
 }
@@ -372,9 +379,11 @@ extern "C" int rk_page_select(const rk_geom* geom, const float* scores, int64_t 
     p.shift = page_shift(page); p.n_new = n_new; p.Hkv = geom->n_kv_heads; p.k = k; p.keep_first = keep_first; p.keep_last = keep_last;
     p.idx = idx; p.pred = pred; p.pred_val = pred_val;
     const int64_t n = s_stride;
-    auto kernel = n <= 192 ? page_select_kernel<1, 3> : n <= 384 ? page_select_kernel<1, 6> : n <= 640 ? page_select_kernel<1, 10> : n <= 1024 ? page_select_kernel<1, 16> : n <= 4096 ? page_select_kernel<4, 16>
+    const bool four = n > 4096 ? false : n > 1024 || (n > 640 && rows <= 4 * kComputeUnits);
+    auto kernel = n <= 192 ? page_select_kernel<1, 3> : n <= 384 ? page_select_kernel<1, 6> : n <= 640 ? page_select_kernel<1, 10>
+                  : n <= 1024 ? (four ? page_select_kernel<4, 4> : page_select_kernel<1, 16>) : n <= 4096 ? page_select_kernel<4, 16>
                   : n <= kSelectMost ? page_select_kernel<16, 16> : page_select_long_kernel;
-    const int threads = n <= 1024 ? 64 : n <= 4096 ? 256 : n <= kSelectMost ? 1024 : kSelectThreads;
+    const int threads = four || n > kSelectMost ? 256 : n <= 1024 ? 64 : 1024;
     hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, (hipStream_t)stream, p);
     return launch_status();
 }

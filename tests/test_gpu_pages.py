@@ -211,6 +211,11 @@ SCORES = {
     "three_first": (2, 6, 2, 5, [333, 0], [5, 0], 16, "first"),
     "prompt": (1, 7, 1, 200, [200], None, 16, "max"),
     "many_pages": (1, 8, 2, 2, [20000], None, 16, "max"),
+    "many_sequences": (34, 8, 8, 1, [50 + 37 * b for b in range(34)], None, 16, "max"),
+    "many_sequences_seven": (33, 56, 8, 3, [300 + 9 * b for b in range(33)], [b % 4 for b in range(33)], 32, "mean"),
+    "many_sequences_tokens": (32, 16, 8, 16, [700 - 11 * b for b in range(32)], [16] * 31 + [0], 128, "first"),
+    "many_sequences_drafts": (32, 24, 8, 7, [70 * b for b in range(32)], [min(7, 70 * b) for b in range(32)], 16, "max"),
+    "both_many": (32, 16, 8, 17, [500] * 32, None, 16, "mean"),
 }
 
 
@@ -308,3 +313,19 @@ def test_select(rk, B, T, H, W, page, lens, new, k, first, last, values):
             own = (lens[b] - nl[b] + i) // page
             for h in range(H):
                 np.testing.assert_array_equal(got[b, i, h], o.select(x[b, i, h], own, k, first, last), err_msg=str((b, i, h)))
+
+
+@gpu
+@pytest.mark.parametrize("B,T,H,W", [(1, 200, 8, 700), (2, 513, 1, 1024), (1, 129, 8, 641), (1, 128, 8, 641), (3, 1, 4, 1024), (1, 1, 2, 640)])
+def test_select_in_many_and_few_rows(rk, B, T, H, W):
+    say("select in rows", B, T, H, W)
+    geom = rk.Geom(B, H, H, 128, 1.0)
+    r = np.random.default_rng(W + T)
+    x = np.round(r.standard_normal((B, T, H, W)) * 50).astype(np.float32)
+    lens, idx = [W * 16 - 7 * b for b in range(B)], torch.full((B, T, H, 33), 77, dtype=torch.int32, device="cuda")
+    rk.rk_page_select(geom, torch.from_numpy(x).cuda(), 16, i32(lens), 33, idx, keep_first=2, keep_last=2)
+    got = idx.cpu().numpy()
+    for b in range(B):
+        for i in range(T):
+            for h in range(H):
+                np.testing.assert_array_equal(got[b, i, h], o.select(x[b, i, h], (lens[b] - T + i) // 16, 33, 2, 2), err_msg=str((b, i, h)))
