@@ -31,19 +31,21 @@ __device__ __forceinline__ PartRow part_row(const PartSource& s, const PromptPar
 // The running maximum is in units of ln 2 and follows the true one only when that has grown by more than 8 (see prompt_tile).  A chosen token's rows are no more
 // than 8: the upper eight columns repeat them, and hold the weights' low parts beside the high ones of the lower, so that one matrix instruction takes both; and as
 // tokens share rows, which come out of the L2 then, its keys are read in whole rows and turned into the operand's layout by way of LDS: straight into it, every 16
-// lanes of a request touch 16 lines (500 tokens of 28 heads over 4, 32 pages of 64 rows each: 163 us so, 126 in whole rows; requests that pass the caches by, as
-// where each row is read once: 294 and 169 us, before that step).  The form without a cap or bias has room for three wavefronts to a SIMD without spilling (124 -> 120 us).
+// lanes of a request touch 16 lines (500 tokens of 28 heads over 4, 32 pages of 64 rows each: 163 us so, 126 in whole rows).
+// kRowsChosenOnce: few tokens to a page, whose rows pass the caches by as streamed ones do elsewhere.  16 sequences of 32 heads over 8, 64 of 1024 pages of 32 rows for each token, once
+// and kept: 1 token 28.0 and 31.8 us, 4 tokens 81 and 87, 8 tokens 152 and 149, 16 tokens 279 and 233; the 500 tokens 198 and 110.
+// The form without a cap or bias has room for three wavefronts to a SIMD without spilling (124 -> 120 us).
 // What is left there is what the L2s miss: 2.1 GB are asked for, 0.8 GB come from behind them, at 6.5 TB/s.
 constexpr int kTurnRow = kD * 2 + 16, kTurn = kTileRows * kTurnRow;      // (rows of LDS: 16 of an operand fall on different banks)
 template <int W, int ROWS> constexpr int cols_lds() {
-    constexpr int merge = (int)sizeof(ColMergeLds<W, 16>), turn = ROWS == kRowsChosen ? W * kTurn : 0;
+    constexpr int merge = (int)sizeof(ColMergeLds<W, 16>), turn = ROWS == kRowsChosen || ROWS == kRowsChosenOnce ? W * kTurn : 0;
     return merge > turn ? merge : turn;
 }
 template <int W, int CAP, bool SLOPE, int ROWS, int SUB = 1>
 __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, const int y0, const int z0, unsigned char* room) {
     auto leave = [&]() { if constexpr (SUB > 1) __syncthreads(); };
     if (SUB > 1 && x0 < 0) { leave(); return; }
-    constexpr bool CHOSEN = ROWS == kRowsChosen, SHARED = ROWS == kRowsShared;
+    constexpr bool CHOSEN = ROWS == kRowsChosen || ROWS == kRowsChosenOnce, SHARED = ROWS == kRowsShared;
     int b, g, split, slot, parts = p.splits, token = 0;
     if constexpr (CHOSEN) {                   // (KV heads fastest: those of all tokens that share rows meet in few caches)
         g = (int)((uint32_t)x0 % (uint32_t)p.Hkv);
@@ -148,7 +150,7 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
     auto buffer = [&](const uint16_t* base, const Tile& x, int c) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(base) + x.at[c]), 0, x.rows[c] * (kD * 2), 0x00020000);
     };
-    constexpr int kAux = CHOSEN ? 0 : kStreamAux;
+    constexpr int kAux = ROWS == kRowsChosen ? 0 : kStreamAux;
     TileRows<kBf16> rows;
     auto ask_keys = [&](const Tile& x) {
 #pragma unroll
@@ -313,7 +315,7 @@ __device__ __forceinline__ void paged_cols(const PromptParams& p, const int x0, 
 }
 
 template <int W, int CAP, bool SLOPE, int ROWS>
-__global__ __launch_bounds__(W * 64, ROWS == kRowsChosen && CAP == kNoCap && !SLOPE ? 3 : W == kColWaves ? 2 : 1)
+__global__ __launch_bounds__(W * 64, (ROWS == kRowsChosen || ROWS == kRowsChosenOnce) && CAP == kNoCap && !SLOPE ? 3 : W == kColWaves ? 2 : 1)
 void paged_cols_kernel(const PromptParams p) {
     __shared__ __attribute__((aligned(16))) unsigned char room[cols_lds<W, ROWS>()];
     paged_cols<W, CAP, SLOPE, ROWS>(p, (int)blockIdx.x, (int)blockIdx.y, (int)blockIdx.z, room);
@@ -647,7 +649,10 @@ extern "C" int rk_sparse_attn(const rk_geom* geom, const void* q, int64_t q_stri
     set_plan(p, plan);
     if (plan.splits > 1 && !place_parts(p, plan, pairs, p.G, (char*)workspace, workspace_bytes)) return RK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    hipLaunchKernelGGL((cols_form<kColWaves, kRowsChosen>(cap, slope)), dim3((unsigned)(pairs * plan.splits)), dim3(kColWaves * 64), 0, st, p);
+    // (whether tokens meet in a page, for all that is known here: half a token to a page or more)
+    const bool often = n_new > 1 && 2 * (int64_t)n_new * k >= table_width;
+    auto kernel = often ? cols_form<kColWaves, kRowsChosen>(cap, slope) : cols_form<kColWaves, kRowsChosenOnce>(cap, slope);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * plan.splits)), dim3(kColWaves * 64), 0, st, p);
     if ((rc = launch_status()) != RK_OK || plan.splits == 1) return rc;
     const PartSource s = source_of(p, kRowsChosen, p.G);
     return launch_merge<1>(p, s, s, st);

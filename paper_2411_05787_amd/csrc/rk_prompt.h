@@ -47,9 +47,9 @@ struct PromptParams {
 //   kRowsPlain   one behind the other, a buffer of their own;
 //   kRowsPaged   row r in page table[b][r >> shift] of a pool (behind a shared prefix: from row *bound on);
 //   kRowsShared  the first *bound rows, in the pages of one table, the same for the queries of all sequences;
-//   kRowsChosen  the rows of the pages that idx names for a token (rk_paged.hip).
+//   kRowsChosen  the rows of the pages that idx names for a token (rk_paged.hip); kRowsChosenOnce: where few tokens share a page.
 // Tables hold any numbers: a page outside the pool has no rows.
-enum RowsOf { kRowsPlain, kRowsPaged, kRowsShared, kRowsChosen };
+enum RowsOf { kRowsPlain, kRowsPaged, kRowsShared, kRowsChosen, kRowsChosenOnce };
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 

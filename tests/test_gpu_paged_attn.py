@@ -335,6 +335,14 @@ SPARSE = {
     "no_tokens": dict(B=2, Hq=2, H=1, T=2, lens=[0, 40], new=[0, 2], page=32, k=2),
     "negative": dict(B=3, Hq=4, H=2, T=3, lens=[-9, 2, -2 ** 31], new=None, page=16, k=2),
     "eight_heads": dict(B=2, Hq=16, H=2, T=3, lens=[200, 190], new=None, page=16, k=5),
+    "step_capped": dict(B=2, Hq=8, H=2, T=1, lens=[700, 90], new=None, page=16, k=9, cap=4.0),
+    "step_far_cap": dict(B=1, Hq=7, H=1, T=1, lens=[900], new=None, page=32, k=6, cap=200.0),
+    "step_biased": dict(B=1, Hq=16, H=4, T=1, lens=[1500], new=None, page=64, k=12, slopes=True),
+    "few_of_many_pages": dict(B=2, Hq=8, H=2, T=2, lens=[2600, 1900], new=[2, 1], page=16, k=11, cap=150.0, slopes=True),
+    "few_with_holes": dict(B=2, Hq=12, H=2, T=3, lens=[900, 850], new=None, page=16, k=4, masks="holes"),
+    "few_missing": dict(B=2, Hq=8, H=4, T=2, lens=[800, 700], new=None, page=16, missing=5, k=7),
+    "tokens_far_cap": dict(B=1, Hq=6, H=2, T=11, lens=[500], new=None, page=32, k=5, cap=300.0, slopes=True),
+    "tokens_half_a_page": dict(B=1, Hq=8, H=1, T=4, lens=[1024], new=None, page=16, k=8),
 }
 
 
