@@ -739,7 +739,7 @@ int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64
  * table[b * table_width + r / page]; the calls below take the table (device int32 [batch, table_width]) beside the pool.  Sequences may name
  * the same pages (a prefix that they share) as long as none is appended to.  A number outside [0, n_pages) names no page: rows there are not
  * written, and nobody sees them.  Rows from table_width * page on do not exist.
- *   k, v         bf16 [n_pages, n_kv_heads, page, 128], strides in elements (non-negative multiples of 8, the pool within 2^46 of them), 16-byte aligned
+ *   k, v         bf16 [n_pages, n_kv_heads, page, 128], strides in elements (non-negative multiples of 8, the pool within 2^46 of them, stride_h below 2^40), 16-byte aligned
  *   k_min, k_max bf16 [n_pages, n_kv_heads, 128] contiguous, 16-byte aligned, or both NULL: the least and the largest of a page's keys in each dim, in
  *                the order -NaN < -infinity < .. < -0 < +0 < .. < +infinity < NaN (rk_rope_append_paged keeps them, rk_page_scores reads them)
  *   page         16, 32, 64 or 128 (RK_ERR_UNSUPPORTED otherwise) */
@@ -789,7 +789,7 @@ int rk_prefix_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64
  * with q = q[b,i,h,:] and the bounds of page table[b][j]: where scale >= 0 no row of the page scores more with head h.  Sums in fp32; a bound that is infinite or no
  * number makes a score that is +infinity or no number.  A page that the pool does not have: -infinity.  Other entries are left as they were.
  *   agg     RK_AGG_MAX, RK_AGG_MEAN or RK_AGG_FIRST, as in rk_topk_select
- *   scores  fp32 [batch, n_new, n_kv_heads, s_stride] */
+ *   scores  fp32 [batch, n_new, n_kv_heads, s_stride]; n_new is at most 2^30 (RK_ERR_UNSUPPORTED) */
 int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
                    const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens, int32_t agg,
                    float* scores, int64_t s_stride, const int32_t* pred, int32_t pred_val, void* stream);
@@ -797,7 +797,7 @@ int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stride_b, int64
 /* The pages that a token reads: of the N = min(p / page + 1, s_stride) pages of token i (none: N = 0) those with the k largest scores, for every KV
  * head; equal ones, and the last places, to the lower page.  The first keep_first pages and the last keep_last (of p / page + 1: the token's own page is the last)
  * count as +infinity, and so does a score that is no number.  idx int32 [batch, n_new, n_kv_heads, k]: min(k, N) page numbers within the sequence in
- * ascending order, then -1.  Entries of tokens that there are not are left as they were. */
+ * ascending order, then -1.  Entries of tokens that there are not are left as they were.  k * page is below 2^31 - 2^16 (RK_ERR_UNSUPPORTED). */
 int rk_page_select(const rk_geom* geom, const float* scores, int64_t s_stride, int32_t n_new, int32_t page, const int32_t* seq_lens,
                    const int32_t* new_lens, int32_t k, int32_t keep_first, int32_t keep_last, int32_t* idx,
                    const int32_t* pred, int32_t pred_val, void* stream);

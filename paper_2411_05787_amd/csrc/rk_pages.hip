@@ -334,7 +334,7 @@ extern "C" int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stri
     if (rc != RK_OK) return rc;
     if (!q || !seq_lens || !scores || n_new <= 0 || s_stride <= 0 || !aligned16(q) || ((uintptr_t)scores & 3u)) return RK_ERR_INVALID_ARG;
     if (q_stride_b < 0 || q_stride_t < 0 || q_stride_b % 8 != 0 || q_stride_t % 8 != 0) return RK_ERR_INVALID_ARG;
-    if (agg != RK_AGG_MAX && agg != RK_AGG_MEAN && agg != RK_AGG_FIRST) return RK_ERR_UNSUPPORTED;
+    if ((agg != RK_AGG_MAX && agg != RK_AGG_MEAN && agg != RK_AGG_FIRST) || n_new > 1 << 30) return RK_ERR_UNSUPPORTED;      // (tokens are counted past the last in 32 bits)
     if ((rc = check_pages(pages, false, true)) != RK_OK || (rc = check_table(pages, table, table_width)) != RK_OK) return rc;
     ScoreParams p{};
     p.q = (const uint16_t*)q; p.q_b = q_stride_b; p.q_t = q_stride_t;
@@ -372,6 +372,7 @@ extern "C" int rk_page_select(const rk_geom* geom, const float* scores, int64_t 
     if (!scores || !seq_lens || !idx || n_new <= 0 || s_stride <= 0 || k <= 0 || keep_first < 0 || keep_last < 0) return RK_ERR_INVALID_ARG;
     if (((uintptr_t)scores & 3u) || ((uintptr_t)idx & 3u)) return RK_ERR_INVALID_ARG;
     if (page != 16 && page != 32 && page != 64 && page != 128) return RK_ERR_UNSUPPORTED;
+    if ((int64_t)k * page > INT32_MAX - 2 * kMaxChunks * kMinChunk) return RK_ERR_UNSUPPORTED;      // (more than any sequence has, as for rk_sparse_attn)
     const int64_t rows = (int64_t)geom->batch * n_new * geom->n_kv_heads;
     if (!fits_launch(rows, 1024)) return RK_ERR_UNSUPPORTED;
     SelectParams p{};

@@ -62,6 +62,21 @@ def test_refusals_before_any_launch(rk):
     assert select(n=0) == -1 and select(ss=0) == -1 and select(n=2 ** 30) == -2 and select(geom=_Geom(2, 32, 8, 64, 0.1)) == -2
 
 
+def test_refuses_counts_that_32_bits_do_not_step_past(rk):
+    from paper_2411_05787_amd.binding import _Geom, _Pages
+    f = 0x10000
+    g, pages = _Geom(1, 1, 1, 128, 0.1), _Pages(f, f, f, f, 2048, 2048, 8, 16)
+
+    def select(k, page=16):
+        return rk.lib.rk_page_select(C.byref(g), f, 8, 1, page, f, None, k, 0, 1, f, None, 0, None)
+
+    def scores(n):
+        return rk.lib.rk_page_scores(C.byref(g), f, 0, 0, n, C.byref(pages), f, 8, f, None, 0, f, 8, None, 0, None)
+
+    assert select(2 ** 31 - 1) == -2 and select(2 ** 27) == -2 and select(2 ** 24, 128) == -2
+    assert scores(2 ** 30 + 1) == -2 and scores(2 ** 31 - 1) == -2
+
+
 def test_the_oracle_orders_and_selects():
     x = np.array([0xFF80, 0x8000, 0x0000, 0x7F80, 0x7FC0, 0xFFC0, 0xBF80, 0x3F80])
     assert np.argsort(o.in_order(x)).tolist() == [5, 0, 6, 1, 2, 7, 3, 4]
