@@ -161,8 +161,9 @@ template <bool TOKENS> static ScoreKernel score_kernel(int agg) {
 // W wavefronts to a row of up to 64 W R scores, which stay in registers, R to a lane; bound by its chain of instructions.  The threshold is built bit by bit
 // from the top: the largest T with k keys or more at or above it, and as soon as there are k exactly the pages are found (mostly after a third of the 32
 // steps).  One wavefront needs no exchange for its counts, four have a quarter of the compares each: 128 rows of 313 scores 4.8 us with one, 6.0 with four, of 600 6.6
-// and 6.3, of 1000 9.7 and 7.4; where the rows fill the chip the exchange only costs: 1024 rows of 1000 scores 10.3 and 9.1 us, 2048 rows 10.9 and 12.7, 16384
-// rows 36 and 63.  So one up to 640 scores, four beyond that for up to 1024 rows.  Rows of more scores than 16384 go to the long form.
+// and 6.3, of 1000 9.7 and 7.4 (6.9 with two bits at a time); where the rows fill the chip the exchange only costs: 1024 rows of 1000 scores 10.3 and 9.1 us, 2048 rows 10.9 and 12.7, 16384
+// rows 36 and 63.  So one up to 640 scores, four beyond that for up to 1024 rows, and for any beyond 1024 scores.  R only follows the width
+// (16384 rows of 1100 scores with 16 to a lane 169 us, with 8 101).  Rows of more scores than 16384 go to the long form.
 constexpr int kSelectThreads = 256, kSelectMost = 16 * 16 * 64;
 struct SelectParams {
     const float* scores; int64_t s_stride;
@@ -212,33 +213,45 @@ void page_select_kernel(const SelectParams p) {
     uint32_t x[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) { const int j = (w * R + r) * 64 + lane; x[r] = j < n ? select_key(p, row, j, s[r]) : 0u; }
-    __shared__ int sCount[2][W], sBase[W][2];
+    // (few scores to a lane and an exchange: of three thresholds at once, two bits for one exchange.  128 rows of 1000 scores 8.0 -> 7.3 us, of 4000, 16 to a lane,
+    // 11.7 -> 13.9)
+    constexpr int kBits = W > 1 && R <= 4 ? 2 : 1, N = (1 << kBits) - 1;
+    struct Counts { int c[N]; };
+    __shared__ __attribute__((aligned(16))) int sCount[2][W][4];
+    __shared__ int sBase[W][2];
     int turn = 0;
-    // keys of the row at or above v
-    auto count = [&](uint32_t v) {
-        int c = 0;
+    // keys of the row at or above v, v + step, ..
+    auto count = [&](uint32_t v, uint32_t step) {
+        Counts n{};
 #pragma unroll
-        for (int r = 0; r < R; ++r) c += __popcll(__ballot(x[r] >= v));
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r) n.c[i] += __popcll(__ballot(x[r] >= v + i * step));
         if constexpr (W > 1) {
-            if (lane == 0) sCount[turn][w] = c;
+            if (lane < N) sCount[turn][w][lane] = lane == 0 ? n.c[0] : lane == 1 ? n.c[N / 2] : n.c[N - 1];
             lds_barrier();
-            c = 0;
+            n = Counts{};
 #pragma unroll
-            for (int y = 0; y < W; ++y) c += sCount[turn][y];
+            for (int y = 0; y < W; ++y)
+#pragma unroll
+                for (int i = 0; i < N; ++i) n.c[i] += sCount[turn][y][i];
             turn ^= 1;                        // (the next count's words: these may still be read)
-            c = __builtin_amdgcn_readfirstlane(c);
+#pragma unroll
+            for (int i = 0; i < N; ++i) n.c[i] = __builtin_amdgcn_readfirstlane(n.c[i]);
         }
-        return c;
+        return n;
     };
     uint32_t at = 0;
     int above = -1;                           // keys above `at`, where some that equal it stay out
     bool exact = false;
-    for (int bit = 31; bit >= 0 && !exact; --bit) {
-        const uint32_t v = at | 1u << bit;
-        const int c = count(v);
-        if (c >= k) { at = v; exact = c == k; }
+    for (int bit = 32 - kBits; bit >= 0 && !exact; bit -= kBits) {
+        const uint32_t step = 1u << bit, from = at;
+        const Counts n = count(from + step, step);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (n.c[i] >= k) { at = from + (i + 1) * step; exact = n.c[i] == k; }
     }
-    if (!exact) above = at == 0xffffffffu ? 0 : count(at + 1);
+    if (!exact) above = at == 0xffffffffu ? 0 : count(at + 1, 0).c[0];
     const int left = exact ? 0 : k - above;   // of the keys that equal `at`
     int done = 0, ties = 0;
     if constexpr (W > 1) {
@@ -382,7 +395,7 @@ extern "C" int rk_page_select(const rk_geom* geom, const float* scores, int64_t 
     const int64_t n = s_stride;
     const bool four = n > 4096 ? false : n > 1024 || (n > 640 && rows <= 4 * kComputeUnits);
     auto kernel = n <= 192 ? page_select_kernel<1, 3> : n <= 384 ? page_select_kernel<1, 6> : n <= 640 ? page_select_kernel<1, 10>
-                  : n <= 1024 ? (four ? page_select_kernel<4, 4> : page_select_kernel<1, 16>) : n <= 4096 ? page_select_kernel<4, 16>
+                  : n <= 1024 ? (four ? page_select_kernel<4, 4> : page_select_kernel<1, 16>) : n <= 2048 ? page_select_kernel<4, 8> : n <= 4096 ? page_select_kernel<4, 16>
                   : n <= kSelectMost ? page_select_kernel<16, 16> : page_select_long_kernel;
     const int threads = four || n > kSelectMost ? 256 : n <= 1024 ? 64 : 1024;
     hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, (hipStream_t)stream, p);

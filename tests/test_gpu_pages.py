@@ -331,7 +331,7 @@ def test_select(rk, B, T, H, W, page, lens, new, k, first, last, values):
 
 
 @gpu
-@pytest.mark.parametrize("B,T,H,W", [(1, 200, 8, 700), (2, 513, 1, 1024), (1, 129, 8, 641), (1, 128, 8, 641), (3, 1, 4, 1024), (1, 1, 2, 640)])
+@pytest.mark.parametrize("B,T,H,W", [(1, 200, 8, 700), (2, 513, 1, 1024), (1, 129, 8, 641), (1, 128, 8, 641), (3, 1, 4, 1024), (1, 1, 2, 640), (2, 3, 2, 1025), (1, 2, 1, 2048), (1, 2, 2, 2049), (2, 1, 1, 4096), (1, 1, 2, 4097)])
 def test_select_in_many_and_few_rows(rk, B, T, H, W):
     say("select in rows", B, T, H, W)
     geom = rk.Geom(B, H, H, 128, 1.0)
