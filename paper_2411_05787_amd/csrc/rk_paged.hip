@@ -524,6 +524,15 @@ template <bool ALL_COLS, int OWN_COLS> static PrefixKernel prefix_form(int cap, 
         default: return slope ? prefix_kernel<kNoCap, true, ALL_COLS, OWN_COLS> : prefix_kernel<kNoCap, false, ALL_COLS, OWN_COLS>;
     }
 }
+// What is launched, and how many of the sequences' own (pair, part)s a workgroup takes: all columns (a sequence has no more rows than the batch), columns of a
+// sequence, or neither.  Two pairs to a workgroup only where a form of that kind is: the grid goes by what is returned here.
+struct PrefixLaunch { PrefixKernel kernel; int per_wg; };
+static PrefixLaunch prefix_launch(const PromptPlan& all, const PromptPlan& own, int64_t wgs_own, int cap, bool slope) {
+    if (all.cols) return {prefix_form<true, kColWaves>(cap, slope), 1};
+    if (!own.cols) return {prefix_form<false, 0>(cap, slope), 1};
+    if (own.splits == 1 && wgs_own > kComputeUnits) return {prefix_form<false, 2>(cap, slope), 2};
+    return {prefix_form<false, kColWaves>(cap, slope), 1};
+}
 // The workgroups over the shared rows: one to a compute unit, beside those over the sequences' own (one token of 64 sequences behind 8192 rows: 33.8 us, with
 // two to a compute unit, which both wait for the matrix cores and leave twice the partial results, 44.0).
 static PromptPlan shared_plan(int64_t pairs, int64_t rows, int64_t max_len) {
@@ -615,11 +624,8 @@ extern "C" int rk_prefix_attn(const rk_geom* geom, const void* q, int64_t q_stri
     if (workspace_bytes < first || !place_parts(all, plan_all, own.Hkv, all_rows, (char*)workspace, first) ||
         !place_parts(own, plan_own, pairs, rows, (char*)workspace + first, workspace_bytes - first)) return RK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    // (a sequence has no more rows than the batch: columns all, columns of a sequence, or neither)
-    const bool two = plan_own.cols && plan_own.splits == 1 && wgs_own > kComputeUnits;
-    auto kernel = plan_all.cols ? prefix_form<true, kColWaves>(cap, slope) : !plan_own.cols ? prefix_form<false, 0>(cap, slope)
-                  : two ? prefix_form<false, 2>(cap, slope) : prefix_form<false, kColWaves>(cap, slope);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs_all + (two ? (wgs_own + 1) / 2 : wgs_own))), dim3(256), 0, st, all, own, (int32_t)wgs_all, (int32_t)wgs_own);
+    const PrefixLaunch f = prefix_launch(plan_all, plan_own, wgs_own, cap, slope);
+    hipLaunchKernelGGL(f.kernel, dim3((unsigned)(wgs_all + (wgs_own + f.per_wg - 1) / f.per_wg)), dim3(256), 0, st, all, own, (int32_t)wgs_all, (int32_t)wgs_own);
     if ((rc = launch_status()) != RK_OK) return rc;
     return launch_merge<2>(own, source_of(all, kRowsShared, (int)all_rows), source_of(own, kRowsPaged, (int)rows), st);
 }
