@@ -762,7 +762,8 @@ int rk_rope_append_paged(const rk_geom* geom, const rk_new_rows* rows, const rk_
                          void* q_out, const int32_t* pred, int32_t pred_val, void* stream);
 
 /* rk_prompt_attn over a cache in pages: whole prompts, chunks, drafted tokens or a decode step's single token.  Arguments, results and workspace
- * (rk_prompt_workspace_bytes) as there. */
+ * (rk_prompt_workspace_bytes) as there.  RK_ERR_UNSUPPORTED where batch * n_kv_heads * ceil(n_new * G / 128) is 2^24 or more (of 256 rows each where those
+ * are 512 or more and there is neither cap nor slope). */
 int rk_paged_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
                   const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens, int32_t max_len,
                   const rk_prompt_scores* scores, void* out, float* lse, const int32_t* pred, int32_t pred_val,
@@ -776,7 +777,9 @@ size_t rk_prefix_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t max
  * batch: rows j < P of every sequence are those of the pages prefix_table[0 .. prefix_width), rows from P on those of its own table, whose
  * entries for whole pages before P are not looked at.  P = *prefix_len (device int32[1], clamped to [0, min(max_prefix, prefix_width * page)]; any number, also
  * within a page).  seq_lens, positions, first and end count from the prefix's first row, as in rk_paged_attn; a sequence that is shorter than the
- * prefix has its first rows.  max_prefix, max_own: host bounds of P and of seq_lens[b] - P (rows from P + max_own on are not seen). */
+ * prefix has its first rows.  max_prefix, max_own: host bounds of P and of seq_lens[b] - P (rows from P + max_own on are not seen).
+ * RK_ERR_UNSUPPORTED where n_new * G is 2^24 or more, batch * n_new * G 2^31 - 128, or the workgroups of 128 rows (n_kv_heads * ceil(batch * n_new * G / 128)
+ * and batch * n_kv_heads * ceil(n_new * G / 128)) are 2^24 together. */
 int rk_prefix_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
                    const int32_t* prefix_table, int32_t prefix_width, const int32_t* prefix_len, int32_t max_prefix,
                    const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens, int32_t max_own,
@@ -808,7 +811,7 @@ size_t rk_sparse_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t k, 
 
 /* Attention of each new token over some pages of its sequence, its own for every KV head: rk_paged_attn in which the query heads of KV head g see, of
  * the rows that token i sees, those in the pages idx[b,i,g,0 .. k) (numbers within the sequence, as rk_page_select leaves them, in any order; a
- * number outside [0, table_width): no page; one that is there twice counts twice). */
+ * number outside [0, table_width): no page; one that is there twice counts twice).  batch * n_new * n_kv_heads is below 2^24 (RK_ERR_UNSUPPORTED). */
 int rk_sparse_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
                    const int32_t* table, int32_t table_width, const int32_t* idx, int32_t k,
                    const int32_t* seq_lens, const int32_t* new_lens, const rk_prompt_scores* scores, void* out, float* lse,

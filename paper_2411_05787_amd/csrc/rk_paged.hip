@@ -572,7 +572,7 @@ extern "C" int rk_paged_attn(const rk_geom* geom, const void* q, int64_t q_strid
     const bool slope = (scores && scores->slopes) || (geom->scale == 0.f && cap == kNoCap);
     const int64_t pairs = (int64_t)p.batch * p.Hkv, rows = (int64_t)n_new * p.G;
     const PromptPlan plan = prompt_plan(geom, n_new, p.max_len, cap == kNoCap && !slope);
-    if (!fits_launch(pairs * plan.row_tiles * plan.splits, plan.alone ? kColAlone * 64 : 256) || !fits_launch(rows * pairs, 256)) return RK_ERR_UNSUPPORTED;
+    if (!plan.cols && !fits_launch(pairs * plan.row_tiles * plan.splits, 256)) return RK_ERR_UNSUPPORTED;      // (a launch that splits, and so the join, is small)
     set_plan(p, plan);
     if (plan.splits > 1) {
         if (!place_parts(p, plan, pairs, rows, (char*)workspace, workspace_bytes)) return RK_ERR_WORKSPACE;
@@ -617,7 +617,7 @@ extern "C" int rk_prefix_attn(const rk_geom* geom, const void* q, int64_t q_stri
     PromptPlan plan_own = prompt_plan_of(pairs, rows, own.most_own, false, false);
     plan_own.alone = false;
     const int64_t wgs_all = (int64_t)own.Hkv * plan_all.row_tiles * plan_all.splits, wgs_own = pairs * plan_own.row_tiles * plan_own.splits;
-    if (!fits_launch(wgs_all + wgs_own, 256) || !fits_launch(rows * pairs, 256)) return RK_ERR_UNSUPPORTED;
+    if (!fits_launch(wgs_all + wgs_own, 256) || !fits_launch(rows, 256)) return RK_ERR_UNSUPPORTED;      // (the join: up to a workgroup to a row of a pair)
     set_plan(all, plan_all);
     set_plan(own, plan_own);
     const size_t first = paged_scratch(own.Hkv, all_rows, own.most_shared);
@@ -651,7 +651,7 @@ extern "C" int rk_sparse_attn(const rk_geom* geom, const void* q, int64_t q_stri
     const int64_t pairs = (int64_t)p.batch * n_new * p.Hkv;
     PromptPlan plan = prompt_plan_of(pairs, p.G, chosen, false, false);
     plan.alone = false;
-    if (!fits_launch(pairs * plan.splits, 256) || !fits_launch(pairs * p.G, 256)) return RK_ERR_UNSUPPORTED;
+    if (!fits_launch(pairs * plan.splits, 256)) return RK_ERR_UNSUPPORTED;       // (a launch that splits, and so the join, is small)
     set_plan(p, plan);
     if (plan.splits > 1 && !place_parts(p, plan, pairs, p.G, (char*)workspace, workspace_bytes)) return RK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;

@@ -17,7 +17,7 @@ static inline int check_pages(const rk_pages* c, bool rows, bool bounds) {
     if (!aligned16(c->k_min) || !aligned16(c->k_max)) return RK_ERR_INVALID_ARG;
     return RK_OK;
 }
-// What a launch takes: fewer than 2^32 threads.
+// What a launch takes along its first axis: fewer than 2^32 threads.
 static inline bool fits_launch(int64_t workgroups, int64_t threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
 // A table of `width` page numbers to a sequence: its rows are numbered in 32 bits, and the kernels step past the end by up to kMaxChunks * kMinChunk.
 static inline int check_table(const rk_pages* c, const int32_t* table, int32_t width) {

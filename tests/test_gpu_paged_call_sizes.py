@@ -1,0 +1,73 @@
+"""Calls over pages with room for 2^24 rows of queries and more, of which few are there: the same results as from calls with room for these alone, and
+nothing else written."""
+import pytest
+import torch
+
+from test_gpu_paged_attn import SCALE, i32, rk, say  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+B, Hq, H, T, FEW, PAGE, N = 64, 32, 8, 8192, 40, 16, 128
+NEW = [(7 * b) % (FEW + 1) for b in range(B)]
+
+
+def enough():
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GiB")
+
+
+@pytest.fixture(scope="module")
+def pool(rk):  # noqa: F811
+    g = torch.Generator(device="cuda").manual_seed(2)
+    K, V = (torch.randn(B * N // PAGE, H, PAGE, 128, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    table = torch.randperm(B * N // PAGE, generator=g, device="cuda").view(B, -1).int()
+    q = torch.randn(B, FEW, Hq, 128, generator=g, device="cuda").to(torch.bfloat16)
+    return rk.Geom(B, Hq, H, 128, SCALE), rk.Pages(K, V), table, q, i32([N - b % 50 for b in range(B)]), i32(NEW)
+
+
+@pytest.mark.parametrize("kind", ["paged", "sparse", "prefix"])
+def test_attentions(rk, pool, kind):  # noqa: F811
+    say("room for many rows", kind)
+    enough()
+    geom, pages, table, q, lens, new = pool
+    idx = torch.randint(0, N // PAGE, (B, FEW, H, 3), generator=torch.Generator().manual_seed(1), dtype=torch.int32).cuda()
+    if kind == "prefix":                                                         # everybody's first rows are the first sequence's
+        table = table.clone()
+        table[:, :2] = table[0, :2]
+    res = []
+    for n in (FEW, T):
+        qn = torch.zeros(B, n, Hq, 128, dtype=torch.bfloat16, device="cuda")
+        qn[:, :FEW] = q
+        out, lse = torch.full_like(qn, 9.0), torch.full((B, n, Hq), 9.0, device="cuda")
+        if kind == "paged":
+            rk.rk_paged_attn(geom, qn, pages, table, lens, N, out, new_lens=new, lse=lse, workspace=rk.PromptWorkspace(geom, n, N))
+        elif kind == "sparse":
+            ix = torch.zeros(B, n, H, 3, dtype=torch.int32, device="cuda")
+            ix[:, :FEW] = idx
+            rk.rk_sparse_attn(geom, qn, pages, table, ix, lens, out, new_lens=new, lse=lse, workspace=rk.SparseWorkspace(geom, n, 3, PAGE))
+        else:
+            rk.rk_prefix_attn(geom, qn, pages, table[0, :2].contiguous(), i32([30]), 30, table, lens, N, out, new_lens=new, lse=lse, workspace=rk.PrefixWorkspace(geom, n, 30, N))
+        torch.cuda.synchronize()
+        assert n == FEW or bool((out[:, FEW:] == 9).all() and (lse[:, FEW:] == 9).all())
+        res.append((out[:, :FEW].clone(), lse[:, :FEW].clone()))
+        del qn, out, lse
+    # weights as bf16 on both sides, at most 2^-8 of the values' size each, and half a step of the output's; sums and their order in fp32
+    (a, la), (c, lc) = res
+    there = torch.arange(FEW, device="cuda")[None] < new[:, None]
+    assert (c[~there] == 9).all() and (lc[~there] == 9).all()
+    assert (a.double() - c.double()).abs().max() <= 4 * 2.0 ** -8 * float(pages.v.abs().max())
+    none = la == -float("inf")                                                   # (tokens whose chosen pages lie behind them)
+    assert torch.equal(none, lc == -float("inf")) and (la - lc).masked_fill(none, 0.0).abs().max() <= 1e-4
+    if kind != "prefix":
+        b = next(i for i in range(B) if NEW[i])
+        p = int(lens[b]) - NEW[b]
+        rows = torch.arange(N, device="cuda")
+        K, V = (y[table[b].long(), 0].reshape(N, 128).double() for y in (pages.k, pages.v))
+        s = SCALE * K @ q[b, 0, 0].double()
+        seen = rows <= p
+        if kind == "sparse":
+            seen = seen & (rows[:, None] // PAGE == idx[b, 0, 0]).any(dim=1)
+            s = s + torch.log((rows[:, None] // PAGE == idx[b, 0, 0]).sum(dim=1).clamp(min=1).double())      # (a page that is there twice counts twice)
+        s = s.masked_fill(~seen, -float("inf"))
+        want = torch.softmax(s, 0) @ V
+        assert (c[b, 0, 0].double() - want).abs().max() <= 2 * 2.0 ** -8 * float(V.abs().max())
