@@ -800,7 +800,8 @@ int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stride_b, int64
 /* The pages that a token reads: of the N = min(p / page + 1, s_stride) pages of token i (none: N = 0) those with the k largest scores, for every KV
  * head; equal ones, and the last places, to the lower page.  The first keep_first pages and the last keep_last (of p / page + 1: the token's own page is the last)
  * count as +infinity, and so does a score that is no number.  idx int32 [batch, n_new, n_kv_heads, k]: min(k, N) page numbers within the sequence in
- * ascending order, then -1.  Entries of tokens that there are not are left as they were.  k * page is below 2^31 - 2^16 (RK_ERR_UNSUPPORTED). */
+ * ascending order, then -1.  Entries of tokens that there are not are left as they were.  k * page is below 2^31 - 2^16, and batch * n_new * n_kv_heads below
+ * 2^26 for s_stride <= 1024, 2^24 up to 4096 and beyond 16384, 2^22 between them (RK_ERR_UNSUPPORTED). */
 int rk_page_select(const rk_geom* geom, const float* scores, int64_t s_stride, int32_t n_new, int32_t page, const int32_t* seq_lens,
                    const int32_t* new_lens, int32_t k, int32_t keep_first, int32_t keep_last, int32_t* idx,
                    const int32_t* pred, int32_t pred_val, void* stream);

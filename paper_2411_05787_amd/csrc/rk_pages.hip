@@ -387,7 +387,6 @@ extern "C" int rk_page_select(const rk_geom* geom, const float* scores, int64_t 
     if (page != 16 && page != 32 && page != 64 && page != 128) return RK_ERR_UNSUPPORTED;
     if ((int64_t)k * page > INT32_MAX - 2 * kMaxChunks * kMinChunk) return RK_ERR_UNSUPPORTED;      // (more than any sequence has, as for rk_sparse_attn)
     const int64_t rows = (int64_t)geom->batch * n_new * geom->n_kv_heads;
-    if (!fits_launch(rows, 1024)) return RK_ERR_UNSUPPORTED;
     SelectParams p{};
     p.scores = scores; p.s_stride = s_stride; p.seq_lens = seq_lens; p.new_lens = new_lens;
     p.shift = page_shift(page); p.n_new = n_new; p.Hkv = geom->n_kv_heads; p.k = k; p.keep_first = keep_first; p.keep_last = keep_last;
@@ -398,6 +397,7 @@ extern "C" int rk_page_select(const rk_geom* geom, const float* scores, int64_t 
                   : n <= 1024 ? (four ? page_select_kernel<4, 4> : page_select_kernel<1, 16>) : n <= 2048 ? page_select_kernel<4, 8> : n <= 4096 ? page_select_kernel<4, 16>
                   : n <= kSelectMost ? page_select_kernel<16, 16> : page_select_long_kernel;
     const int threads = four || n > kSelectMost ? 256 : n <= 1024 ? 64 : 1024;
+    if (!fits_launch(rows, threads)) return RK_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, (hipStream_t)stream, p);
     return launch_status();
 }

@@ -71,3 +71,22 @@ def test_attentions(rk, pool, kind):  # noqa: F811
         s = s.masked_fill(~seen, -float("inf"))
         want = torch.softmax(s, 0) @ V
         assert (c[b, 0, 0].double() - want).abs().max() <= 2 * 2.0 ** -8 * float(V.abs().max())
+
+
+def test_selection(rk):  # noqa: F811
+    say("room for many rows of scores")
+    enough()
+    b, t, n, k, page, few = 16, 32768, 41, 5, 128, 100
+    geom = rk.Geom(b, Hq, H, 128, SCALE)
+    scores = torch.randn(b, t, H, n, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    lens, new = [n * page - 90 * x for x in range(b)], [few - x for x in range(b)]
+    idx = torch.full((b, t, H, k), 77, dtype=torch.int32, device="cuda")
+    rk.rk_page_select(geom, scores, page, i32(lens), k, idx, new_lens=i32(new), keep_first=1, keep_last=1)
+    for x in range(b):
+        own = (torch.arange(new[x], device="cuda") + lens[x] - new[x]) // page
+        s, j = scores[x, :new[x]].clone(), torch.arange(n, device="cuda")
+        s[..., 0] = float("inf")
+        s.masked_fill_((j == own[:, None])[:, None], float("inf"))
+        s.masked_fill_((j > own[:, None])[:, None], -float("inf"))
+        assert torch.equal(idx[x, :new[x]].long(), s.topk(k, dim=-1).indices.sort(dim=-1).values), x
+        assert (idx[x, new[x]:] == 77).all()

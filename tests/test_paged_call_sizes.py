@@ -38,6 +38,9 @@ def calls():
 
         def sparse(self):
             return lib.rk_sparse_attn(*self.q, C.byref(self.pages), FAR, self.width, FAR, self.k, FAR, None, *self.rest)
+
+        def select(self, n):
+            return lib.rk_page_select(C.byref(self.g), FAR, n, self.T, self.page, FAR, None, self.k, 0, 1, FAR, None, 0, None)
     return Calls
 
 
@@ -53,6 +56,15 @@ def test_whole_prompts(calls, shape):
     assert B * T * Hq >= 1 << 24
     assert x.prompt() != UNSUPPORTED and x.paged() != UNSUPPORTED and x.prefix() != UNSUPPORTED
     assert (x.sparse() == UNSUPPORTED) == (B * T * H > (2 ** 32 - 1) // 256)
+
+
+@pytest.mark.parametrize("n,threads", [(1, 64), (640, 64), (641, 64), (1024, 64), (1025, 256), (4096, 256), (4097, 1024), (16384, 1024), (16385, 256)])
+def test_selection(calls, n, threads):
+    """As many rows of scores as the form that is launched has room for."""
+    most = (2 ** 32 - 1) // threads                                              # of batch * new tokens * KV heads
+    assert calls(1, 1, 1, most, 512).select(n) != UNSUPPORTED
+    assert calls(1, 1, 1, most + 1, 512).select(n) == UNSUPPORTED
+    assert calls(16, 32, 8, 32768, 32768).select(n) == (UNSUPPORTED if threads == 1024 else calls(1, 1, 1, 1, 16).select(n))
 
 
 def test_what_no_launch_holds_is_refused(calls):
