@@ -790,7 +790,8 @@ int rk_prefix_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64
  * sequence b at position p = seq_lens[b] - n + i >= 0 (tokens as in rk_prompt_attn), KV head g and the pages j <= p / page, j < min(table_width, s_stride),
  *     scores[b,i,g,j] = agg over the heads h of g of  scale * sum_d (max(q_d, 0) * k_max_d + min(q_d, 0) * k_min_d)
  * with q = q[b,i,h,:] and the bounds of page table[b][j]: where scale >= 0 no row of the page scores more with head h.  Sums in fp32; a bound that is infinite or no
- * number makes a score that is +infinity or no number.  A page that the pool does not have: -infinity.  Other entries are left as they were.
+ * number makes a score that is +infinity or no number.  A page that the pool does not have, and one behind the table's last (table_width <= j <= p / page,
+ * j < s_stride): -infinity.  Other entries are left as they were.
  *   agg     RK_AGG_MAX, RK_AGG_MEAN or RK_AGG_FIRST, as in rk_topk_select
  *   scores  fp32 [batch, n_new, n_kv_heads, s_stride]; n_new is at most 2^30 (RK_ERR_UNSUPPORTED) */
 int rk_page_scores(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,

@@ -151,6 +151,15 @@ void page_score_kernel(const ScoreParams p) {
             if (j0 + 16 * x + n < seen) to[16 * x] = best[x];
         }
     }
+    // Pages that tokens see behind the table's last one, whose rows do not exist (mostly none): whoever has that page says so.
+    if (p.s_stride <= most || j0 + 16 * P < most || (start + t_end - 1) >> p.shift < most) return;
+    for (int t0 = t_mine; t0 < t_end; t0 += step) {
+        const int i = t0 + gr;
+        if (i >= t_end || start + i < 0) continue;
+        float* to = p.scores + (((int64_t)b * p.n_new + i) * p.Hkv + g) * p.s_stride;
+        const int all = (int)min(((start + i) >> p.shift) + 1, p.s_stride);
+        for (int j = most + n; j < all; j += 16) to[j] = -INFINITY;
+    }
 }
 using ScoreKernel = void (*)(const ScoreParams);
 template <bool TOKENS> static ScoreKernel score_kernel(int agg) {
