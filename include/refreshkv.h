@@ -738,7 +738,8 @@ int rk_prompt_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64
 /* A pool of pages, each with `page` rows of every KV head, for the sequences of any number of batches.  Row r of sequence b is row r % page of page
  * table[b * table_width + r / page]; the calls below take the table (device int32 [batch, table_width]) beside the pool.  Sequences may name
  * the same pages (a prefix that they share) as long as none is appended to.  A number outside [0, n_pages) names no page: rows there are not
- * written, and nobody sees them.  Rows from table_width * page on do not exist.
+ * written, and nobody sees them.  Rows from table_width * page on do not exist.  The steps and selections over C_f and C_p above, the trigger, the full step
+ * with its weights, the gather and the cache of 8 bits know rows one behind the other only: over pages there is the selection of pages, no refreshed small cache.
  *   k, v         bf16 [n_pages, n_kv_heads, page, 128], strides in elements (non-negative multiples of 8, the pool within 2^46 of them, stride_h below 2^40), 16-byte aligned
  *   k_min, k_max bf16 [n_pages, n_kv_heads, 128] contiguous, 16-byte aligned, or both NULL: the least and the largest of a page's keys in each dim, in
  *                the order -NaN < -infinity < .. < -0 < +0 < .. < +infinity < NaN (rk_rope_append_paged keeps them, rk_page_scores reads them)
@@ -775,9 +776,11 @@ size_t rk_prefix_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t max
 
 /* rk_paged_attn for sequences that begin with the same rows (a system prompt, a document that all ask about), which are read once for the whole
  * batch: rows j < P of every sequence are those of the pages prefix_table[0 .. prefix_width), rows from P on those of its own table, whose
- * entries for whole pages before P are not looked at.  P = *prefix_len (device int32[1], clamped to [0, min(max_prefix, prefix_width * page)]; any number, also
+ * entries for whole pages before P have no part.  P = *prefix_len (device int32[1], clamped to [0, min(max_prefix, prefix_width * page)]; any number, also
  * within a page).  seq_lens, positions, first and end count from the prefix's first row, as in rk_paged_attn; a sequence that is shorter than the
  * prefix has its first rows.  max_prefix, max_own: host bounds of P and of seq_lens[b] - P (rows from P + max_own on are not seen).
+ * The softmax weights over the shared rows enter the product with V as bf16 where batch * n_new * G > 16, those over a sequence's own where n_new * G > 16, to
+ * 2^-17 otherwise: a decode step behind a prefix has coarser weights than rk_paged_attn gives it.
  * RK_ERR_UNSUPPORTED where n_new * G is 2^24 or more, batch * n_new * G 2^31 - 128, or the workgroups of 128 rows (n_kv_heads * ceil(batch * n_new * G / 128)
  * and batch * n_kv_heads * ceil(n_new * G / 128)) are 2^24 together. */
 int rk_prefix_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
@@ -813,7 +816,9 @@ size_t rk_sparse_workspace_bytes(const rk_geom* geom, int32_t n_new, int32_t k, 
 
 /* Attention of each new token over some pages of its sequence, its own for every KV head: rk_paged_attn in which the query heads of KV head g see, of
  * the rows that token i sees, those in the pages idx[b,i,g,0 .. k) (numbers within the sequence, as rk_page_select leaves them, in any order; a
- * number outside [0, table_width): no page; one that is there twice counts twice).  batch * n_new * n_kv_heads is below 2^24 (RK_ERR_UNSUPPORTED). */
+ * number outside [0, table_width): no page; one that is there twice counts twice).  Weights enter the product with V to 2^-17.  batch * n_new * n_kv_heads is below
+ * 2^24 (RK_ERR_UNSUPPORTED).  Where n_new > 1, which of two forms is taken (equal results, rows kept in the caches or not) goes by n_new * k and table_width: a table
+ * that is much wider than the sequences can cost time. */
 int rk_sparse_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
                    const int32_t* table, int32_t table_width, const int32_t* idx, int32_t k,
                    const int32_t* seq_lens, const int32_t* new_lens, const rk_prompt_scores* scores, void* out, float* lse,

@@ -322,9 +322,16 @@ void paged_cols_kernel(const PromptParams p) {
 }
 
 // ---- a shared prefix ----
-// The first `shared_wgs` workgroups go over the shared rows for the queries of all sequences, the others over each sequence's own: in one launch, as the former are
-// bound by the matrix cores and the latter by what they wait for (one token of 64 sequences of 32 heads over 8 behind 8192 rows, 200-1000 rows of their own: 51 us
-// in two launches, 41 in one).  Both leave partial results.  OWN: wavefronts to a pair where a sequence's own are columns, 0: row tiles.  Two, and two pairs to a
+// The first `shared_wgs` workgroups go over the shared rows for the queries of all sequences, the others over each sequence's own: in one launch, as both wait more
+// than they work (one token of 64 sequences of 32 heads over 8 behind 8192 rows, 200-1000 rows of their own: 51 us in two launches, 41 in one).  The matrix
+// cores are busy for 4.3 of its 32 us, and for 7.6 of 36 with five tokens of 6 sequences of 28 heads over 4 behind 32777 rows, the vector units for 6 and 8.
+// The shared part, with a row or two of the sequences' own: behind 8192, 16384, 32768, 65536 rows 22.6, 33.0, 56.4, 104.7 us (the drafted tokens
+// 17.7, 21.9, 34.4, 52.4), that is about 12 and 0.65-0.75 for each stage of 32 rows in 256 workgroups.  With one wavefront to a SIMD and requests two stages
+// ahead that is waiting; for which of the reads has not been measured.
+// Weights: where all query rows of a KV head together are more than 16, those over the shared rows meet V as bf16, 2^-8 (prompt_tile, half the matrix instructions of two
+// parts), also where a sequence's own rows are columns, whose weights keep 2^-17 there: errors against 64 bits 0.0023 and 0.0017 of the outputs, the
+// latter all by their own rounding.
+// Both leave partial results.  OWN: wavefronts to a pair where a sequence's own are columns, 0: row tiles.  Two, and two pairs to a
 // workgroup, where one workgroup to a pair would be more than the chip has room for beside the shared ones (there: 33.7 -> 31.1 us).
 template <int CAP, bool SLOPE, bool ALL_COLS, int OWN>
 __global__ __launch_bounds__(256, 2)
@@ -655,7 +662,8 @@ extern "C" int rk_sparse_attn(const rk_geom* geom, const void* q, int64_t q_stri
     set_plan(p, plan);
     if (plan.splits > 1 && !place_parts(p, plan, pairs, p.G, (char*)workspace, workspace_bytes)) return RK_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    // (whether tokens meet in a page, for all that is known here: half a token to a page or more)
+    // (whether tokens meet in a page, for all that is known here: half a token to a page of the table or more.  The pages that there are are the device's to know:
+    // where the table is far wider than those, tokens that do meet are taken for such that do not)
     const bool often = n_new > 1 && 2 * (int64_t)n_new * k >= table_width;
     auto kernel = often ? cols_form<kColWaves, kRowsChosen>(cap, slope) : cols_form<kColWaves, kRowsChosenOnce>(cap, slope);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * plan.splits)), dim3(kColWaves * 64), 0, st, p);

@@ -25,7 +25,7 @@ struct ScoreParams {
 // tokens, so that a bound is requested once in whole rows and a query is read and its signs parted once for 64 pages; it also makes four times the
 // workgroups.  Otherwise they have pages of their own and all tokens, which leaves the barrier out and asks for four times as much before the first wait.
 // 32 heads over 8, TOKENS against the other: one token, 1 sequence of 1024 pages 4.0 and 7.1 us, 4 sequences 5.1 and 7.6, 8 sequences 10.2 and 9.3, 16
-// sequences 16.5 and 14.3 (33.6 MB of bounds: 2.3 TB/s of scattered rows of 256 bytes); 16 tokens of 16 sequences 20.3 and 18.9, 32 of 8 15.2 and 17.2, 128 of 16 63.7 and
+// sequences 16.5 and 14.3 (67.1 MB of bounds: 4.7 TB/s of scattered rows of 256 bytes); 16 tokens of 16 sequences 20.3 and 18.9, 32 of 8 15.2 and 17.2, 128 of 16 63.7 and
 // 64.6, 256 of 16 111 and 118; 1000 tokens of 28 heads over 4, 313 pages 11.9 and 20.4.
 constexpr int kScoreBlocks = 4;               // of 16 pages
 template <bool TOKENS, int AGG>
@@ -169,10 +169,10 @@ template <bool TOKENS> static ScoreKernel score_kernel(int agg) {
 // ---- the pages with the largest ----
 // W wavefronts to a row of up to 64 W R scores, which stay in registers, R to a lane; bound by its chain of instructions.  The threshold is built bit by bit
 // from the top: the largest T with k keys or more at or above it, and as soon as there are k exactly the pages are found (mostly after a third of the 32
-// steps).  One wavefront needs no exchange for its counts, four have a quarter of the compares each: 128 rows of 313 scores 4.8 us with one, 6.0 with four, of 600 6.6
-// and 6.3, of 1000 9.7 and 7.4 (6.9 with two bits at a time); where the rows fill the chip the exchange only costs: 1024 rows of 1000 scores 10.3 and 9.1 us, 2048 rows 10.9 and 12.7, 16384
-// rows 36 and 63.  So one up to 640 scores, four beyond that for up to 1024 rows, and for any beyond 1024 scores.  R only follows the width
-// (16384 rows of 1100 scores with 16 to a lane 169 us, with 8 101).  Rows of more scores than 16384 go to the long form.
+// steps).  One wavefront needs no exchange for its counts, four have a quarter of the compares each: 128 rows of 313 scores 4.7 us with one, 6.4 with four, of 600 6.4
+// and 6.4, of 1000 9.3 and 6.8; where the rows fill the chip the exchange only costs: 1024 rows of 1000 scores 10.1 and 9.7 us, 2048 rows 10.8 and 13.9, 16384
+// rows 36 and 73.  So one up to 640 scores, four beyond that for up to 1024 rows, and for any beyond 1024 scores.  R only follows the width
+// (with 16 to a lane and 8: 128 rows of 2000 scores 11.8 and 8.8 us, 16384 rows of 1100 156 and 93).  Rows of more scores than 16384 go to the long form.
 constexpr int kSelectThreads = 256, kSelectMost = 16 * 16 * 64;
 struct SelectParams {
     const float* scores; int64_t s_stride;
@@ -222,8 +222,8 @@ void page_select_kernel(const SelectParams p) {
     uint32_t x[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) { const int j = (w * R + r) * 64 + lane; x[r] = j < n ? select_key(p, row, j, s[r]) : 0u; }
-    // (few scores to a lane and an exchange: of three thresholds at once, two bits for one exchange.  128 rows of 1000 scores 8.0 -> 7.3 us, of 4000, 16 to a lane,
-    // 11.7 -> 13.9)
+    // (few scores to a lane and an exchange: of three thresholds at once, two bits for one exchange.  One bit at a time and two: 128 rows of 1000 scores 6.8 and 6.6 us,
+    // 512 rows 7.9 and 8.0, 1024 rows 9.15 and 9.8; of 4000, 16 to a lane, 11.6 and 13.9)
     constexpr int kBits = W > 1 && R <= 4 ? 2 : 1, N = (1 << kBits) - 1;
     struct Counts { int c[N]; };
     __shared__ __attribute__((aligned(16))) int sCount[2][W][4];

@@ -90,3 +90,22 @@ def test_selection(rk):  # noqa: F811
         s.masked_fill_((j > own[:, None])[:, None], -float("inf"))
         assert torch.equal(idx[x, :new[x]].long(), s.topk(k, dim=-1).indices.sort(dim=-1).values), x
         assert (idx[x, new[x]:] == 77).all()
+
+
+@pytest.mark.parametrize("T", [2, 5, 30])
+def test_a_wider_table_changes_no_bit(rk, T):  # noqa: F811
+    """The form that keeps chosen rows in the caches and the one that passes them by, which a table's width decides between."""
+    say("chosen pages of a wider table", T)
+    geom, g = rk.Geom(3, 16, 4, 128, SCALE), torch.Generator().manual_seed(5)
+    K, V = (torch.randn(3 * 20, 4, PAGE, 128, generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    table, q = torch.randperm(60, generator=g).view(3, 20).int(), torch.randn(3, T, 16, 128, generator=g).to(torch.bfloat16).cuda()
+    idx = torch.randint(0, 20, (3, T, 4, 6), generator=g, dtype=torch.int32).cuda()
+    outs = []
+    for width in (20, 4000):
+        wide = torch.full((3, width), -1, dtype=torch.int32)
+        wide[:, :20] = table
+        out, lse = torch.zeros_like(q), torch.zeros(3, T, 16, device="cuda")
+        rk.rk_sparse_attn(geom, q, rk.Pages(K, V), wide.cuda(), idx, i32([320, 300, 111]), out, lse=lse, workspace=rk.SparseWorkspace(geom, T, 6, PAGE))
+        assert (2 * T * 6 >= width) == (width == 20)
+        outs.append((out, lse))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
