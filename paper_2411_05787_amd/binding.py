@@ -1051,6 +1051,14 @@ class Pages:
         return cls(new(n_pages, H, page, D), new(n_pages, H, page, D), *((new(n_pages, H, D), new(n_pages, H, D)) if bounds else ()))
 
 
+def _i32(x, name: str) -> int:
+    """A host number that the C call takes in 32 bits (ctypes would drop the bits above)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError("%s = %d is beyond 32 bits" % (name, x))
+    return x
+
+
 def _pool(geom: Geom, pages: Pages) -> torch.Tensor:
     """One tensor of the pool, once it is known to be of this geometry."""
     if not isinstance(pages, Pages):
@@ -1084,7 +1092,7 @@ def rk_rope_append_paged(geom: Geom, q, k, v, rope: Optional[Rope], pages: Pages
     dev = _same_device(k, q, v, None if rope is None else rope.table, _pool(geom, pages), table, seq_lens, q_out, new_lens, positions, pred)
     tp, width = _page_table(table, geom.batch)
     _launch("rk_rope_append_paged", dev, stream, C.byref(geom.c()), rows, r, pos, C.byref(pages._c), tp, width, lens, new, qo,
-            _dev(pred, torch.int32, "pred", (geom.batch,), optional=True), int(pred_val))
+            _dev(pred, torch.int32, "pred", (geom.batch,), optional=True), _i32(pred_val, "pred_val"))
 
 
 class PrefixWorkspace:
@@ -1105,7 +1113,7 @@ class SparseWorkspace:
 
 
 def _scratch(ws, name: str, sizes: tuple, device) -> None:
-    ws.nbytes = int(getattr(lib, name)(C.byref(ws.geom.c()), *(int(x) for x in sizes)))
+    ws.nbytes = int(getattr(lib, name)(C.byref(ws.geom.c()), *(_i32(x, "a size") for x in sizes)))
     if ws.nbytes == 0:
         raise RkError(name, -1)
     ws.buf = torch.empty(ws.nbytes + 256, dtype=torch.uint8, device=device)
@@ -1120,7 +1128,7 @@ def _attention_rest(geom: Geom, T: int, first, end, cap, slopes, out, lse, pred,
                            _dev(first, torch.int32, "first", (B, T), optional=True), _dev(end, torch.int32, "end", (B, T), optional=True))
     ws, nb = (None, 0) if workspace is None else (workspace.ptr, workspace.nbytes)
     return (C.byref(scores), _dev(out, torch.bfloat16, "out", (B, T, Hq, D)), _dev(lse, torch.float32, "lse", (B, T, Hq), optional=True),
-            _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val), ws, nb)
+            _dev(pred, torch.int32, "pred", (B,), optional=True), _i32(pred_val, "pred_val"), ws, nb)
 
 
 def rk_paged_attn(geom: Geom, q, pages: Pages, table, seq_lens, max_len: int, out, new_lens=None, first=None, end=None, cap: float = 0.0,
@@ -1136,7 +1144,7 @@ def rk_paged_attn(geom: Geom, q, pages: Pages, table, seq_lens, max_len: int, ou
     if max_len > width * pages.page:
         raise ValueError("max_len %d exceeds the table's %d pages of %d rows" % (max_len, width, pages.page))
     _launch("rk_paged_attn", dev, stream, C.byref(geom.c()), qp, sb, st, T, C.byref(pages._c), tp, width,
-            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(max_len),
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), _i32(max_len, "max_len"),
             *_attention_rest(geom, T, first, end, cap, slopes, out, lse, pred, pred_val, workspace))
 
 
@@ -1154,13 +1162,13 @@ def rk_prefix_attn(geom: Geom, q, pages: Pages, prefix_table, prefix_len, max_pr
     dev = _same_device(_pool(geom, pages), q, prefix_table, prefix_len, table, seq_lens, out, new_lens, first, end, slopes, lse, pred, workspace.buf)
     qp, sb, st, T = _queries(geom, q)
     tp, width = _page_table(table, B)
-    if prefix_table.dim() != 1:
+    if not isinstance(prefix_table, torch.Tensor) or prefix_table.dim() != 1:
         raise ValueError("prefix_table must be [pages of the prefix]")
     if max_prefix > prefix_table.shape[0] * pages.page:
         raise ValueError("max_prefix %d exceeds the prefix's %d pages of %d rows" % (max_prefix, prefix_table.shape[0], pages.page))
     _launch("rk_prefix_attn", dev, stream, C.byref(geom.c()), qp, sb, st, T, C.byref(pages._c), _dev(prefix_table, torch.int32, "prefix_table"),
-            prefix_table.shape[0], _dev(prefix_len, torch.int32, "prefix_len", (1,)), int(max_prefix), tp, width,
-            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(max_own),
+            prefix_table.shape[0], _dev(prefix_len, torch.int32, "prefix_len", (1,)), _i32(max_prefix, "max_prefix"), tp, width,
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), _i32(max_own, "max_own"),
             *_attention_rest(geom, T, first, end, cap, slopes, out, lse, pred, pred_val, workspace))
 
 
@@ -1176,12 +1184,12 @@ def rk_page_scores(geom: Geom, q, pages: Pages, table, seq_lens, scores, new_len
         raise ValueError("the pool keeps no bounds of its pages")
     qp, sb, st, T = _queries(geom, q)
     tp, width = _page_table(table, B)
-    if scores.dim() != 4:
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 4:
         raise ValueError("scores must be [batch, n_new, n_kv_heads, pages]")
     _launch("rk_page_scores", dev, stream, C.byref(geom.c()), qp, sb, st, T, C.byref(pages._c), tp, width,
-            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(agg),
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), _i32(agg, "agg"),
             _dev(scores, torch.float32, "scores", (B, T, H, scores.shape[3])), scores.shape[3],
-            _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val))
+            _dev(pred, torch.int32, "pred", (B,), optional=True), _i32(pred_val, "pred_val"))
 
 
 def rk_page_select(geom: Geom, scores, page: int, seq_lens, k: int, idx, new_lens=None, keep_first: int = 0, keep_last: int = 1, pred=None,
@@ -1195,9 +1203,9 @@ def rk_page_select(geom: Geom, scores, page: int, seq_lens, k: int, idx, new_len
         raise ValueError("scores must be [batch, n_new, n_kv_heads, pages]")
     dev = _same_device(scores, seq_lens, idx, new_lens, pred)
     T, width = scores.shape[1], scores.shape[3]
-    _launch("rk_page_select", dev, stream, C.byref(geom.c()), _dev(scores, torch.float32, "scores", (B, T, H, width)), width, T, int(page),
-            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), int(k), int(keep_first),
-            int(keep_last), _dev(idx, torch.int32, "idx", (B, T, H, k)), _dev(pred, torch.int32, "pred", (B,), optional=True), int(pred_val))
+    _launch("rk_page_select", dev, stream, C.byref(geom.c()), _dev(scores, torch.float32, "scores", (B, T, H, width)), width, T, _i32(page, "page"),
+            _dev(seq_lens, torch.int32, "seq_lens", (B,)), _dev(new_lens, torch.int32, "new_lens", (B,), optional=True), _i32(k, "k"), _i32(keep_first, "keep_first"),
+            _i32(keep_last, "keep_last"), _dev(idx, torch.int32, "idx", (B, T, H, k)), _dev(pred, torch.int32, "pred", (B,), optional=True), _i32(pred_val, "pred_val"))
 
 
 def rk_sparse_attn(geom: Geom, q, pages: Pages, table, idx, seq_lens, out, new_lens=None, first=None, end=None, cap: float = 0.0, slopes=None,
@@ -1210,7 +1218,7 @@ def rk_sparse_attn(geom: Geom, q, pages: Pages, table, idx, seq_lens, out, new_l
     dev = _same_device(_pool(geom, pages), q, table, idx, seq_lens, out, new_lens, first, end, slopes, lse, pred, None if workspace is None else workspace.buf)
     qp, sb, st, T = _queries(geom, q)
     tp, width = _page_table(table, B)
-    if idx.dim() != 4:
+    if not isinstance(idx, torch.Tensor) or idx.dim() != 4:
         raise ValueError("idx must be [batch, n_new, n_kv_heads, k]")
     _launch("rk_sparse_attn", dev, stream, C.byref(geom.c()), qp, sb, st, T, C.byref(pages._c), tp, width,
             _dev(idx, torch.int32, "idx", (B, T, geom.n_kv_heads, idx.shape[3])), idx.shape[3],
