@@ -763,8 +763,8 @@ int rk_rope_append_paged(const rk_geom* geom, const rk_new_rows* rows, const rk_
                          void* q_out, const int32_t* pred, int32_t pred_val, void* stream);
 
 /* rk_prompt_attn over a cache in pages: whole prompts, chunks, drafted tokens or a decode step's single token.  Arguments, results and workspace
- * (rk_prompt_workspace_bytes) as there.  RK_ERR_UNSUPPORTED where batch * n_kv_heads * ceil(n_new * G / 128) is 2^24 or more (of 256 rows each where those
- * are 512 or more and there is neither cap nor slope). */
+ * (rk_prompt_workspace_bytes) as there.  RK_ERR_UNSUPPORTED where n_new * G > 16 and batch * n_kv_heads * ceil(n_new * G / 128) is 2^24 or more (of 256
+ * rows each where those are 512 or more and there is neither cap nor slope). */
 int rk_paged_attn(const rk_geom* geom, const void* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_new, const rk_pages* pages,
                   const int32_t* table, int32_t table_width, const int32_t* seq_lens, const int32_t* new_lens, int32_t max_len,
                   const rk_prompt_scores* scores, void* out, float* lse, const int32_t* pred, int32_t pred_val,

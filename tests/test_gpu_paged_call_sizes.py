@@ -109,3 +109,20 @@ def test_a_wider_table_changes_no_bit(rk, T):  # noqa: F811
         assert (2 * T * 6 >= width) == (width == 20)
         outs.append((out, lse))
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_more_threads_than_32_bits_count(rk):  # noqa: F811
+    """A token of as many sequences and KV heads as make 2^32 threads and more, along three axes: equal keys, so each output is the mean of the values seen."""
+    say("2^32 threads")
+    enough()
+    b, h = 65535, 300
+    assert b * h * 256 >= 1 << 32
+    V = torch.arange(16, device="cuda").to(torch.bfloat16)[None, None, :, None].expand(1, h, 16, 128).contiguous()
+    pool = rk.Pages(torch.zeros_like(V), V)
+    q = torch.ones(b, 1, h, 128, dtype=torch.bfloat16, device="cuda")
+    lens = torch.arange(b, device="cuda", dtype=torch.int32) % 16 + 1
+    out = torch.full_like(q, 99.0)
+    rk.rk_paged_attn(rk.Geom(b, h, h, 128, SCALE), q, pool, torch.zeros(b, 1, dtype=torch.int32, device="cuda"), lens, 16, out)
+    torch.cuda.synchronize()
+    want = ((lens - 1).float() / 2).to(torch.bfloat16)
+    assert bool((out == want[:, None, None, None]).all())
